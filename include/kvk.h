@@ -386,6 +386,27 @@ kvk_status kvk_append_token(const kvk_table* table, int32_t layer_begin, int32_t
                             const void* k, const void* v, int32_t in_dtype, int32_t n_stored,
                             void* arena, hipStream_t stream);
 
+/* Append of a chunk of new tokens to every anchor layer in [layer_begin, layer_end), GQA
+ * tables: draft tokens, a chunk of a long prompt, the prompts of a batch of different lengths.
+ * The streams are left as n_new[b] calls of kvk_append_token would leave them, bit for bit
+ * (every token passes through the bf16 window, so fp32 inputs are rounded to bf16 first).
+ *   k, v     : device [layer_end-layer_begin][B][Hkv][n_chunk][d_h], dtype in_dtype; of
+ *              sequence b the first n_new[b] tokens (rows of inheriting layers and tokens past
+ *              n_new[b] are not read).
+ *   n_stored : host [B], tokens stored per stream of each sequence before the call.
+ *   n_new    : host [B], tokens appended per sequence, 0..n_chunk, n_stored[b] + n_new[b] at
+ *              most the capacity; NULL: n_chunk for every sequence.
+ *   arena    : device; only full blocks n_stored[b]/32 .. (n_stored[b] + n_new[b])/32 - 1 and
+ *              the tails are written.  Tail slots past the last token are left undefined.
+ * Sequences of different lengths: at most KVK_MAX_BATCH_PLANS (any number of equal ones).  The
+ * host arrays are read before the call returns.
+ * Errors: KVK_ERR_INVALID (range, lengths, NULL pointers, dtype, misalignment: k, v and arena
+ *         16 B, host memory), KVK_ERR_UNSUPPORTED (MLA table: kvk_append_token; sequences of
+ *         different lengths beyond the limit), KVK_ERR_DEVICE. */
+kvk_status kvk_append_chunk(const kvk_table* table, int32_t layer_begin, int32_t layer_end, const void* k, const void* v,
+                            int32_t in_dtype, int32_t n_chunk, const int32_t* n_stored, const int32_t* n_new,
+                            void* arena, hipStream_t stream);
+
 /* Query-aware keep list of one anchor layer at prefill, for a table that evicts
  * (keep_tokens > 0): the eviction the paper composes with its configurations
  * (§3.4: the configurations drop no positions, so an evictor runs on the same
@@ -444,6 +465,69 @@ kvk_status kvk_snapkv_select_mla(const kvk_table* table, int32_t layer, const vo
 kvk_status kvk_snapkv_select(const kvk_table* table, int32_t layer, const void* k, const void* q_obs,
                              int32_t in_dtype, int32_t n_tokens, float scale, int32_t* keep_out,
                              float* importance, void* workspace, size_t ws_bytes, hipStream_t stream);
+
+/* How a tensor of rows lies in memory: token t of sequence s, head h, starts at element
+ * s * seq + h * head + t * token (seq > 0: one place per sequence, a padded batch) or, with
+ * seq = 0, at h * head + (rows of the sequences before s + t) * token (packed).  A row's
+ * head_dim elements are contiguous.  Strides are non-negative multiples of 8 elements; a head
+ * stride of 0 reads the same row for every head. */
+typedef struct {
+  int64_t seq, head, token;
+} kvk_strides;
+
+/* Attention of whole prompts at prefill: every token attends to the tokens of its own
+ * sequence up to itself, softmax(scale q.k) v, with grouped heads (query head h reads KV head
+ * h / (Hq / Hkv)).  Sequences of different lengths run in one launch.
+ *   seq_tokens: host [n_seqs], tokens of each sequence (0 allowed); n_seqs 1..KVK_MAX_BATCH_PLANS.
+ *   q, k, v   : device bf16; head_dim 64 or 128.
+ *   strides   : host [4] of q, k, v and out; NULL: packed rows [tokens][heads][head_dim] each.
+ *   out       : device bf16, Hq heads; only the rows of the sequences' tokens are written.
+ *   lse       : NULL, or device fp32: ln sum_t exp(scale q.k_t) of every row, per sequence
+ *               [Hq][tokens], one sequence after another (a batch of one length: [B][Hq][n]).
+ * Scores and sums are fp32; the probabilities enter the second product in bf16, hence the
+ * bf16 output.  Later tokens of a sequence (and whatever lies past it) do not reach a row,
+ * infinities and NaN among them.  A row whose visible scores are all -inf yields NaN and the
+ * log-sum-exp -inf, a row that sees a NaN score yields NaN.
+ * Errors: KVK_ERR_INVALID (sizes, strides, NULL, misalignment: q, k, v and out 16 B, lse 4 B;
+ *         a scale that is not finite; host memory), KVK_ERR_UNSUPPORTED (head_dim, n_seqs),
+ *         KVK_ERR_DEVICE. */
+kvk_status kvk_prompt_attention(int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t n_seqs,
+                                const int32_t* seq_tokens, const void* q, const void* k, const void* v,
+                                const kvk_strides* strides, float scale, void* out, float* lse, hipStream_t stream);
+
+/* The attention weight that each position of a prompt collects: for KV head j and token t
+ *   weight = sum over the query heads of j and the rows i >= t of exp(scale q_i.k_t - lse_i),
+ * the column sums of the prompt's attention probabilities, on which eviction by accumulated
+ * weight goes (the evictors of App. F.3 that sum over all queries; kvk_snapkv_select sums
+ * over a window).  kvk_keep_heaviest turns the weights into a keep list.
+ *   q, k, strides [2], seq_tokens: as for kvk_prompt_attention.
+ *   lse       : device fp32, as kvk_prompt_attention returns it (same scale).
+ *   weight    : device fp32, per sequence [Hkv][tokens], one sequence after another.
+ *   workspace : device, >= kvk_attention_weight_workspace_bytes(...), 256-byte aligned (NULL
+ *               where that is 0: one query head per KV head).
+ * Sums are fp32 in a fixed order (two calls give the same bits).
+ * Errors: those of kvk_prompt_attention, KVK_ERR_BUFFER (workspace). */
+kvk_status kvk_attention_weight_workspace_bytes(int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t n_seqs,
+                                                const int32_t* seq_tokens, size_t* out_bytes);
+kvk_status kvk_attention_weight(int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t n_seqs,
+                                const int32_t* seq_tokens, const void* q, const void* k, const kvk_strides* strides,
+                                const float* lse, float scale, float* weight, void* workspace, size_t ws_bytes,
+                                hipStream_t stream);
+
+/* The keep list of the heaviest positions, for a table that evicts (keep_tokens > 0): the last
+ * n_recent positions and the keep_tokens - n_recent earlier ones of largest weight (equal
+ * weights: the lower position), in increasing order.  The result is kvk_compress_layer's
+ * keep_idx.
+ *   weight   : device fp32 [streams][n_tokens], streams = B * Hkv (GQA) or B (MLA):
+ *              kvk_attention_weight's, an importance of kvk_snapkv_select, or a sum of such.
+ *              Negative weights are allowed; a NaN weight ranks below every other.
+ *   n_tokens : keep_tokens .. max_tokens.
+ *   n_recent : 0 .. keep_tokens.
+ *   keep_out : device int32 [streams][keep_tokens].
+ * Errors: KVK_ERR_INVALID (table without eviction, sizes, NULL pointers, misalignment, host
+ *         memory), KVK_ERR_DEVICE. */
+kvk_status kvk_keep_heaviest(const kvk_table* table, const float* weight, int32_t n_tokens, int32_t n_recent,
+                             int32_t* keep_out, hipStream_t stream);
 
 /* The selector's forward pass (§2.3; App. B "Selector architecture"): the prompt's
  * token embeddings (the backbone's own) -> a linear map to width 256 -> two
@@ -586,6 +670,35 @@ kvk_status kvk_decode_attention_noalloc(const kvk_table* table, int32_t layer_be
                                         const void* q, int32_t q_dtype, int32_t n_stored, float scale,
                                         const void* w_uk, const void* w_uv, const void* arena, float* out,
                                         hipStream_t stream);
+
+/* Attention of a chunk of new tokens over GQA caches that already hold them (after
+ * kvk_append_chunk or kvk_append_token): verification of draft tokens, chunked prefill, and,
+ * with one token each, decoding of sequences of different lengths.  Row i of the n_new[b] rows
+ * of sequence b is its stored token n_stored[b] - n_new[b] + i and attends to the stored tokens
+ * up to itself, as they are stored: a token whose 32-token group is complete in its quantised
+ * form, for the group's own rows too.  Layers of [layer_begin, layer_end) that share an anchor
+ * are served by one read of it.
+ *   q        : device bf16 [layer_end-layer_begin][B][Hq][n_chunk][d_h]; n_chunk 1..capacity.
+ *   n_stored : host [B], tokens stored per stream of each sequence, the chunk among them.
+ *   n_new    : host [B], rows of each sequence, 0..min(n_chunk, n_stored[b]); NULL: n_chunk.
+ *   scale    : softmax scale, finite.
+ *   out      : device bf16, as q; rows past n_new[b] are left as they were.
+ *   workspace: device, >= kvk_chunk_workspace_bytes of the range and n_chunk, 256-byte
+ *              aligned; its contents on entry are ignored.  Calls that overlap on one
+ *              workspace race.
+ * Per-sequence tables need no set-up.  Quantised layers are dequantised to fp16: their values
+ * and the queries on them must lie in the fp16 range.  Scores, sums and outputs are
+ * accumulated in fp32.  Tokens a row does not see (and stale slots) do not reach it,
+ * infinities and NaN among them.  The host arrays are read before the call returns.
+ * Errors: KVK_ERR_INVALID (range, lengths, scale, NULL pointers, misalignment: q, arena and out
+ *         16 B, workspace 256 B; host memory), KVK_ERR_UNSUPPORTED (MLA table; a batch beyond
+ *         65535), KVK_ERR_BUFFER (workspace), KVK_ERR_DEVICE. */
+kvk_status kvk_chunk_workspace_bytes(const kvk_table* table, int32_t layer_begin, int32_t layer_end, int32_t n_chunk,
+                                     size_t* out_bytes);
+kvk_status kvk_chunk_attention(const kvk_table* table, int32_t layer_begin, int32_t layer_end, const void* q,
+                               int32_t n_chunk, const int32_t* n_stored, const int32_t* n_new, float scale,
+                               const void* arena, void* out, void* workspace, size_t workspace_bytes,
+                               hipStream_t stream);
 
 /* Algorithmic bytes one decode call over [layer_begin, layer_end) reads from the
  * arena with n_stored tokens per stream: each distinct anchor's full blocks and

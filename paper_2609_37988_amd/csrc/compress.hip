@@ -811,6 +811,129 @@ __global__ __launch_bounds__(128) void group_write_kernel(AppendArgs a) {
 #undef KVK_GROUP_BITS
 }
 
+// A chunk of new tokens to every anchor of a layer range: what as many calls of the kernels
+// above would leave, at once.
+constexpr int kChunkItems = 56;  // items per launch
+constexpr int kChunkSeqs = KVK_MAX_BATCH_PLANS;
+
+struct ChunkWriteArgs {
+  const void* k;        // [rows][B][Hkv][m][D]
+  const void* v;
+  uint8_t* arena;
+  int32_t in_f32;
+  int32_t m;            // tokens of a sequence in the inputs
+  int32_t nb_cap, Hkv;
+  int32_t n_streams;    // streams per item: B * Hkv, or Hkv under per-sequence plans
+  int32_t units;        // blocks of a stream that the launch provides for
+  int64_t row_stride;   // elements between the rows of consecutive layers in k and v
+  int32_t uniform;      // every sequence as the first
+  int32_t pos[kChunkSeqs], fresh[kChunkSeqs];  // per sequence: tokens stored before the call, new ones
+  AppendItem items[kChunkItems];
+};
+static_assert(sizeof(ChunkWriteArgs) <= 4096, "kernel arguments");
+
+// One wave writes the keys or the values of one block that the chunk touches (of two blocks at
+// d_h 64).  Unit u of a stream is block pos / 32 + u.  A block that the chunk fills is quantised
+// from its bf16 tokens, the first one's from the tail and the chunk together; its wave also
+// writes what is left over to the tail, after it has read it.  A chunk that stays in the tail
+// only adds its tokens to it.
+template <int D, int QS>
+__global__ __launch_bounds__(128) void chunk_write_kernel(ChunkWriteArgs a) {
+  using L = Lanes<D>;
+  constexpr int kImg = kImageBytes<D, 8, QS>;
+  __shared__ __align__(16) uint8_t img_all[2 * L::kBlocks * kImg];
+  const int lane = threadIdx.x & 63, part = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);  // 0: keys, 1: values
+  const int l = lane % L::kPerBlock, q = l % L::kQ, tg = l / L::kQ, sub = lane / L::kPerBlock;
+  const uint32_t id = blockIdx.x * L::kBlocks + sub;
+  if (id >= (uint32_t)a.n_streams * (uint32_t)a.units) return;
+  const int sidx = id / (uint32_t)a.units, u = id - (uint32_t)sidx * a.units;
+  const AppendItem& it = a.items[blockIdx.y];
+  const int seq = a.uniform ? 0 : (it.s0 + sidx) / a.Hkv;
+  const int pos = a.pos[seq], end = pos + a.fresh[seq];
+  const int blk = (pos >> 5) + u, full = end >> 5;  // full blocks afterwards
+  if (end == pos || blk > full || (blk == full && u > 0)) return;
+  uint8_t* base = a.arena + it.region + (int64_t)sidx * it.stream_bytes;
+  uint8_t* tailb = base + (int64_t)a.nb_cap * it.block_bytes;
+  const void* in = part ? a.v : a.k;
+  // the element of the row of stored token t, channel 8 q
+  const int64_t e0 = (int64_t)it.row * a.row_stride + (int64_t)(it.s0 + sidx) * a.m * D + 8 * q;
+  const auto new_row = [&](int t) -> u4v {
+    const int64_t e = e0 + (int64_t)(t - pos) * D;
+    if (a.in_f32) {
+      Rows<true> x;
+      x.load<false>(in, e, 0);
+      return x.bf16(0);
+    }
+    return *reinterpret_cast<const u4v*>(static_cast<const uint16_t*>(in) + e);
+  };
+  if (blk == full) {  // no block completed: the tokens of each lane's row set, into their slots
+    for (int t = pos + tg; t < end; t += 4) {
+      const u4v w = new_row(t);
+      const int s = t & 31;
+      if (part == 0) {
+        *reinterpret_cast<u4v*>(tailb + k_bf16_byte(D, s, 8 * q)) = w;
+      } else {
+#pragma unroll
+        for (int c = 0; c < 8; ++c)
+          *reinterpret_cast<uint16_t*>(tailb + v_bf16_byte(D, s, 8 * q + c)) = (uint16_t)(w[c >> 1] >> (16 * (c & 1)));
+      }
+    }
+    return;
+  }
+  Rows<false> rows;
+  if (u == 0 && (pos & 31)) {
+    if (part == 0) {
+#pragma unroll
+      for (int n = 0; n < 8; ++n)
+        rows.w[n] = *reinterpret_cast<const u4v*>(tailb + k_bf16_byte(D, row_token(n, tg), 8 * q));
+    } else {
+      u4v vc[8];
+#pragma unroll
+      for (int n = 0; n < 8; ++n)
+        vc[n] = *reinterpret_cast<const u4v*>(tailb + 64 * D + share_byte(D, 16 * tg + ((8 * q + n) & 15), q >> 1 << 4));
+#pragma unroll
+      for (int n = 0; n < 8; ++n)
+#pragma unroll
+        for (int p = 0; p < 4; ++p)
+          rows.w[n][p] = __builtin_amdgcn_perm(vc[2 * p + 1][n >> 1], vc[2 * p][n >> 1], n & 1 ? 0x07060302u : 0x05040100u);
+    }
+  }
+#pragma unroll
+  for (int n = 0; n < 8; ++n) {
+    const int t = 32 * blk + row_token(n, tg);
+    if (t >= pos) rows.w[n] = new_row(t);
+  }
+  uint8_t* img = img_all + (part * L::kBlocks + sub) * kImg;
+  uint8_t* out = base + (int64_t)blk * it.block_bytes;
+#define KVK_CHUNK_BITS(B) \
+  { \
+    if (part == 0) quant_keys<D, B, QS>(rows, q, tg, img); \
+    else quant_values<D, B, QS>(rows, q, tg, img); \
+    copy_quant_part<D, B, QS>(img, out, part, l); \
+  }
+  if (it.bits == 16) {
+    if (part == 0) bf16_keys<D>(rows, q, tg, img);
+    else bf16_values<D>(rows, q, tg, img);
+    copy_bf16_part<D>(img, out, part, l);
+  } else if (it.bits == 8) KVK_CHUNK_BITS(8)
+  else if (it.bits == 4) KVK_CHUNK_BITS(4)
+  else KVK_CHUNK_BITS(2)
+#undef KVK_CHUNK_BITS
+  if (u > 0 || !(end & 31)) return;
+  // The tokens left over: the new tail, zeros after them.  (This wave alone reads and writes
+  // this part of the tail; what it read is in registers, the fence keeps the stores behind.)
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");
+  wave_lds_fence();
+#pragma unroll
+  for (int n = 0; n < 8; ++n) {
+    const int t = 32 * full + row_token(n, tg);
+    rows.w[n] = t < end ? new_row(t) : u4v{0, 0, 0, 0};
+  }
+  if (part == 0) bf16_keys<D>(rows, q, tg, img);
+  else bf16_values<D>(rows, q, tg, img);
+  copy_bf16_part<D>(img, tailb, part, l);
+}
+
 // Test-only dequantiser: one thread per (stream, token, channel).
 template <int D>
 __global__ __launch_bounds__(256) void dequant_kernel(const uint8_t* region, int64_t stream_bytes,
@@ -1109,6 +1232,100 @@ static kvk_status append_gqa(const kvk_table* t, int32_t l0, int32_t l1, const v
     if (e != hipSuccess) return fail(KVK_ERR_DEVICE, "append launch: %s", hipGetErrorString(e));
   }
   return KVK_OK;
+}
+
+extern "C" kvk_status kvk_append_chunk(const kvk_table* t, int32_t l0, int32_t l1, const void* k, const void* v,
+                                       int32_t in_dtype, int32_t n_chunk, const int32_t* n_stored,
+                                       const int32_t* n_new, void* arena, hipStream_t stream) {
+  const char* what = "kvk_append_chunk";
+  if (!t) return fail(KVK_ERR_INVALID, "%s: NULL table", what);
+  const kvk_dims& d = t->d;
+  if (d.kind != KVK_GQA) return fail(KVK_ERR_UNSUPPORTED, "%s: GQA tables (MLA: kvk_append_token)", what);
+  if (l0 < 0 || l1 > d.n_layers || l0 >= l1)
+    return fail(KVK_ERR_INVALID, "layer range [%d, %d) invalid for %d layers", l0, l1, d.n_layers);
+  if (!k || !v || !n_stored || !arena) return fail(KVK_ERR_INVALID, "%s: NULL buffer", what);
+  if (in_dtype != KVK_BF16 && in_dtype != KVK_F32) return fail(KVK_ERR_INVALID, "in_dtype %d", in_dtype);
+  if (n_chunk < 1 || n_chunk > t->cap)
+    return fail(KVK_ERR_INVALID, "%s: n_chunk %d outside 1..%d", what, n_chunk, t->cap);
+  bool uniform = true;
+  int32_t units = 0;  // blocks that some sequence's chunk touches
+  for (int b = 0; b < d.batch; ++b) {
+    const int32_t m = n_new ? n_new[b] : n_chunk;
+    if (n_stored[b] < 0 || n_stored[b] > t->cap)
+      return fail(KVK_ERR_INVALID, "%s: n_stored[%d] = %d outside 0..%d", what, b, n_stored[b], t->cap);
+    if (m < 0 || m > n_chunk || m > t->cap - n_stored[b])
+      return fail(KVK_ERR_INVALID, "%s: n_new[%d] = %d outside 0..min(n_chunk %d, room %d)", what, b, m, n_chunk,
+                  t->cap - n_stored[b]);
+    uniform &= n_stored[b] == n_stored[0] && m == (n_new ? n_new[0] : n_chunk);
+    if (m > 0) units = std::max(units, std::max(1, (n_stored[b] + m) / KVK_GROUP - n_stored[b] / KVK_GROUP));
+  }
+  if (!uniform && d.batch > kChunkSeqs)
+    return fail(KVK_ERR_UNSUPPORTED, "%s: %d sequences of different lengths (at most %d)", what, d.batch, kChunkSeqs);
+  if ((reinterpret_cast<uintptr_t>(arena) & 15) || (reinterpret_cast<uintptr_t>(k) & 15) ||
+      (reinterpret_cast<uintptr_t>(v) & 15))
+    return fail(KVK_ERR_INVALID, "misaligned buffer (16-byte alignment required)");
+  if (units == 0) return KVK_OK;  // no new tokens
+  const bool per_seq = !t->seq.empty();
+  ChunkWriteArgs a;
+  a.k = k;
+  a.v = v;
+  a.arena = static_cast<uint8_t*>(arena);
+  a.in_f32 = in_dtype == KVK_F32;
+  a.m = n_chunk;
+  a.nb_cap = t->nb_cap;
+  a.Hkv = d.n_kv_heads;
+  a.n_streams = per_seq ? d.n_kv_heads : d.batch * d.n_kv_heads;
+  a.units = units;
+  a.row_stride = (int64_t)d.batch * d.n_kv_heads * n_chunk * d.head_dim;
+  a.uniform = uniform;
+  for (int b = 0; b < (uniform ? 1 : d.batch); ++b) {
+    a.pos[b] = n_stored[b];
+    a.fresh[b] = n_new ? n_new[b] : n_chunk;
+  }
+  const int per_wg = d.head_dim == 128 ? 1 : 2;  // blocks of a workgroup
+  const int64_t grid = ((int64_t)a.n_streams * units + per_wg - 1) / per_wg;
+  if (grid > 0x3fffffffLL) return fail(KVK_ERR_UNSUPPORTED, "%s: grid too large", what);
+  bool checked = false;
+  int n = 0;
+  const auto flush = [&]() -> kvk_status {
+    if (n == 0) return KVK_OK;
+    if (!checked)
+      if (kvk_status st = check_gpu_buffers({k, v, arena}, what)) return st;
+    checked = true;
+    const dim3 g((unsigned)grid, (unsigned)n), b(128);
+    if (d.head_dim == 128) {
+      if (d.qscheme == KVK_Q_KIVI32) hipLaunchKernelGGL((chunk_write_kernel<128, kQsKivi>), g, b, 0, stream, a);
+      else if (d.qscheme == KVK_Q_GROUP64) hipLaunchKernelGGL((chunk_write_kernel<128, kQsG64>), g, b, 0, stream, a);
+      else hipLaunchKernelGGL((chunk_write_kernel<128, kQsSym>), g, b, 0, stream, a);
+    } else {
+      if (d.qscheme == KVK_Q_KIVI32) hipLaunchKernelGGL((chunk_write_kernel<64, kQsKivi>), g, b, 0, stream, a);
+      else if (d.qscheme == KVK_Q_GROUP64) hipLaunchKernelGGL((chunk_write_kernel<64, kQsG64>), g, b, 0, stream, a);
+      else hipLaunchKernelGGL((chunk_write_kernel<64, kQsSym>), g, b, 0, stream, a);
+    }
+    n = 0;
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return fail(KVK_ERR_DEVICE, "%s launch: %s", what, hipGetErrorString(e));
+    return KVK_OK;
+  };
+  // One item per anchor layer, or per (sequence, anchor layer of its plan).
+  for (int b = 0; b < (per_seq ? d.batch : 1); ++b) {
+    if (per_seq && (n_new ? n_new[b] : n_chunk) == 0) continue;
+    const kvk_table* s = per_seq ? t->seq[b] : t;
+    for (int l = l0; l < l1; ++l) {
+      if (s->plan[l].inherit) continue;  // an inheriting layer stores nothing (§2.1)
+      AppendItem& it = a.items[n];
+      it.region = (per_seq ? t->seq_base[b] : 0) + s->info.layer_offset[l];
+      it.stream_bytes = (int32_t)s->info.stream_bytes[l];
+      it.block_bytes = (int32_t)s->block_bytes[l];
+      it.bits = s->bits[l];
+      it.row = l - l0;
+      it.s0 = per_seq ? b * d.n_kv_heads : 0;
+      it.pad = 0;
+      if (++n == kChunkItems)
+        if (kvk_status st = flush()) return st;
+    }
+  }
+  return flush();
 }
 
 extern "C" kvk_status kvk_debug_dequantize(const kvk_table* t, int32_t layer, int32_t n_stored,

@@ -1,0 +1,187 @@
+// Attention tiles on 32x32x16 MFMA: the pieces shared by the kernels whose waves hold 32
+// query rows as the columns of their products.
+//
+//   S^T[token, row] = K[token, :] . q[row, :]     O^T[channel, row] += V^T[channel, token] P^T[token, row]
+//
+// Lane l of a wave holds query row l % 32 of every product, so a row's running maximum and
+// sum live in lanes r and r + 32 and need no transposition.  Of a 32-token subtile S^T puts
+// product rows 8 q + 4 h + r (q, r = 0..3) into half h = l / 32 as element e = 4 q + r, and
+// the second product takes its k-slots in that order: k-step x = 0, 1 of the subtile reads the
+// half's elements 8 x .. 8 x + 7, straight from the registers that the softmax left.
+#pragma once
+
+#include "kvk_device.h"
+
+namespace kvkd {
+
+typedef float f16v __attribute__((ext_vector_type(16)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float f2v __attribute__((ext_vector_type(2)));
+
+constexpr float kLn2 = 0.6931471805599453f;
+
+template <bool HALF>
+__device__ __forceinline__ f16v mfma32(u4v a, u4v b, f16v c) {
+  if constexpr (HALF) return __builtin_amdgcn_mfma_f32_32x32x16_f16(bitcast<half8>(a), bitcast<half8>(b), c, 0, 0, 0);
+  else return __builtin_amdgcn_mfma_f32_32x32x16_bf16(bitcast<bf16x8>(a), bitcast<bf16x8>(b), c, 0, 0, 0);
+}
+
+__device__ __forceinline__ f16v zero16() {
+  f16v z;
+#pragma unroll
+  for (int e = 0; e < 16; ++e) z[e] = 0.0f;
+  return z;
+}
+
+// Over the two halves of the wave (lanes l and l ^ 32).
+__device__ __forceinline__ float halves_max(float x) {
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+__device__ __forceinline__ float halves_sum(float x) {
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+
+// Two values rounded to nearest even, the first in the low half.
+template <bool HALF>
+__device__ __forceinline__ uint32_t pack2(float a, float b) {
+  if constexpr (HALF) {
+    return bitcast<uint32_t>(h2(a, b));
+  } else {
+    const bf16x2 r = __builtin_convertvector((f2v{a, b}), bf16x2);
+    return bitcast<uint32_t>(r);
+  }
+}
+
+// Product row of element e in half h of a 32-token subtile.
+__device__ __forceinline__ constexpr int tile_row(int e, int h) { return 8 * (e >> 2) + 4 * h + (e & 3); }
+
+// Running state of a wave's 32 query rows: output accumulators (32 NM channels), reference
+// maximum in base-2 logits, and the lane's share of the sum.
+template <int NM>
+struct RowState {
+  f16v o[NM];
+  float m, l;
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int i = 0; i < NM; ++i) o[i] = zero16();
+    m = -INFINITY;
+    l = 0.0f;
+  }
+};
+
+// A row's reference moves only when a logit exceeds it by more than this (base-2): the
+// accumulators hold values up to 2^kSlack times larger than with the true maximum, in fp32,
+// and most steps need no rescaling.
+constexpr float kSlack = 8.0f;
+
+// One online-softmax step over NT subtiles: scores s (times c = log2-scale: base-2 logits)
+// become probabilities 2^(c s - m + BIAS), packed for the second product in p.  c > 0.  A
+// row whose logits have all been -inf so far keeps the reference -inf, and its probabilities
+// 2^(-inf) = 0 are formed against 0.
+template <int NM, int NT, bool HALF>
+__device__ __forceinline__ void softmax_step(RowState<NM>& st, f16v (&s)[NT], float c, float bias, u4v (&p)[NT][2]) {
+  float mx = s[0][0];
+#pragma unroll
+  for (int i = 0; i < NT; ++i)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[i][e]);
+  mx = halves_max(mx) * c;
+  if (__any(mx > st.m + kSlack)) {
+    const float mnew = fmaxf(st.m, mx);
+    const float alpha = mnew == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(st.m - mnew);
+    st.m = mnew;
+    st.l *= alpha;
+#pragma unroll
+    for (int i = 0; i < NM; ++i) st.o[i] *= alpha;
+  }
+  const float ref = (st.m == -INFINITY ? 0.0f : st.m) - bias;
+  float sum = 0.0f;
+#pragma unroll
+  for (int i = 0; i < NT; ++i)
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const int e = 8 * x + 2 * w;
+        const float a = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i][e], c, -ref));
+        const float b = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i][e + 1], c, -ref));
+        sum += a + b;
+        p[i][x][w] = pack2<HALF>(a, b);
+      }
+  st.l += sum;
+}
+
+// Whether any of the eight bf16 / fp16 values of a 16-byte unit is infinite or NaN.
+template <bool HALF>
+__device__ __forceinline__ bool any_nonfinite(u4v w) {
+  constexpr uint32_t kExp = HALF ? 0x7c00u : 0x7f80u;
+  bool bad = false;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) bad |= (w[i] & kExp) == kExp || ((w[i] >> 16) & kExp) == kExp;
+  return bad;
+}
+// The unit with its infinite and NaN values replaced by zero.
+template <bool HALF>
+__device__ __forceinline__ u4v only_finite(u4v w) {
+  constexpr uint32_t kExp = HALF ? 0x7c00u : 0x7f80u;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if ((w[i] & kExp) == kExp) w[i] &= 0xffff0000u;
+    if (((w[i] >> 16) & kExp) == kExp) w[i] &= 0x0000ffffu;
+  }
+  return w;
+}
+
+// Infinite and NaN values in a tile that some rows may not see wholly: a masked place has
+// probability 0, and 0 times infinity would reach every row of the product.  The values a row
+// does see are counted by kind in products of indicators, and each kind present is added to
+// the row's outputs (p > 0 times an infinity or a NaN is that value); the caller then replaces
+// them by zero in the tile.  unit(i, x, m): the value operand of subtile i, k-step x, channel
+// tile m.  Rare.
+template <int NM, int NT, bool HALF, class Unit, class Hidden>
+__device__ __forceinline__ void take_nonfinite(RowState<NM>& st, Unit unit, Hidden hidden) {
+  constexpr uint32_t kOne = HALF ? 0x3c00u : 0x3f80u, kExp = HALF ? 0x7c00u : 0x7f80u;
+  // the rows' visible places as ones, built by arithmetic: kept lane masks would fill the
+  // scalar registers
+  u4v seen[NT][2];
+#pragma unroll
+  for (int i = 0; i < NT; ++i)
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const int e = 8 * x + 2 * w;  // hidden(i, e): all ones where the row does not see it, else 0
+        seen[i][x][w] = (kOne & ~hidden(i, e)) | ((kOne << 16) & ~hidden(i, e + 1));
+      }
+#pragma unroll 1
+  for (int kind = 0; kind < 3; ++kind) {  // +infinity, -infinity, NaN
+    // a 16-bit value b is of the kind if (b & keep) - lo < span (unsigned)
+    const uint32_t keep = kind == 2 ? 0x7fffu : 0xffffu, lo = kind == 0 ? kExp : (kind == 1 ? kExp | 0x8000u : kExp + 1);
+    const uint32_t span = kind == 2 ? 0x8000u - (kExp + 1) : 1u;
+#pragma unroll 1
+    for (int m = 0; m < NM; ++m) {
+      f16v n = zero16();
+#pragma unroll
+      for (int i = 0; i < NT; ++i)
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          u4v v = unit(i, x, m);
+#pragma unroll
+          for (int w = 0; w < 4; ++w)
+            v[w] = ((v[w] & keep) - lo < span ? kOne : 0u) | (((v[w] >> 16) & keep) - lo < span ? kOne << 16 : 0u);
+          n = mfma32<HALF>(v, seen[i][x], n);
+        }
+      const float add = kind == 0 ? INFINITY : (kind == 1 ? -INFINITY : __builtin_nanf(""));
+#pragma unroll
+      for (int c = 0; c < NM; ++c)  // (a register array takes no run-time index)
+        if (c == m) {
+#pragma unroll
+          for (int e = 0; e < 16; ++e) st.o[c][e] = n[e] > 0.0f ? st.o[c][e] + add : st.o[c][e];
+        }
+    }
+  }
+}
+
+}  // namespace kvkd
