@@ -524,10 +524,14 @@ kvk_status kvk_attention_weight(int32_t n_q_heads, int32_t n_kv_heads, int32_t h
  *   n_tokens : keep_tokens .. max_tokens.
  *   n_recent : 0 .. keep_tokens.
  *   keep_out : device int32 [streams][keep_tokens].
+ *   workspace: device, >= kvk_keep_workspace_bytes(table, n_tokens), 256-byte aligned; NULL
+ *              where that is 0 (up to 16384 tokens).
  * Errors: KVK_ERR_INVALID (table without eviction, sizes, NULL pointers, misalignment, host
- *         memory), KVK_ERR_DEVICE. */
+ *         memory), KVK_ERR_BUFFER (workspace), KVK_ERR_UNSUPPORTED (more than 65535 streams of
+ *         over 16384 tokens), KVK_ERR_DEVICE. */
+kvk_status kvk_keep_workspace_bytes(const kvk_table* table, int32_t n_tokens, size_t* out_bytes);
 kvk_status kvk_keep_heaviest(const kvk_table* table, const float* weight, int32_t n_tokens, int32_t n_recent,
-                             int32_t* keep_out, hipStream_t stream);
+                             int32_t* keep_out, void* workspace, size_t ws_bytes, hipStream_t stream);
 
 /* The selector's forward pass (§2.3; App. B "Selector architecture"): the prompt's
  * token embeddings (the backbone's own) -> a linear map to width 256 -> two

@@ -60,6 +60,7 @@ struct Shape {
   static constexpr int kRowsWg = 32 * WR;
   static constexpr int kWt = 4 / WR;            // waves over the tokens
   static constexpr int kTb = WR == 1 ? 4 : 2;
+  static constexpr int kBuffers = WR == 1 ? 1 : 2;  // tiles in LDS
   static constexpr int kNt = kTb / kWt;
 };
 
@@ -205,7 +206,7 @@ __global__ __launch_bounds__(256, 2) void chunk_kernel(ChunkArgs a) {
   constexpr int NM = D / 32, NK = D / 16, TB = S::kTb, NT = S::kNt, WT = S::kWt;
   constexpr int kBlk = 128 * D;  // LDS bytes of a block: keys, then values
   constexpr int kSlot = P::MBYTES > 0 ? P::MBYTES / 4 : 1;
-  constexpr int kTile = TB * kBlk, kJoin = (WT - 1) * WR * 64 * NM * 64;
+  constexpr int kTile = S::kBuffers * TB * kBlk, kJoin = (WT - 1) * WR * 64 * NM * 64;
   __shared__ __align__(16) uint8_t img[kTile > kJoin ? kTile : kJoin];
   __shared__ __align__(16) uint32_t slots[4][kSlot];
   __shared__ float2 stats[4][32];
@@ -243,7 +244,8 @@ __global__ __launch_bounds__(256, 2) void chunk_kernel(ChunkArgs a) {
 #pragma unroll
     for (int i = 0; i < TB; ++i) part[i].template load<(WR < 4)>(stream + (int64_t)min(tile * TB + i, nbf - 1) * a.block_bytes, wave, lane);
   };
-  const auto place = [&](int blk) { return img + blk * kBlk + (wave < 2 ? wave * 32 * D : 64 * D + (wave - 2) * 1024 * P::UN); };
+  uint8_t* buf = img;  // the tile in work
+  const auto place = [&](int blk) { return buf + blk * kBlk + (wave < 2 ? wave * 32 * D : 64 * D + (wave - 2) * 1024 * P::UN); };
   if (tile0 < tile1) load(tile0);
 
   u4v qf[NK];
@@ -262,105 +264,100 @@ __global__ __launch_bounds__(256, 2) void chunk_kernel(ChunkArgs a) {
 
   // Key operand: product row col reads the token that puts the values in place (see above).
   const int ktok = 16 * ((col >> 3) & 1) + 8 * (col >> 4) + (col & 7);
-  const uint8_t* kp0 = img + (ktok >> 4) * 32 * D + 16 * (16 * h + (ktok & 15));
-  const uint8_t* vp0 = img + 64 * D + 1024 * (col >> 4) + 16 * (16 * h + (col & 15));
+  const int kat = (ktok >> 4) * 32 * D + 16 * (16 * h + (ktok & 15));
+  const int vat = 64 * D + 1024 * (col >> 4) + 16 * (16 * h + (col & 15));
   const auto key_unit = [&](int blk, int j) {  // octet 2 j + h: sub-chunk j / 2, kg = 2 (j % 2) + h
-    return *reinterpret_cast<const u4v*>(kp0 + blk * kBlk + 1024 * (j >> 1) + 512 * (j & 1));
+    return *reinterpret_cast<const u4v*>(buf + kat + blk * kBlk + 1024 * (j >> 1) + 512 * (j & 1));
   };
   const auto value_unit = [&](int blk, int x, int m) {  // kg = 2 x + h
-    return *reinterpret_cast<const u4v*>(vp0 + blk * kBlk + 2048 * m + 512 * x);
+    return *reinterpret_cast<const u4v*>(buf + vat + blk * kBlk + 2048 * m + 512 * x);
   };
-  // One tile in LDS, whose first token is at position p0; bound: the last position that holds
-  // a token of it.
-  const auto attend = [&](int p0, int bound, bool masked) {
-    const int b0 = wt * NT;
-    if (p0 + 32 * b0 > min(bound, seen_by_any)) return;
-    f16v s[NT];
+
+  // Tiles of full blocks, then the bf16 window (one block) as one more.
+  const int n_tiles = max(tile1 - tile0, 0) + (tail ? 1 : 0);
+  for (int i = 0; i < n_tiles; ++i) {
+    const int tile = tile0 + i;
+    const bool window = tile >= tile1;
+    const int p0 = window ? 32 * nbf : 32 * TB * tile;   // the first token's position
+    const int bound = window ? stored - 1 : 32 * nbf - 1;  // the last position that holds a token of it
+    if (!window) {
 #pragma unroll
-    for (int i = 0; i < NT; ++i) {
-      s[i] = zero16();
+      for (int k = 0; k < TB; ++k) {
+        if (tile * TB + k < nbf) {
+          part[k].store(place(k), slots[wave], wave, lane);
+        } else if (wave >= 2) {  // past the full blocks: no value may enter a product
 #pragma unroll
-      for (int j = 0; j < NK; ++j) s[i] = mfma32<HALF>(key_unit(b0 + i, j), qf[j], s[i]);
+          for (int u = 0; u < P::UN; ++u) reinterpret_cast<u4v*>(place(k) + 16 * lane)[64 * u] = u4v{0, 0, 0, 0};
+        }
+      }
+      if (tile + 1 < tile1) load(tile + 1);
+    } else {
+      const uint8_t* tb = stream + (int64_t)a.nb_cap * a.block_bytes;
+      const u4v* in = reinterpret_cast<const u4v*>(tb + (wave < 2 ? wave * 32 * D : 64 * D + (wave - 2) * 1024 * P::UN)) + lane;
+#pragma unroll
+      for (int u = 0; u < P::UN; ++u) {
+        u4v x = in[64 * u];
+        if (wave >= 2) {  // slots past the tokens hold anything
+#pragma unroll
+          for (int n = 0; n < 8; ++n)
+            if (16 * (n >> 2) + 4 * (lane >> 4) + (n & 3) >= stored % 32) x[n >> 1] &= n & 1 ? 0x0000ffffu : 0xffff0000u;
+#pragma unroll
+          for (int k = 1; k < TB; ++k) reinterpret_cast<u4v*>(place(k) + 16 * lane)[64 * u] = u4v{0, 0, 0, 0};
+        }
+        reinterpret_cast<u4v*>(place(0) + 16 * lane)[64 * u] = HALF ? bf16_to_half_unit(x) : x;
+      }
     }
+    // A tile that some row does not see wholly: masked scores, and a look for infinities and NaN
+    // among its values (see take_nonfinite).
+    const bool masked = p0 + 32 * TB - 1 > min(seen_by_all, bound);
+    const int b0 = wt * NT;  // the wave's blocks
+    const int last = min(limit, bound) - p0 - 32 * b0;  // the last token of them that the row sees
     if (masked) {
-      const int last = min(limit, bound) - p0 - 32 * b0;
-#pragma unroll
-      for (int i = 0; i < NT; ++i)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) s[i][e] = 32 * i + subtile_token(e, h) <= last ? s[i][e] : -INFINITY;
+      bool bad = false;
+      if (wave >= 2) {
+        for (int k = 0; k < TB; ++k) {
+          const u4v* u = reinterpret_cast<const u4v*>(place(k) + 16 * lane);
+          for (int y = 0; y < P::UN; ++y) bad |= any_nonfinite<HALF>(u[64 * y]);
+        }
+      }
+      if (__syncthreads_or(bad)) {
+        asm volatile("");
+        take_nonfinite<NM, NT, HALF>(st, [&](int k, int x, int m) { return value_unit(b0 + k, x, m); },
+                                     [&](int k, int e) { return (uint32_t)((last - 32 * k - subtile_token(e, h)) >> 31); });
+        __syncthreads();
+        if (wave >= 2) {
+          for (int k = 0; k < TB; ++k) {
+            u4v* u = reinterpret_cast<u4v*>(place(k) + 16 * lane);
+            for (int y = 0; y < P::UN; ++y) u[64 * y] = only_finite<HALF>(u[64 * y]);
+          }
+        }
+        __syncthreads();
+      }
+    } else {
+      __syncthreads();
     }
-    u4v p[NT][2];
-    softmax_step<NM, NT, HALF>(st, s, a.c, kBias, p);
 #pragma unroll
-    for (int i = 0; i < NT; ++i)
+    for (int k = 0; k < NT; ++k) {
+      if (p0 + 32 * (b0 + k) > min(bound, seen_by_any)) break;
+      f16v s[1] = {zero16()};
+#pragma unroll
+      for (int j = 0; j < NK; ++j) s[0] = mfma32<HALF>(key_unit(b0 + k, j), qf[j], s[0]);
+      if (masked) {
+        asm volatile("");  // a branch: as selects these would cost every tile vector work
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s[0][e] = 32 * k + subtile_token(e, h) <= last ? s[0][e] : -INFINITY;
+      }
+      u4v p[1][2];
+      softmax_step<NM, 1, HALF>(st, s, a.c, kBias, p);
 #pragma unroll
       for (int x = 0; x < 2; ++x)
 #pragma unroll
-        for (int m = 0; m < NM; ++m) st.o[m] = mfma32<HALF>(value_unit(b0 + i, x, m), p[i][x], st.o[m]);
-  };
-  // A tile some row does not see wholly: infinities and NaN among its values (see take_nonfinite).
-  const auto careful = [&](int p0) {
-    bool bad = false;
-    if (wave >= 2) {
-      for (int i = 0; i < TB; ++i) {
-        const u4v* u = reinterpret_cast<const u4v*>(place(i) + 16 * lane);
-        for (int k = 0; k < P::UN; ++k) bad |= any_nonfinite<HALF>(u[64 * k]);
-      }
+        for (int m = 0; m < NM; ++m) st.o[m] = mfma32<HALF>(value_unit(b0 + k, x, m), p[0][x], st.o[m]);
     }
-    if (!__syncthreads_or(bad)) return;
-    take_nonfinite<NM, NT, HALF>(
-        st, [&](int i, int x, int m) { return value_unit(wt * NT + i, x, m); },
-        [&](int i, int e) { return (uint32_t)((limit - p0 - 32 * (wt * NT + i) - subtile_token(e, h)) >> 31); });
-    __syncthreads();
-    if (wave >= 2) {
-      for (int i = 0; i < TB; ++i) {
-        u4v* u = reinterpret_cast<u4v*>(place(i) + 16 * lane);
-        for (int k = 0; k < P::UN; ++k) u[64 * k] = only_finite<HALF>(u[64 * k]);
-      }
-    }
-    __syncthreads();
-  };
-
-  for (int tile = tile0; tile < tile1; ++tile) {
-    const int p0 = 32 * TB * tile;
-#pragma unroll
-    for (int i = 0; i < TB; ++i) {
-      if (tile * TB + i < nbf) {
-        part[i].store(place(i), slots[wave], wave, lane);
-      } else if (wave >= 2) {  // past the full blocks: no value may enter a product
-#pragma unroll
-        for (int u = 0; u < P::UN; ++u) reinterpret_cast<u4v*>(place(i) + 16 * lane)[64 * u] = u4v{0, 0, 0, 0};
-      }
-    }
-    if (tile + 1 < tile1) load(tile + 1);
-    const bool masked = p0 + 32 * TB - 1 > min(seen_by_all, 32 * nbf - 1);
-    if (masked) careful(p0);
-    __syncthreads();
-    attend(p0, 32 * nbf - 1, masked);
-    __syncthreads();
+    if constexpr (S::kBuffers == 1) __syncthreads();
+    else buf = buf == img ? img + TB * kBlk : img;  // (its last readers are behind this tile's barrier)
   }
-  if (tail) {  // the bf16 window: one block
-    const int p0 = 32 * nbf, ntail = stored % 32;
-    const uint8_t* tb = stream + (int64_t)a.nb_cap * a.block_bytes;
-    const u4v* in = reinterpret_cast<const u4v*>(tb + (wave < 2 ? wave * 32 * D : 64 * D + (wave - 2) * 1024 * P::UN)) + lane;
-#pragma unroll
-    for (int u = 0; u < P::UN; ++u) {
-      u4v x = in[64 * u];
-      if (wave >= 2) {  // slots past the tokens hold anything
-#pragma unroll
-        for (int n = 0; n < 8; ++n)
-          if (16 * (n >> 2) + 4 * (lane >> 4) + (n & 3) >= ntail) x[n >> 1] &= n & 1 ? 0x0000ffffu : 0xffff0000u;
-      }
-      reinterpret_cast<u4v*>(place(0) + 16 * lane)[64 * u] = HALF ? bf16_to_half_unit(x) : x;
-      if (wave >= 2)
-#pragma unroll
-        for (int i = 1; i < TB; ++i) reinterpret_cast<u4v*>(place(i) + 16 * lane)[64 * u] = u4v{0, 0, 0, 0};
-    }
-    careful(p0);
-    __syncthreads();
-    attend(p0, stored - 1, true);
-    __syncthreads();
-  }
+  __syncthreads();
 
   // The states of the waves that share rows meet in the wave with wt = 0.
   float l = halves_sum(st.l);
@@ -426,46 +423,60 @@ __global__ __launch_bounds__(256, 2) void chunk_kernel(ChunkArgs a) {
   if (h == 0) *reinterpret_cast<float2*>(rec + D) = make_float2(st.m, l);
 }
 
-// The splits of every row joined: half a wave per row, D / 32 channels a lane.
+// The splits of every row joined, half a wave per row, D / 32 channels a lane: lane s takes split
+// s's maximum first, then the lanes read eight records at a time.
 template <int D>
 __global__ __launch_bounds__(256) void chunk_merge_kernel(ChunkArgs a, int tb) {
-  typedef float fv __attribute__((ext_vector_type(D / 32)));
+  constexpr int V = D / 32;
+  typedef float fv __attribute__((ext_vector_type(V)));
   const int lane = threadIdx.x & 63, l32 = lane & 31;
-  const int first = (blockIdx.x * 4 + (threadIdx.x >> 6)) * 2;
-  if (first >= a.total_rows) return;
-  const int r = min(first + (lane >> 5), a.total_rows - 1);
-  int sj = 0;
-  for (int j0 = 0; j0 < a.n_seq; j0 += 64) {  // both rows' sequences: one ballot each
-    const int j = j0 + lane;
-    const int start = j < a.n_seq ? a.row0[j] : 0x7fffffff;
-    const uint64_t b0 = __ballot(start <= first), b1 = __ballot(start <= min(first + 1, a.total_rows - 1));
-    const uint64_t b = lane >> 5 ? b1 : b0;
-    if (b) sj = j0 + 63 - __clzll(b);
-  }
-  const int stored = a.stored[sj], fresh = a.fresh[sj];
-  const int nsplit = splits_of(stored, tb, a.split_tiles);
-  if (nsplit == 1 || first + (lane >> 5) >= a.total_rows) return;  // written by its workgroup
-  const int R = a.geff * fresh, x = r - a.row0[sj], kvh = x / R, row = x - kvh * R;
+  const int r0 = __builtin_amdgcn_readfirstlane(2 * (blockIdx.x * 4 + (threadIdx.x >> 6)));
+  if (r0 >= a.total_rows) return;
+  const int r1 = min(r0 + 1, a.total_rows - 1);
+  const int s0j = find_seq(a.row0, a.n_seq, r0, lane), s1j = find_seq(a.row0, a.n_seq, r1, lane);
+  const int r = lane < 32 ? r0 : r1, sj = lane < 32 ? s0j : s1j;
+  const int nsplit = splits_of(a.stored[sj], tb, a.split_tiles);
+  const bool live = nsplit > 1 && r0 + (lane >> 5) < a.total_rows;  // (one split: written by its workgroup)
+  const int n = live ? nsplit : 0;
+  const int R = a.geff * a.fresh[sj], x = r - a.row0[sj], kvh = x / R, row = x - kvh * R;
   const float* rec = a.ws + (a.rec0[sj] + (int64_t)kvh * nsplit * R + row) * (D + 4);
   const int64_t step = (int64_t)R * (D + 4);
   float M = -INFINITY;
-  for (int s = 0; s < nsplit; ++s) M = fmaxf(M, rec[s * step + D]);
+  for (int s = l32; s < n; s += 32) M = fmaxf(M, rec[s * step + D]);
+  M = max16(M);
+  {  // over the half wave's two rows of 16 lanes
+    const auto y = __builtin_amdgcn_permlane16_swap(__float_as_uint(M), __float_as_uint(M), false, false);
+    M = fmaxf(__uint_as_float(y[0]), __uint_as_float(y[1]));
+  }
   float l = 0.0f;
   fv o;
 #pragma unroll
-  for (int k = 0; k < D / 32; ++k) o[k] = 0.0f;
-  for (int s = 0; s < nsplit; ++s) {
-    const float2 ml = *reinterpret_cast<const float2*>(rec + s * step + D);
-    const float f = ml.x == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(ml.x - M);  // (no mass, or NaN)
-    l += ml.y * f;
-    o += *reinterpret_cast<const fv*>(rec + s * step + D / 32 * l32) * f;
+  for (int k = 0; k < V; ++k) o[k] = 0.0f;
+  for (int i0 = 0; i0 < n; i0 += 8) {
+    fv v[8];
+    float2 ml[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float* p = rec + min(i0 + i, n - 1) * step;
+      v[i] = *reinterpret_cast<const fv*>(p + V * l32);
+      ml[i] = *reinterpret_cast<const float2*>(p + D);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if (i0 + i < n) {
+        const float w = ml[i].x == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(ml[i].x - M);  // (no mass, or NaN)
+        l += ml[i].y * w;
+        o += v[i] * w;
+      }
+    }
   }
+  if (!live) return;
   const float inv = 1.0f / l;
   const int tok = row / a.geff, rl = (row - tok * a.geff) / a.G, g = row - tok * a.geff - rl * a.G;
-  uint16_t* op = a.out + ((((int64_t)(a.layer0 + rl) * a.B + a.index[sj]) * a.Hq + kvh * a.G + g) * a.m + tok) * D + D / 32 * l32;
+  uint32_t* op = reinterpret_cast<uint32_t*>(
+      a.out + ((((int64_t)(a.layer0 + rl) * a.B + a.index[sj]) * a.Hq + kvh * a.G + g) * a.m + tok) * D + V * l32);
 #pragma unroll
-  for (int k = 0; k < D / 64; ++k)
-    reinterpret_cast<uint32_t*>(op)[k] = pack2<false>(o[2 * k] * inv, o[2 * k + 1] * inv);
+  for (int k = 0; k < V / 2; ++k) op[k] = pack2<false>(o[2 * k] * inv, o[2 * k + 1] * inv);
 }
 
 }  // namespace
@@ -474,10 +485,13 @@ using namespace kvk;
 
 namespace {
 
-// Workgroups that a launch's splits aim at, and the fewest tiles of a split (a split pays its
-// start, and a record per row written and read).
+// Workgroups that a launch's splits aim at: four per CU, so that the last ones to end leave
+// little idle, or the two that a CU holds at once where four would be short (a split pays its
+// start, and a record per row written and read).  4-bit, 64 streams of 8192 tokens, one new
+// token: two per CU 37 us, four 42; 8-bit, 256 streams, four new tokens: 131 and 122.
 constexpr int64_t kAimWgs = 1024;
-constexpr int kMinTiles = 4;
+constexpr int kLongSplit = 16;  // tiles
+constexpr int kMinTiles = 2;
 
 int waves_over_rows(int64_t rows) { return rows <= 32 ? 1 : (rows <= 64 ? 2 : 4); }
 int blocks_of_tile(int wr) { return wr == 1 ? 4 : 2; }
@@ -517,7 +531,8 @@ kvk_status lay_out(ChunkLaunch& L) {
     wgs += n;
     work += n * ((a.stored[j] / 32 + tb - 1) / tb);
   }
-  a.split_tiles = wgs >= kAimWgs ? 0x7fffffff : (int32_t)std::max<int64_t>(kMinTiles, (work + kAimWgs - 1) / kAimWgs);
+  const int64_t aim = work / kAimWgs >= kLongSplit ? kAimWgs : kAimWgs / 2;
+  a.split_tiles = wgs >= aim ? 0x7fffffff : (int32_t)std::max<int64_t>(kMinTiles, (work + aim - 1) / aim);
   int64_t wg = 0, rec = 0, row = 0;
   for (int j = 0; j < a.n_seq; ++j) {
     const int64_t R = (int64_t)a.geff * a.fresh[j], nrb = (R + rows - 1) / rows;

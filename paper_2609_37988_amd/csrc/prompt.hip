@@ -89,45 +89,51 @@ __device__ __forceinline__ int64_t row_base(const Strides& s, const SeqList& l, 
 // Causal attention of whole prompts
 // ---------------------------------------------------------------------------
 
-// LDS image of a tile of kTok<D> tokens: K rows of D bf16 padded by one 16-byte unit, and V
-// transposed into units of eight tokens of one channel (the operand of one lane and k-step),
-// one unit of padding after every eight channels.  Both the staging writes and the operand
-// reads of eight neighbouring lanes then fall into different banks.
+// LDS image of a tile of kTok tokens: K rows of D bf16, padded by one 16-byte unit so that eight
+// neighbouring tokens' units of one octet lie in different banks; V rows as they are, the units
+// of a row exchanged by v_turn of its token.  The value operands come out of V by transposing
+// reads (four tokens by sixteen channels for sixteen lanes); the exchange puts the four tokens'
+// 32 bytes (and, for two such groups at a time, their 64 bytes) into different banks.
+constexpr int kTok = 64;    // tokens of a tile
 constexpr int kRows = 128;  // query rows of a workgroup
-template <int D>
-constexpr int kTok = D == 128 ? 64 : 128;  // 16 KiB of keys either way
 template <int D>
 constexpr int kPitchK = 2 * D + 16;
 template <int D>
-constexpr int kPitchV = 16 * (D + D / 8);  // one group of eight tokens
+constexpr int kBytesK = kTok * kPitchK<D>;
 template <int D>
-constexpr int kBytesK = kTok<D>* kPitchK<D>;
+constexpr int kBytesV = kTok * 2 * D;
 template <int D>
-constexpr int kBytesV = kTok<D> / 8 * kPitchV<D>;
-
-// Token n of the eight in V group g of a tile (group 2 x + h: k-step x, wave half h).
-__device__ __forceinline__ constexpr int v_token(int g, int n) {
-  return 16 * (g >> 1) + 8 * (n >> 2) + 4 * (g & 1) + (n & 3);
+__device__ __forceinline__ int v_turn(int token) {
+  const int r = token & 3;
+  return D == 128 ? 4 * r + 2 * ((r & 1) ^ (r >> 1)) : 2 * r;
 }
 
-// A thread's share of a tile: eight 16-byte pieces.  Threads 0 .. 127 stage the keys (piece
-// i: token t0 + 8 i... of one channel octet), threads 128 .. 255 the values (one octet of the
-// eight tokens of one group).
+// A thread's share of a tile: 16-byte pieces of K and V rows.
 template <int D>
 struct Stage {
-  static constexpr int kOct = D / 8;
-  u4v w[8];
+  static constexpr int kOct = D / 8, kStep = 256 / kOct;  // tokens between a thread's pieces
+  static constexpr int kPieces = kTok / kStep;
+  u4v k[kPieces], v[kPieces];
 
-  // first: the tile's first token; last: the sequence's last token (later ones read it)
-  __device__ __forceinline__ void load(const uint16_t* base, int64_t token_stride, int first, int last, bool values,
-                                       int tid) {
-    const int u = tid & 127, o = u % kOct, r = u / kOct;
-    const uint16_t* p = base + (int64_t)first * token_stride;
+  // kp, vp: the row of the thread's first token in tile 0, at its octet; first: the tile's first
+  // token; last: the sequence's last token (later ones read it).
+  __device__ __forceinline__ void load(const uint16_t* kp, const uint16_t* vp, int64_t ks, int64_t vs, int first,
+                                       int last, int r) {
+    if (first + kTok - 1 <= last) {
+      const uint16_t *ka = kp + (int64_t)first * ks, *va = vp + (int64_t)first * vs;
 #pragma unroll
-    for (int n = 0; n < 8; ++n) {
-      int t = values ? v_token(r, n) : r + (128 / kOct) * n;
-      if (first + t > last) t = last - first;
-      w[n] = *reinterpret_cast<const u4v*>(p + (int64_t)t * token_stride + 8 * o);
+      for (int n = 0; n < kPieces; ++n) {
+        k[n] = *reinterpret_cast<const u4v*>(ka + kStep * n * ks);
+        v[n] = *reinterpret_cast<const u4v*>(va + kStep * n * vs);
+      }
+    } else {
+#pragma unroll
+      for (int n = 0; n < kPieces; ++n) {
+        const int t = min(first + r + kStep * n, last) - r;
+        k[n] = *reinterpret_cast<const u4v*>(kp + (int64_t)t * ks);
+        v[n] = *reinterpret_cast<const u4v*>(vp + (int64_t)t * vs);
+        if (first + r + kStep * n > last) v[n] = u4v{0, 0, 0, 0};  // no value past the sequence may enter a product
+      }
     }
   }
 
@@ -135,41 +141,37 @@ struct Stage {
   __device__ __forceinline__ bool nonfinite() const {
     bool bad = false;
 #pragma unroll
-    for (int n = 0; n < 8; ++n) bad |= any_nonfinite<false>(w[n]);
+    for (int n = 0; n < kPieces; ++n) bad |= any_nonfinite<false>(v[n]);
     return bad;
   }
 
-  __device__ __forceinline__ void store(uint8_t* kimg, uint8_t* vimg, int first, int last, bool values, int tid) {
-    const int u = tid & 127, o = u % kOct, r = u / kOct;
-    if (!values) {
+  __device__ __forceinline__ void store(uint8_t* kimg, uint8_t* vimg, int o, int r) const {
 #pragma unroll
-      for (int n = 0; n < 8; ++n)
-        *reinterpret_cast<u4v*>(kimg + (r + (128 / kOct) * n) * kPitchK<D> + 16 * o) = w[n];
-      return;
-    }
-    if (first + kTok<D> - 1 > last) {  // tokens past the sequence: no value may enter a product
-#pragma unroll
-      for (int n = 0; n < 8; ++n)
-        if (first + v_token(r, n) > last) w[n] = u4v{0, 0, 0, 0};
-    }
-#pragma unroll
-    for (int ch = 0; ch < 8; ++ch) {
-      u4v x;
-#pragma unroll
-      for (int p = 0; p < 4; ++p)
-        x[p] = __builtin_amdgcn_perm(w[2 * p + 1][ch >> 1], w[2 * p][ch >> 1], ch & 1 ? 0x07060302u : 0x05040100u);
-      *reinterpret_cast<u4v*>(vimg + r * kPitchV<D> + 16 * (9 * o + ch)) = x;
+    for (int n = 0; n < kPieces; ++n) {
+      const int t = r + kStep * n;
+      *reinterpret_cast<u4v*>(kimg + t * kPitchK<D> + 16 * o) = k[n];
+      *reinterpret_cast<u4v*>(vimg + t * 2 * D + 16 * (o ^ v_turn<D>(t))) = v[n];
     }
   }
 };
 
-// One workgroup: 128 query rows of one head (four waves of 32) against the keys up to its
-// last row, in tiles of kTok<D> tokens.
+// One workgroup: 128 query rows of one head (four waves of 32) against the keys up to its last
+// row, in tiles of kTok tokens, double-buffered in LDS and loaded one tile ahead through
+// registers.  A wave works in steps of 32 tokens, each in two phases:
+//   V(s)  softmax of the scores of step s, after the reads of the next phase's operands from
+//         LDS (values of s, keys of s + 1); in a tile's first step the tile after it goes to LDS
+//   M(s)  O^T += V^T P^T of step s, S^T = K Q^T of step s + 1: matrix instructions only
+// so that one wave's matrix instructions run beside the softmax of the other wave of its SIMD,
+// which belongs to another workgroup (two share a CU).  A barrier ends every step: tile t is
+// last read in V(2 t + 1), overwritten by tile t + 2 in V(2 t + 2), and that first read (its
+// keys) in V(2 t + 3).
 template <int D>
 __global__ __launch_bounds__(256, 2) void prompt_kernel(PromptArgs a) {
-  constexpr int NM = D / 32, NK = D / 16, TOK = kTok<D>, NT = TOK / 32;
+  constexpr int NM = D / 32, NK = D / 16;
+  using St = Stage<D>;
   __shared__ __align__(16) uint8_t kimg[2][kBytesK<D>];
   __shared__ __align__(16) uint8_t vimg[2][kBytesV<D>];
+  __shared__ int odd_tile[2];  // per buffer: one more than the last tile whose values are not all finite
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int col = lane & 31, h = lane >> 5;
   // KV head fastest: where there are 8 KV heads (or a divisor of 8) the workgroups of one
@@ -182,16 +184,22 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(PromptArgs a) {
   const int last_row = min(len, q0 + kRows) - 1;
   const int w0 = q0 + 32 * wave;                 // the wave's first row
   const int row = min(w0 + col, len - 1);
+  const int nt = last_row / kTok + 1;
+  const int live = w0 < len ? w0 / 32 + 1 : 0;   // steps in which some row of the wave sees a token
 
-  const uint16_t* kb = a.k + row_base(a.sk, a.sl, en.j, kvh);
-  const uint16_t* vb = a.v + row_base(a.sv, a.sl, en.j, kvh);
-  const bool values = wave >= 2;
-  const uint16_t* sbase = values ? vb : kb;
-  const int64_t sstride = values ? a.sv.token : a.sk.token;
-  const int nt = last_row / TOK + 1;
+  const int oct = tid % St::kOct, r0 = tid / St::kOct;
+  const uint16_t* kp = a.k + row_base(a.sk, a.sl, en.j, kvh) + (int64_t)r0 * a.sk.token + 8 * oct;
+  const uint16_t* vp = a.v + row_base(a.sv, a.sl, en.j, kvh) + (int64_t)r0 * a.sv.token + 8 * oct;
+  St stg;
+  const auto load = [&](int tile) { stg.load(kp, vp, a.sk.token, a.sv.token, tile * kTok, len - 1, r0); };
+  const auto masked = [&](int tile) { return (tile + 1) * kTok - 1 > q0; };  // some row does not see all of it
+  const auto store = [&](int tile) {
+    stg.store(kimg[tile & 1], vimg[tile & 1], oct, r0);
+    if (masked(tile))
+      if (stg.nonfinite()) odd_tile[tile & 1] = tile + 1;
+  };
 
-  Stage<D> stg;
-  stg.load(sbase, sstride, 0, len - 1, values, tid);
+  load(0);
   u4v qf[NK];
   {
     const uint16_t* qp = a.q + row_base(a.sq, a.sl, en.j, head) + (int64_t)row * a.sq.token + 8 * h;
@@ -204,62 +212,90 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(PromptArgs a) {
         for (int i = 0; i < 4; ++i) qf[j][i] = a.qsign < 0 ? qf[j][i] ^ 0x80008000u : 0u;
     }
   }
+  if (tid < 2) odd_tile[tid] = 0;
   RowState<NM> st;
   st.clear();
-  stg.store(kimg[0], vimg[0], 0, len - 1, values, tid);
-  bool bad = TOK - 1 > q0 && values && stg.nonfinite();
-  if (nt > 1) stg.load(sbase, sstride, TOK, len - 1, values, tid);
-  bool careful = false;
-  if (TOK - 1 > q0) careful = __syncthreads_or(bad);
-  else __syncthreads();
+  __syncthreads();
+  store(0);
+  if (nt > 1) load(1);
+  __syncthreads();
 
-  for (int t = 0; t < nt; ++t) {
-    const int t0 = t * TOK, buf = t & 1;
-    const uint8_t* vp = vimg[buf] + h * kPitchV<D> + 16 * (col + (col >> 3));
-    if (careful) {  // (the tile's values stay as they are until every wave has read them)
-      take_nonfinite<NM, NT, false>(
-          st, [&](int i, int x, int m) { return *reinterpret_cast<const u4v*>(vp + 2 * (2 * i + x) * kPitchV<D> + 16 * 36 * m); },
-          [&](int i, int k) { return (uint32_t)((row - t0 - 32 * i - tile_row(k, h)) >> 31); });
-      __syncthreads();
-      for (int i = tid; i < kBytesV<D> / 16; i += 256) {
-        u4v* p = reinterpret_cast<u4v*>(vimg[buf]) + i;
-        *p = only_finite<false>(*p);
-      }
-      __syncthreads();
+  // Key operand of step s, k-step j: token 32 s + col, octet 2 j + h.
+  const int kat = col * kPitchK<D> + 16 * h;
+  u4v kf[NK];
+  const auto read_keys = [&](int s) {
+    const uint8_t* p = kimg[(s >> 1) & 1] + 32 * (s & 1) * kPitchK<D> + kat;
+#pragma unroll
+    for (int j = 0; j < NK; ++j) kf[j] = *reinterpret_cast<const u4v*>(p + 32 * j);
+  };
+  // Value operand of step s, k-step x, channel tile m: channel 32 m + col, tokens
+  // 16 x + 4 h + {0 .. 3, 8 .. 11} of the step.  The lane points at token 4 h + (lane / 4) % 4,
+  // channels 16 (lane / 16 % 2) + 4 (lane % 4) of a transposing read.
+  const int vtok = 4 * h + ((lane >> 2) & 3), vunit = 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1);
+  int vat[NM];
+#pragma unroll
+  for (int m = 0; m < NM; ++m) vat[m] = vtok * 2 * D + 16 * ((4 * m + vunit) ^ v_turn<D>(vtok)) + 8 * (lane & 1);
+  const auto value_unit = [&](int s, int x, int m) {
+    const uint8_t* p = vimg[(s >> 1) & 1] + vat[m] + (32 * (s & 1) + 16 * x) * 2 * D;
+    const u2v lo = read_transposed(p), hi = read_transposed(p + 8 * 2 * D);
+    return u4v{lo[0], lo[1], hi[0], hi[1]};
+  };
+  f16v sc[1] = {zero16()};
+  const auto scores = [&]() {
+    sc[0] = zero16();
+#pragma unroll
+    for (int j = 0; j < NK; ++j) sc[0] = mfma32<false>(kf[j], qf[j], sc[0]);
+  };
+
+  if (live > 0) {
+    read_keys(0);
+    scores();
+  }
+  for (int s = 0; s < 2 * nt; ++s) {
+    u4v vf[2][NM], p[1][2];
+    // V(s)
+    if (s < live) {
+#pragma unroll
+      for (int x = 0; x < 2; ++x)
+#pragma unroll
+        for (int m = 0; m < NM; ++m) vf[x][m] = value_unit(s, x, m);
+      if (s + 1 < live) read_keys(s + 1);
+      __builtin_amdgcn_sched_barrier(0);
     }
-    if (t + 1 < nt) {
-      stg.store(kimg[buf ^ 1], vimg[buf ^ 1], t0 + TOK, len - 1, values, tid);
-      bad = t0 + 2 * TOK - 1 > q0 && values && stg.nonfinite();
+    if (!(s & 1)) {
+      const int t = s >> 1;
+      if (t + 1 < nt) store(t + 1);
+      if (t + 2 < nt) load(t + 2);
     }
-    if (t + 2 < nt) stg.load(sbase, sstride, t0 + 2 * TOK, len - 1, values, tid);
-    if (t0 <= w0 + 31 && w0 < len) {
-      f16v s[NT];
+    if (s < live) {
+      if (32 * s + 31 > w0) {
+        asm volatile("");  // a branch: as selects these would cost every step a quarter of its vector work
 #pragma unroll
-      for (int i = 0; i < NT; ++i) s[i] = zero16();
-      const uint8_t* kp = kimg[buf] + col * kPitchK<D> + 16 * h;
-#pragma unroll
-      for (int i = 0; i < NT; ++i)
-#pragma unroll
-        for (int j = 0; j < NK; ++j)
-          s[i] = mfma32<false>(*reinterpret_cast<const u4v*>(kp + 32 * i * kPitchK<D> + 32 * j), qf[j], s[i]);
-      if (t0 + TOK - 1 > w0) {
-#pragma unroll
-        for (int i = 0; i < NT; ++i)
-#pragma unroll
-          for (int k = 0; k < 16; ++k) s[i][k] = t0 + 32 * i + tile_row(k, h) <= w0 + col ? s[i][k] : -INFINITY;
+        for (int k = 0; k < 16; ++k) sc[0][k] = 32 * s + tile_row(k, h) <= w0 + col ? sc[0][k] : -INFINITY;
       }
-      u4v p[NT][2];
-      softmax_step<NM, NT, false>(st, s, a.c, 0.0f, p);
-#pragma unroll
-      for (int i = 0; i < NT; ++i)
+      softmax_step<NM, 1, false>(st, sc, a.c, 0.0f, p);
+      if (masked(s >> 1) && odd_tile[(s >> 1) & 1] == (s >> 1) + 1) {
+        asm volatile("");
+        take_nonfinite<NM, 1, false>(
+            st, [&](int, int x, int m) { return vf[x][m]; },
+            [&](int, int k) { return (uint32_t)((row - 32 * s - tile_row(k, h)) >> 31); });
 #pragma unroll
         for (int x = 0; x < 2; ++x)
 #pragma unroll
-          for (int m = 0; m < NM; ++m)
-            st.o[m] = mfma32<false>(*reinterpret_cast<const u4v*>(vp + 2 * (2 * i + x) * kPitchV<D> + 16 * 36 * m), p[i][x], st.o[m]);
+          for (int m = 0; m < NM; ++m) vf[x][m] = only_finite<false>(vf[x][m]);
+      }
     }
-    if (t0 + 2 * TOK - 1 > q0) careful = __syncthreads_or(bad);
-    else __syncthreads();
+    __builtin_amdgcn_sched_barrier(0);
+    // M(s)
+    if (s < live) {
+#pragma unroll
+      for (int x = 0; x < 2; ++x)
+#pragma unroll
+        for (int m = 0; m < NM; ++m) st.o[m] = mfma32<false>(vf[x][m], p[0][x], st.o[m]);
+    }
+    if (s + 1 < live) scores();
+    __builtin_amdgcn_sched_barrier(0);
+    __syncthreads();
   }
 
   if (w0 + col >= len) return;
@@ -362,6 +398,7 @@ __global__ __launch_bounds__(256, 2) void weight_kernel(WeightArgs a) {
         const float l2 = lse2[buf][32 * y + col];
         const int row = q0 + 32 * y + col;
         if (q0 + 32 * y < kw + 63) {  // some row of the subtile precedes some key of the wave
+          asm volatile("");  // (a branch, not selects in every step)
 #pragma unroll
           for (int i = 0; i < 2; ++i)
 #pragma unroll

@@ -57,6 +57,14 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
 // Product row of element e in half h of a 32-token subtile.
 __device__ __forceinline__ constexpr int tile_row(int e, int h) { return 8 * (e >> 2) + 4 * h + (e & 3); }
 
+// Transposing read of LDS: of sixteen lanes, four each point at sixteen consecutive 16-bit values
+// of one row (lane 4 r + i at values 4 i .. 4 i + 3 of row r); lane n receives value n of the four
+// rows.  (The layout was checked on gfx950 lane by lane.)
+__device__ __forceinline__ u2v read_transposed(const uint8_t* p) {
+  typedef short s4v __attribute__((ext_vector_type(4)));
+  return bitcast<u2v>(__builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s4v*)(p)));
+}
+
 // Running state of a wave's 32 query rows: output accumulators (32 NM channels), reference
 // maximum in base-2 logits, and the lane's share of the sum.
 template <int NM>
@@ -90,7 +98,8 @@ __device__ __forceinline__ void softmax_step(RowState<NM>& st, f16v (&s)[NT], fl
   mx = halves_max(mx) * c;
   if (__any(mx > st.m + kSlack)) {
     const float mnew = fmaxf(st.m, mx);
-    const float alpha = mnew == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(st.m - mnew);
+    // (a row without mass has outputs of 0, or infinities and NaN by take_nonfinite: they stay)
+    const float alpha = st.m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(st.m - mnew);
     st.m = mnew;
     st.l *= alpha;
 #pragma unroll
@@ -137,49 +146,36 @@ __device__ __forceinline__ u4v only_finite(u4v w) {
 // Infinite and NaN values in a tile that some rows may not see wholly: a masked place has
 // probability 0, and 0 times infinity would reach every row of the product.  The values a row
 // does see are counted by kind in products of indicators, and each kind present is added to
-// the row's outputs (p > 0 times an infinity or a NaN is that value); the caller then replaces
-// them by zero in the tile.  unit(i, x, m): the value operand of subtile i, k-step x, channel
-// tile m.  Rare.
+// the row's outputs (p > 0 times an infinity or a NaN is that value); the caller then takes the
+// product over the finite ones.  unit(i, x, m): the value operand of subtile i, k-step x, channel
+// tile m; hidden(i, e): all ones where the row does not see element e of subtile i, else 0.  Rare.
 template <int NM, int NT, bool HALF, class Unit, class Hidden>
 __device__ __forceinline__ void take_nonfinite(RowState<NM>& st, Unit unit, Hidden hidden) {
   constexpr uint32_t kOne = HALF ? 0x3c00u : 0x3f80u, kExp = HALF ? 0x7c00u : 0x7f80u;
-  // the rows' visible places as ones, built by arithmetic: kept lane masks would fill the
-  // scalar registers
-  u4v seen[NT][2];
-#pragma unroll
-  for (int i = 0; i < NT; ++i)
-#pragma unroll
-    for (int x = 0; x < 2; ++x)
-#pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        const int e = 8 * x + 2 * w;  // hidden(i, e): all ones where the row does not see it, else 0
-        seen[i][x][w] = (kOne & ~hidden(i, e)) | ((kOne << 16) & ~hidden(i, e + 1));
-      }
 #pragma unroll 1
   for (int kind = 0; kind < 3; ++kind) {  // +infinity, -infinity, NaN
     // a 16-bit value b is of the kind if (b & keep) - lo < span (unsigned)
     const uint32_t keep = kind == 2 ? 0x7fffu : 0xffffu, lo = kind == 0 ? kExp : (kind == 1 ? kExp | 0x8000u : kExp + 1);
     const uint32_t span = kind == 2 ? 0x8000u - (kExp + 1) : 1u;
-#pragma unroll 1
+#pragma unroll
     for (int m = 0; m < NM; ++m) {
       f16v n = zero16();
 #pragma unroll
       for (int i = 0; i < NT; ++i)
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
-          u4v v = unit(i, x, m);
+          u4v v = unit(i, x, m), seen;
 #pragma unroll
-          for (int w = 0; w < 4; ++w)
+          for (int w = 0; w < 4; ++w) {
+            const int e = 8 * x + 2 * w;
+            seen[w] = (kOne & ~hidden(i, e)) | ((kOne << 16) & ~hidden(i, e + 1));
             v[w] = ((v[w] & keep) - lo < span ? kOne : 0u) | (((v[w] >> 16) & keep) - lo < span ? kOne << 16 : 0u);
-          n = mfma32<HALF>(v, seen[i][x], n);
+          }
+          n = mfma32<HALF>(v, seen, n);
         }
       const float add = kind == 0 ? INFINITY : (kind == 1 ? -INFINITY : __builtin_nanf(""));
 #pragma unroll
-      for (int c = 0; c < NM; ++c)  // (a register array takes no run-time index)
-        if (c == m) {
-#pragma unroll
-          for (int e = 0; e < 16; ++e) st.o[c][e] = n[e] > 0.0f ? st.o[c][e] + add : st.o[c][e];
-        }
+      for (int e = 0; e < 16; ++e) st.o[m][e] = n[e] > 0.0f ? st.o[m][e] + add : st.o[m][e];
     }
   }
 }

@@ -84,7 +84,8 @@ def load() -> ctypes.CDLL:
             "kvk_prompt_attention": (I32, [I32, I32, I32, I32, P, P, P, P, P, F, P, P, P]),
             "kvk_attention_weight_workspace_bytes": (I32, [I32, I32, I32, I32, P, ctypes.POINTER(ctypes.c_size_t)]),
             "kvk_attention_weight": (I32, [I32, I32, I32, I32, P, P, P, P, P, F, P, P, ctypes.c_size_t, P]),
-            "kvk_keep_heaviest": (I32, [P, P, I32, I32, P, P]),
+            "kvk_keep_workspace_bytes": (I32, [P, I32, ctypes.POINTER(ctypes.c_size_t)]),
+            "kvk_keep_heaviest": (I32, [P, P, I32, I32, P, P, ctypes.c_size_t, P]),
             "kvk_append_chunk": (I32, [P, I32, I32, P, P, I32, I32, P, P, P, P]),
             "kvk_chunk_workspace_bytes": (I32, [P, I32, I32, I32, ctypes.POINTER(ctypes.c_size_t)]),
             "kvk_chunk_attention": (I32, [P, I32, I32, P, I32, P, P, F, P, P, P, ctypes.c_size_t, P]),
@@ -116,7 +117,8 @@ def exported_symbols() -> List[str]:
             "kvk_snapkv_select_mla",
             "kvk_append_token", "kvk_snapkv_workspace_bytes", "kvk_snapkv_select",
             "kvk_selector_weight_elems", "kvk_selector_workspace_bytes", "kvk_selector_forward",
-            "kvk_prompt_attention", "kvk_attention_weight_workspace_bytes", "kvk_attention_weight", "kvk_keep_heaviest",
+            "kvk_prompt_attention", "kvk_attention_weight_workspace_bytes", "kvk_attention_weight", "kvk_keep_workspace_bytes",
+            "kvk_keep_heaviest",
             "kvk_append_chunk", "kvk_chunk_workspace_bytes", "kvk_chunk_attention",
             "kvk_decode_attention", "kvk_decode_splits", "kvk_decode_merge", "kvk_decode_attention_noalloc", "kvk_decode_setup",
             "kvk_read_bytes", "kvk_debug_dequantize",
@@ -511,45 +513,55 @@ def selector_forward(d_model: int, n_layers: int, weights: torch.Tensor, emb: to
                                        _nbytes(workspace), _stream(stream)))
 
 
-class Strides(ctypes.Structure):
-    _fields_ = [("seq", ctypes.c_int64), ("head", ctypes.c_int64), ("token", ctypes.c_int64)]
-
-
 def _here(*tensors):
-    """The multi-token calls' buffers lie on the current device, whose stream they run on."""
-    dev = torch.cuda.current_device() if torch.cuda.is_available() else None
+    """The multi-token calls' buffers lie on the current device, whose stream they run on.
+    (get_device, -1 on the host: a third of the time of the device objects.)"""
+    dev = torch.cuda.current_device() if torch.cuda.is_initialized() else 0
     for x in tensors:
-        _need(x is None or (x.is_cuda and x.device.index == dev), "buffers must be GPU tensors on the current device")
+        if x is not None and x.get_device() != dev:
+            raise ValueError("buffers must be GPU tensors on the current device")
 
 
 def _lengths(n, count: int, name: str):
     """A host int32 array of `count` lengths from one number or one per sequence."""
-    vals = [int(n)] * count if isinstance(n, int) else [int(x) for x in n]
-    _need(len(vals) == count, f"{name} must hold one length per sequence ({count})")
-    _need(all(-2**31 <= x < 2**31 for x in vals), f"{name} beyond 32 bits")
+    vals = [n] * count if isinstance(n, int) else [int(x) for x in n]
+    if len(vals) != count:
+        raise ValueError(f"{name} must hold one length per sequence ({count})")
+    if vals and not (-2**31 <= min(vals) and max(vals) < 2**31):
+        raise ValueError(f"{name} beyond 32 bits")
     return (ctypes.c_int32 * count)(*vals)
 
 
-def _row_strides(x: torch.Tensor, lens: Sequence[int], name: str) -> Strides:
-    """Where the rows of a packed [tokens, heads, d] or padded [B, heads, n, d] tensor lie."""
-    _need(x.dim() in (3, 4) and (x.stride(-1) == 1 or x.numel() == 0), f"{name}: [tokens, heads, d] or [B, heads, n, d], rows contiguous")
-    if x.dim() == 3:
-        _need(x.shape[0] == sum(lens), f"{name} must hold the tokens of all sequences ({sum(lens)})")
-        return Strides(0, x.stride(1) if x.shape[1] > 1 else x.shape[2], x.stride(0) if x.shape[0] > 1 else x.shape[1] * x.shape[2])
-    _need(x.shape[0] == len(lens) and x.shape[2] >= max(lens, default=0), f"{name} must hold every sequence's tokens")
-    b, h, n, d = x.shape
+def _row_strides(x: torch.Tensor, name: str, rank: int, width: int, total: int, count: int, longest: int):
+    """Where the rows of a packed [tokens, heads, d] or padded [B, heads, n, d] bf16 tensor lie:
+    element strides of sequence, head and token."""
+    shape, st = x.shape, x.stride()
+    if x.dtype != torch.bfloat16 or len(shape) != rank or shape[-1] != width or st[-1] != 1:
+        raise ValueError(f"{name} must be bf16, of q's layout and head width, with contiguous rows")
     # the stride of a dimension of one element is never taken: any valid one stands for it
-    return Strides(x.stride(0) if b > 1 else h * n * d, x.stride(1) if h > 1 else n * d, x.stride(2) if n > 1 else d)
+    if rank == 3:
+        n, h, d = shape
+        if n != total:
+            raise ValueError(f"{name} must hold the tokens of all sequences ({total})")
+        return 0, st[1] if h > 1 else d, st[0] if n > 1 else h * d
+    b, h, n, d = shape
+    if b != count or n < longest:
+        raise ValueError(f"{name} must hold every sequence's tokens")
+    return st[0] if b > 1 else h * n * d, st[1] if h > 1 else n * d, st[2] if n > 1 else d
 
 
 def _prompt_args(q: torch.Tensor, others, seq_tokens: Sequence[int]):
+    """The sequences' count, total and C array of lengths, and the C array of strides."""
     lens = [int(n) for n in seq_tokens]
-    _need(all(n >= 0 for n in lens), "sequence lengths must not be negative")
-    for name, x in [("q", q)] + others:
-        _need(x.dtype == torch.bfloat16, f"{name} must be bf16")
-        _need(x.dim() == q.dim() and x.shape[-1] == q.shape[-1], f"{name}: of q's layout and head width")
-    strides = [_row_strides(x, lens, name) for name, x in [("q", q)] + others]
-    return lens, (Strides * len(strides))(*strides)
+    total, count, longest, rank = sum(lens), len(lens), max(lens, default=0), q.dim()
+    if rank not in (3, 4) or min(lens, default=0) < 0:
+        raise ValueError("q must be [tokens, heads, d] or [B, heads, n, d], and sequence lengths not negative")
+    width = q.shape[-1]
+    flat = [*_row_strides(q, "q", rank, width, total, count, longest)]
+    for name, x in others:
+        flat += _row_strides(x, name, rank, width, total, count, longest)
+    # kvk_strides entries are three 64-bit numbers each
+    return count, total, _lengths(lens, count, "seq_tokens"), (ctypes.c_int64 * len(flat))(*flat)
 
 
 def prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, seq_tokens: Sequence[int], scale: float,
@@ -558,15 +570,15 @@ def prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, seq_toke
     sequences one after another) or padded [B, heads, n, d]; any strides with contiguous rows
     (views of a fused projection).  seq_tokens: the sequences' lengths.  lse (optional) fp32,
     contiguous: Hq * tokens values, per sequence [Hq, length] (see kvk.h)."""
-    lens, st = _prompt_args(q, [("k", k), ("v", v), ("out", out)], seq_tokens)
+    count, total, lens, strides = _prompt_args(q, (("k", k), ("v", v), ("out", out)), seq_tokens)
     Hq, Hkv = q.shape[1], k.shape[1]
-    _need(v.shape[1] == Hkv and out.shape[1] == Hq, "k and v must have the same heads, out those of q")
+    if v.shape[1] != Hkv or out.shape[1] != Hq:
+        raise ValueError("k and v must have the same heads, out those of q")
     _here(q, k, v, out, lse)
-    if lse is not None:
-        _need(lse.dtype == torch.float32 and lse.is_contiguous() and lse.numel() == Hq * sum(lens),
-              "lse must be contiguous fp32, Hq values per token")
-    _check(load().kvk_prompt_attention(Hq, Hkv, q.shape[-1], len(lens), _lengths(lens, len(lens), "seq_tokens"), _ptr(q),
-                                       _ptr(k), _ptr(v), st, float(scale), _ptr(out), _ptr(lse), _stream(stream)))
+    if lse is not None and (lse.dtype != torch.float32 or not lse.is_contiguous() or lse.numel() != Hq * total):
+        raise ValueError("lse must be contiguous fp32, Hq values per token")
+    _check(load().kvk_prompt_attention(Hq, Hkv, q.shape[-1], count, lens, q.data_ptr(), k.data_ptr(), v.data_ptr(), strides,
+                                       scale, out.data_ptr(), None if lse is None else lse.data_ptr(), _stream(stream)))
 
 
 def attention_weight_workspace_bytes(n_q_heads: int, n_kv_heads: int, head_dim: int, seq_tokens: Sequence[int]) -> int:
@@ -582,30 +594,49 @@ def attention_weight(q: torch.Tensor, k: torch.Tensor, lse: torch.Tensor, seq_to
     """The attention weight each position collects over a prompt's rows.  q, k as for
     prompt_attention, lse as it returns it; weight fp32, contiguous: Hkv * tokens values, per
     sequence [Hkv, length]."""
-    lens, st = _prompt_args(q, [("k", k)], seq_tokens)
+    count, total, lens, strides = _prompt_args(q, (("k", k),), seq_tokens)
     Hq, Hkv = q.shape[1], k.shape[1]
     _here(q, k, lse, weight, workspace)
-    _need(lse.dtype == torch.float32 and lse.is_contiguous() and lse.numel() == Hq * sum(lens),
-          "lse must be contiguous fp32, Hq values per token")
-    _need(weight.dtype == torch.float32 and weight.is_contiguous() and weight.numel() == Hkv * sum(lens),
-          "weight must be contiguous fp32, Hkv values per token")
-    _check(load().kvk_attention_weight(Hq, Hkv, q.shape[-1], len(lens), _lengths(lens, len(lens), "seq_tokens"), _ptr(q),
-                                       _ptr(k), st, _ptr(lse), float(scale), _ptr(weight), _ptr(workspace),
+    if lse.dtype != torch.float32 or not lse.is_contiguous() or lse.numel() != Hq * total:
+        raise ValueError("lse must be contiguous fp32, Hq values per token")
+    if weight.dtype != torch.float32 or not weight.is_contiguous() or weight.numel() != Hkv * total:
+        raise ValueError("weight must be contiguous fp32, Hkv values per token")
+    _check(load().kvk_attention_weight(Hq, Hkv, q.shape[-1], count, lens, q.data_ptr(), k.data_ptr(), strides,
+                                       lse.data_ptr(), scale, weight.data_ptr(),
+                                       None if workspace is None else workspace.data_ptr(),
                                        0 if workspace is None else _nbytes(workspace), _stream(stream)))
 
 
-def keep_heaviest(t: Table, weight: torch.Tensor, n_tokens: int, n_recent: int, keep_out: torch.Tensor, stream=None):
+def keep_workspace_bytes(t: Table, n_tokens: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check(load().kvk_keep_workspace_bytes(t.handle, n_tokens, ctypes.byref(out)))
+    return out.value
+
+
+KEEP_RESIDENT = 16384  # streams of up to so many tokens need no workspace
+
+
+def keep_heaviest(t: Table, weight: torch.Tensor, n_tokens: int, n_recent: int, keep_out: torch.Tensor,
+                  workspace: Optional[torch.Tensor] = None, stream=None):
     """The keep list of the last n_recent positions and the heaviest earlier ones.  weight fp32
     [B, Hkv, n_tokens] (MLA: [B, n_tokens]); keep_out int32 [B, Hkv, keep_tokens] (MLA:
-    [B, keep_tokens]), which compress_layer takes."""
+    [B, keep_tokens]), which compress_layer takes.  workspace: keep_workspace_bytes bytes;
+    without one, what a long prompt needs comes from torch's allocator for the call."""
     d = t.dims
     streams = d.batch if d.kind == MLA else d.batch * d.n_kv_heads
     _here(weight, keep_out)
-    _need(weight.dtype == torch.float32 and weight.is_contiguous() and weight.numel() == streams * n_tokens,
-          "weight must be contiguous fp32, streams*n_tokens")
-    _need(keep_out.dtype == torch.int32 and keep_out.is_contiguous() and keep_out.numel() == streams * d.keep_tokens,
-          "keep_out must be contiguous int32, streams*keep_tokens")
-    _check(load().kvk_keep_heaviest(t.handle, _ptr(weight), n_tokens, n_recent, _ptr(keep_out), _stream(stream)))
+    if weight.dtype != torch.float32 or not weight.is_contiguous() or weight.numel() != streams * n_tokens:
+        raise ValueError("weight must be contiguous fp32, streams*n_tokens")
+    if keep_out.dtype != torch.int32 or not keep_out.is_contiguous() or keep_out.numel() != streams * d.keep_tokens:
+        raise ValueError("keep_out must be contiguous int32, streams*keep_tokens")
+    if workspace is None and n_tokens > KEEP_RESIDENT:
+        workspace = torch.empty(keep_workspace_bytes(t, n_tokens), dtype=torch.uint8, device=weight.device)
+        if stream is not None:
+            workspace.record_stream(stream)
+    _here(workspace)
+    _check(load().kvk_keep_heaviest(t.handle, weight.data_ptr(), n_tokens, n_recent, keep_out.data_ptr(),
+                                    None if workspace is None else workspace.data_ptr(),
+                                    0 if workspace is None else _nbytes(workspace), _stream(stream)))
 
 
 def append_chunk(t: Table, layer_begin: int, layer_end: int, k: torch.Tensor, v: torch.Tensor, n_stored, n_new,
@@ -614,17 +645,18 @@ def append_chunk(t: Table, layer_begin: int, layer_end: int, k: torch.Tensor, v:
     [layers, B, Hkv, chunk, d_h], contiguous bf16/fp32; n_stored (before the call) and n_new
     (None: the whole chunk): one length, or one per sequence, on the host."""
     d = t.dims
-    nl = layer_end - layer_begin
-    _need(k.dtype == v.dtype and k.is_contiguous() and v.is_contiguous() and k.dim() == 5 and k.shape == v.shape,
-          "k and v must be contiguous [layers, B, Hkv, chunk, d_h] tensors of one dtype")
-    _need(d.kind == MLA or tuple(k.shape[:3]) + (k.shape[4],) == (nl, d.batch, d.n_kv_heads, d.head_dim),
-          "k/v must be [layers, B, Hkv, chunk, d_h]")
+    shape = k.shape
+    if k.dtype != v.dtype or not k.is_contiguous() or not v.is_contiguous() or len(shape) != 5 or shape != v.shape:
+        raise ValueError("k and v must be contiguous [layers, B, Hkv, chunk, d_h] tensors of one dtype")
+    B = d.batch
+    if d.kind != MLA and (shape[0], shape[1], shape[2], shape[4]) != (layer_end - layer_begin, B, d.n_kv_heads, d.head_dim):
+        raise ValueError("k/v must be [layers, B, Hkv, chunk, d_h]")
     _here(k, v, arena)
-    _need(_nbytes(arena) >= t.arena_bytes, "arena smaller than arena_bytes")
-    _check(load().kvk_append_chunk(t.handle, layer_begin, layer_end, _ptr(k), _ptr(v), _dtype_code(k), k.shape[3],
-                                   _lengths(n_stored, d.batch, "n_stored"),
-                                   None if n_new is None else _lengths(n_new, d.batch, "n_new"), _ptr(arena),
-                                   _stream(stream)))
+    if _nbytes(arena) < t.arena_bytes:
+        raise ValueError("arena smaller than arena_bytes")
+    _check(load().kvk_append_chunk(t.handle, layer_begin, layer_end, k.data_ptr(), v.data_ptr(), _dtype_code(k), shape[3],
+                                   _lengths(n_stored, B, "n_stored"), None if n_new is None else _lengths(n_new, B, "n_new"),
+                                   arena.data_ptr(), _stream(stream)))
 
 
 def chunk_workspace_bytes(t: Table, layer_begin: int, layer_end: int, n_chunk: int) -> int:
@@ -639,17 +671,20 @@ def chunk_attention(t: Table, layer_begin: int, layer_end: int, q: torch.Tensor,
     [layers, B, Hq, chunk, d_h]; n_stored (the chunk among them) and n_new (None: the whole
     chunk): one length, or one per sequence, on the host.  Rows past n_new stay as they were."""
     d = t.dims
-    nl = layer_end - layer_begin
-    _need(q.dtype == out.dtype == torch.bfloat16 and q.is_contiguous() and out.is_contiguous() and q.dim() == 5 and
-          q.shape == out.shape, "q and out must be contiguous bf16 [layers, B, Hq, chunk, d_h]")
-    _need(d.kind == MLA or tuple(q.shape[:3]) + (q.shape[4],) == (nl, d.batch, d.n_q_heads, d.head_dim),
-          "q must be [layers, B, Hq, chunk, d_h]")
+    shape = q.shape
+    if (q.dtype != torch.bfloat16 or out.dtype != torch.bfloat16 or not q.is_contiguous() or not out.is_contiguous()
+            or len(shape) != 5 or shape != out.shape):
+        raise ValueError("q and out must be contiguous bf16 [layers, B, Hq, chunk, d_h]")
+    B = d.batch
+    if d.kind != MLA and (shape[0], shape[1], shape[2], shape[4]) != (layer_end - layer_begin, B, d.n_q_heads, d.head_dim):
+        raise ValueError("q must be [layers, B, Hq, chunk, d_h]")
     _here(q, arena, out, workspace)
-    _need(_nbytes(arena) >= t.arena_bytes, "arena smaller than arena_bytes")
-    _check(load().kvk_chunk_attention(t.handle, layer_begin, layer_end, _ptr(q), q.shape[3],
-                                      _lengths(n_stored, d.batch, "n_stored"),
-                                      None if n_new is None else _lengths(n_new, d.batch, "n_new"), float(scale),
-                                      _ptr(arena), _ptr(out), _ptr(workspace), _nbytes(workspace), _stream(stream)))
+    if _nbytes(arena) < t.arena_bytes:
+        raise ValueError("arena smaller than arena_bytes")
+    _check(load().kvk_chunk_attention(t.handle, layer_begin, layer_end, q.data_ptr(), shape[3],
+                                      _lengths(n_stored, B, "n_stored"), None if n_new is None else _lengths(n_new, B, "n_new"),
+                                      scale, arena.data_ptr(), out.data_ptr(), workspace.data_ptr(), _nbytes(workspace),
+                                      _stream(stream)))
 
 
 def decode_attention(t: Table, layer_begin: int, layer_end: int, q: torch.Tensor, n_stored: int,

@@ -234,7 +234,8 @@ def _keep_ref(w, keep, recent):
 
 
 @pytest.mark.parametrize("n,keep,recent", [(1, 1, 0), (1, 1, 1), (5, 3, 3), (64, 64, 0), (65, 1, 0), (1000, 250, 64), (1024, 1000, 0),
-                                           (4097, 33, 32), (16384, 8192, 1), (16400, 8200, 16), (16385, 1, 0), (40001, 20000, 333)])
+                                           (4097, 33, 32), (16384, 8192, 1), (16400, 8200, 16), (16385, 1, 0), (16385, 16385, 0),
+                                           (33000, 32999, 5), (40001, 20000, 333), (131072, 65536, 4096)])
 @pytest.mark.parametrize("kind", ["spread", "equal", "ties", "signs"])
 def test_keep_heaviest(n, keep, recent, kind):
     rng = np.random.default_rng(n + keep)

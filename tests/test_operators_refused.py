@@ -15,7 +15,7 @@ def _arr(vals):
 
 
 def _strides(*triples):
-    return (kvk.Strides * len(triples))(*[kvk.Strides(*t) for t in triples])
+    return (ctypes.c_int64 * (3 * len(triples)))(*[x for t in triples for x in t])  # kvk_strides entries
 
 
 def _refused(status, want, *words):
@@ -87,18 +87,33 @@ def _table(kind=kvk.GQA, **kw):
 
 
 def test_keep_heaviest():
-    call = kvk.load().kvk_keep_heaviest
+    lib = kvk.load()
+
+    def call(t, weight=P0, n=50, recent=0, out=P0, ws=None, ws_bytes=0):
+        return lib.kvk_keep_heaviest(t.handle if t else None, weight, n, recent, out, ws, ws_bytes, None)
+
     t = _table(keep_tokens=40)
-    _refused(call(None, P0, 50, 0, P0, None), kvk.ERR_INVALID, "NULL table")
-    _refused(call(_table().handle, P0, 50, 0, P0, None), kvk.ERR_INVALID, "does not evict")
-    _refused(call(t.handle, P0, 39, 0, P0, None), kvk.ERR_INVALID, "n_tokens 39")
-    _refused(call(t.handle, P0, 101, 0, P0, None), kvk.ERR_INVALID, "n_tokens 101")
-    _refused(call(t.handle, P0, 50, 41, P0, None), kvk.ERR_INVALID, "n_recent 41")
-    _refused(call(t.handle, P0, 50, -1, P0, None), kvk.ERR_INVALID, "n_recent -1")
-    _refused(call(t.handle, None, 50, 0, P0, None), kvk.ERR_INVALID, "NULL")
-    _refused(call(t.handle, P0, 50, 0, None, None), kvk.ERR_INVALID, "NULL")
-    _refused(call(t.handle, P0 + 2, 50, 0, P0, None), kvk.ERR_INVALID, "misaligned")
-    _refused(call(t.handle, P0, 50, 0, P0, None), kvk.ERR_INVALID, "not GPU-accessible")
+    _refused(call(None), kvk.ERR_INVALID, "NULL table")
+    _refused(call(_table()), kvk.ERR_INVALID, "does not evict")
+    _refused(call(t, n=39), kvk.ERR_INVALID, "n_tokens 39")
+    _refused(call(t, n=101), kvk.ERR_INVALID, "n_tokens 101")
+    _refused(call(t, recent=41), kvk.ERR_INVALID, "n_recent 41")
+    _refused(call(t, recent=-1), kvk.ERR_INVALID, "n_recent -1")
+    _refused(call(t, weight=None), kvk.ERR_INVALID, "NULL")
+    _refused(call(t, out=None), kvk.ERR_INVALID, "NULL")
+    _refused(call(t, weight=P0 + 2), kvk.ERR_INVALID, "misaligned")
+    _refused(call(t), kvk.ERR_INVALID, "not GPU-accessible")
+    assert kvk.keep_workspace_bytes(t, 100) == 0
+    t = _table(keep_tokens=40, max_tokens=40000)
+    sizes = [kvk.keep_workspace_bytes(t, n) for n in (16384, 16385, 32768, 40000)]
+    assert sizes[0] == 0 and sizes == sorted(sizes) and sizes[1] > 0
+    _refused(call(t, n=40000), kvk.ERR_INVALID, "NULL")
+    _refused(call(t, n=40000, ws=P0 + 128, ws_bytes=1 << 30), kvk.ERR_INVALID, "misaligned")
+    _refused(call(t, n=40000, ws=P0, ws_bytes=sizes[-1] - 1), kvk.ERR_BUFFER, "workspace")
+    _refused(call(t, n=40000, ws=P0, ws_bytes=sizes[-1]), kvk.ERR_INVALID, "not GPU-accessible")
+    out = ctypes.c_size_t()
+    _refused(lib.kvk_keep_workspace_bytes(_table().handle, 50, ctypes.byref(out)), kvk.ERR_INVALID, "does not evict")
+    _refused(lib.kvk_keep_workspace_bytes(t.handle, 50, None), kvk.ERR_INVALID)
 
 
 def _append(t, l0=0, l1=2, k=P0, v=P0, dtype=kvk.BF16, m=4, stored=(0, 10, 96), new=None, arena=P0):
