@@ -158,20 +158,32 @@ struct Stage {
 // One workgroup: 128 query rows of one head (four waves of 32) against the keys up to its last
 // row, in tiles of kTok tokens, double-buffered in LDS and loaded one tile ahead through
 // registers.  A wave works in steps of 32 tokens, each in two phases:
-//   V(s)  softmax of the scores of step s, after the reads of the next phase's operands from
-//         LDS (values of s, keys of s + 1); in a tile's first step the tile after it goes to LDS
-//   M(s)  O^T += V^T P^T of step s, S^T = K Q^T of step s + 1: matrix instructions only
+//   V(s)  softmax of the scores of step s: vector instructions
+//   M(s)  O^T += V^T P^T of step s with the reads of the next keys between its products, then
+//         S^T = K Q^T of step s + 1 with the reads of the next values: matrix instructions,
+//         whose issue leaves the time that the reads take (24 reads in a row take 400 clocks)
 // so that one wave's matrix instructions run beside the softmax of the other wave of its SIMD,
-// which belongs to another workgroup (two share a CU).  A barrier ends every step: tile t is
-// last read in V(2 t + 1), overwritten by tile t + 2 in V(2 t + 2), and that first read (its
-// keys) in V(2 t + 3).
+// which belongs to another workgroup (two share a CU).
+// Tile t is read in M(2 t - 1) and M(2 t).  Tile t + 1, in the buffer of tile t - 1, goes to LDS
+// after M(2 t - 1): the barrier after M(2 t - 2) lies behind the last reads of t - 1, the one
+// after M(2 t) before the first ones of t + 1.
+//
+// Bound: power, then issue.  With both matrix and vector units busy the clock falls to about 1.9
+// GHz; 40 / 8 heads of 128 over 8192 tokens take 730 us (940 TFLOP/s; an 8192-wide bf16 library
+// product reaches 1400 to 1550).  Of a step's 2100 clocks per wave (two waves share a SIMD) the
+// softmax takes 860, the products 670 (512 at the full rate), staging 510, the barrier 80.
+// Measured and not kept: eight waves with the last four a phase behind (barriers between
+// phases, 760 us), rows of 64 per wave at one wave per SIMD (accumulator copies, 1120), direct
+// loads to LDS in a ring of four steps (790), staging between the products too (787).
 template <int D>
 __global__ __launch_bounds__(256, 2) void prompt_kernel(PromptArgs a) {
   constexpr int NM = D / 32, NK = D / 16;
   using St = Stage<D>;
   __shared__ __align__(16) uint8_t kimg[2][kBytesK<D>];
   __shared__ __align__(16) uint8_t vimg[2][kBytesV<D>];
-  __shared__ int odd_tile[2];  // per buffer: one more than the last tile whose values are not all finite
+  // One more than the last tile (of those with these low bits) whose values are not all finite:
+  // tile t's is read up to V(2 t + 1), when a wave ahead may be storing tile t + 2.
+  __shared__ int odd_tile[4];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int col = lane & 31, h = lane >> 5;
   // KV head fastest: where there are 8 KV heads (or a divisor of 8) the workgroups of one
@@ -196,7 +208,7 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(PromptArgs a) {
   const auto store = [&](int tile) {
     stg.store(kimg[tile & 1], vimg[tile & 1], oct, r0);
     if (masked(tile))
-      if (stg.nonfinite()) odd_tile[tile & 1] = tile + 1;
+      if (stg.nonfinite()) odd_tile[tile & 3] = tile + 1;
   };
 
   load(0);
@@ -212,7 +224,7 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(PromptArgs a) {
         for (int i = 0; i < 4; ++i) qf[j][i] = a.qsign < 0 ? qf[j][i] ^ 0x80008000u : 0u;
     }
   }
-  if (tid < 2) odd_tile[tid] = 0;
+  if (tid < 4) odd_tile[tid] = 0;
   RowState<NM> st;
   st.clear();
   __syncthreads();
@@ -223,10 +235,8 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(PromptArgs a) {
   // Key operand of step s, k-step j: token 32 s + col, octet 2 j + h.
   const int kat = col * kPitchK<D> + 16 * h;
   u4v kf[NK];
-  const auto read_keys = [&](int s) {
-    const uint8_t* p = kimg[(s >> 1) & 1] + 32 * (s & 1) * kPitchK<D> + kat;
-#pragma unroll
-    for (int j = 0; j < NK; ++j) kf[j] = *reinterpret_cast<const u4v*>(p + 32 * j);
+  const auto key_unit = [&](int s, int j) {
+    return *reinterpret_cast<const u4v*>(kimg[(s >> 1) & 1] + 32 * (s & 1) * kPitchK<D> + kat + 32 * j);
   };
   // Value operand of step s, k-step x, channel tile m: channel 32 m + col, tokens
   // 16 x + 4 h + {0 .. 3, 8 .. 11} of the step.  The lane points at token 4 h + (lane / 4) % 4,
@@ -240,41 +250,33 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(PromptArgs a) {
     const u2v lo = read_transposed(p), hi = read_transposed(p + 8 * 2 * D);
     return u4v{lo[0], lo[1], hi[0], hi[1]};
   };
+
   f16v sc[1] = {zero16()};
-  const auto scores = [&]() {
-    sc[0] = zero16();
+  u4v vf[2][NM];
+  if (live > 0) {
+#pragma unroll
+    for (int j = 0; j < NK; ++j) kf[j] = key_unit(0, j);
 #pragma unroll
     for (int j = 0; j < NK; ++j) sc[0] = mfma32<false>(kf[j], qf[j], sc[0]);
-  };
-
-  if (live > 0) {
-    read_keys(0);
-    scores();
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+#pragma unroll
+      for (int m = 0; m < NM; ++m) vf[x][m] = value_unit(0, x, m);
   }
+  if (nt > 1) store(1);
+  if (nt > 2) load(2);
+  __syncthreads();
   for (int s = 0; s < 2 * nt; ++s) {
-    u4v vf[2][NM], p[1][2];
+    u4v p[1][2];
     // V(s)
     if (s < live) {
-#pragma unroll
-      for (int x = 0; x < 2; ++x)
-#pragma unroll
-        for (int m = 0; m < NM; ++m) vf[x][m] = value_unit(s, x, m);
-      if (s + 1 < live) read_keys(s + 1);
-      __builtin_amdgcn_sched_barrier(0);
-    }
-    if (!(s & 1)) {
-      const int t = s >> 1;
-      if (t + 1 < nt) store(t + 1);
-      if (t + 2 < nt) load(t + 2);
-    }
-    if (s < live) {
       if (32 * s + 31 > w0) {
-        asm volatile("");  // a branch: as selects these would cost every step a quarter of its vector work
+        asm volatile("");
 #pragma unroll
         for (int k = 0; k < 16; ++k) sc[0][k] = 32 * s + tile_row(k, h) <= w0 + col ? sc[0][k] : -INFINITY;
       }
       softmax_step<NM, 1, false>(st, sc, a.c, 0.0f, p);
-      if (masked(s >> 1) && odd_tile[(s >> 1) & 1] == (s >> 1) + 1) {
+      if (masked(s >> 1) && odd_tile[(s >> 1) & 3] == (s >> 1) + 1) {
         asm volatile("");
         take_nonfinite<NM, 1, false>(
             st, [&](int, int x, int m) { return vf[x][m]; },
@@ -284,18 +286,33 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(PromptArgs a) {
 #pragma unroll
           for (int m = 0; m < NM; ++m) vf[x][m] = only_finite<false>(vf[x][m]);
       }
+      __builtin_amdgcn_sched_barrier(0);
+      // M(s)
+      const int sn = min(s + 1, 2 * nt - 1);  // (past the last step: the last one's operands again, not used)
+#pragma unroll
+      for (int i = 0; i < 2 * NM; ++i) {
+        st.o[i % NM] = mfma32<false>(vf[i / NM][i % NM], p[0][i / NM], st.o[i % NM]);
+#pragma unroll
+        for (int j = i * NK / (2 * NM); j < (i + 1) * NK / (2 * NM); ++j) kf[j] = key_unit(sn, j);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      sc[0] = zero16();
+#pragma unroll
+      for (int j = 0; j < NK; ++j) {
+        sc[0] = mfma32<false>(kf[j], qf[j], sc[0]);
+#pragma unroll
+        for (int i = j * 2 * NM / NK; i < (j + 1) * 2 * NM / NK; ++i) vf[i / NM][i % NM] = value_unit(sn, i / NM, i % NM);
+        __builtin_amdgcn_sched_barrier(0);
+      }
     }
     __builtin_amdgcn_sched_barrier(0);
-    // M(s)
-    if (s < live) {
-#pragma unroll
-      for (int x = 0; x < 2; ++x)
-#pragma unroll
-        for (int m = 0; m < NM; ++m) st.o[m] = mfma32<false>(vf[x][m], p[0][x], st.o[m]);
+    const int t = (s + 1) >> 1;   // odd s = 2 t - 1: tile t + 1 to LDS; even s = 2 t: tile t + 2 from memory
+    if (s & 1) {
+      if (t + 1 < nt) store(t + 1);
+    } else {
+      if (t > 0 && t + 2 < nt) load(t + 2);
+      __syncthreads();
     }
-    if (s + 1 < live) scores();
-    __builtin_amdgcn_sched_barrier(0);
-    __syncthreads();
   }
 
   if (w0 + col >= len) return;
