@@ -505,7 +505,9 @@ kvk_status kvk_prompt_attention(int32_t n_q_heads, int32_t n_kv_heads, int32_t h
  *   weight    : device fp32, per sequence [Hkv][tokens], one sequence after another.
  *   workspace : device, >= kvk_attention_weight_workspace_bytes(...), 256-byte aligned (NULL
  *               where that is 0: one query head per KV head).
- * Sums are fp32 in a fixed order (two calls give the same bits).
+ * A row whose log-sum-exp is -inf (no score above -inf) adds nothing; one that is NaN makes the
+ * weights of the tokens it sees NaN.  Sums are fp32 in a fixed order (two calls give the same
+ * bits).
  * Errors: those of kvk_prompt_attention, KVK_ERR_BUFFER (workspace). */
 kvk_status kvk_attention_weight_workspace_bytes(int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t n_seqs,
                                                 const int32_t* seq_tokens, size_t* out_bytes);

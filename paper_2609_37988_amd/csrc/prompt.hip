@@ -344,6 +344,11 @@ constexpr int kWq = 64;     // query rows of a staged tile
 //   part[t] = sum_{i >= t} exp(scale q_i . k_t - lse_i).
 // S^T tiles with the keys as product rows: a lane adds its columns' probabilities up, and the
 // lanes of a key meet once at the end.
+// Bound: the vector units, 24 clocks per wave-wide probability (a product, an exponential of 16
+// clocks, a sum) beside 16 of the matrix unit: 40 / 8 heads over 8192 tokens 371 us, of which
+// the exponentials and sums alone take about 220.  Forming the next scores between the
+// exponentials of the last ones within a wave spilled registers (479 and 656 us); the other
+// wave of the SIMD fills some of the gaps.
 template <int D>
 __global__ __launch_bounds__(256, 2) void weight_kernel(WeightArgs a) {
   constexpr int NK = D / 16, kOct = D / 8, kPieces = kWq * kOct / 256;
@@ -368,7 +373,10 @@ __global__ __launch_bounds__(256, 2) void weight_kernel(WeightArgs a) {
       const int u = tid + 256 * i, r = min(first + u / kOct, len - 1);
       w[i] = *reinterpret_cast<const u4v*>(qb + (int64_t)r * a.sq.token + 8 * (u % kOct));
     }
-    if (tid < kWq) ls = first + tid < len ? lse[first + tid] * kLog2e : INFINITY;  // rows past the end weigh nothing
+    if (tid < kWq) {
+      ls = first + tid < len ? lse[first + tid] * kLog2e : INFINITY;
+      if (ls == -INFINITY) ls = INFINITY;  // rows past the end, and rows without mass, weigh nothing
+    }
   };
   const auto store = [&](int buf) {
 #pragma unroll
@@ -414,18 +422,20 @@ __global__ __launch_bounds__(256, 2) void weight_kernel(WeightArgs a) {
         }
         const float l2 = lse2[buf][32 * y + col];
         const int row = q0 + 32 * y + col;
-        if (q0 + 32 * y < kw + 63) {  // some row of the subtile precedes some key of the wave
-          asm volatile("");  // (a branch, not selects in every step)
+        if (q0 + 32 * y >= kw + 63) {  // every row of the subtile sees every key of the wave
 #pragma unroll
           for (int i = 0; i < 2; ++i)
 #pragma unroll
-            for (int e = 0; e < 16; ++e)
-              s[i][e] = kw + 32 * i + tile_row(e, h) <= row ? s[i][e] : -INFINITY;
+            for (int e = 0; e < 16; ++e) acc[i][e] += __builtin_amdgcn_exp2f(__builtin_fmaf(s[i][e], a.c, -l2));
+        } else {
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i][e], a.c, -l2));
+              acc[i][e] += kw + 32 * i + tile_row(e, h) <= row ? p : 0.0f;  // (p of a hidden place may be NaN)
+            }
         }
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-          for (int e = 0; e < 16; ++e) acc[i][e] += __builtin_amdgcn_exp2f(__builtin_fmaf(s[i][e], a.c, -l2));
       }
     }
     __syncthreads();

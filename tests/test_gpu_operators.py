@@ -217,6 +217,27 @@ def test_attention_weight(lens, hq, hkv, d, layout):
         at += n
 
 
+def test_attention_weight_rows_without_mass_and_nan():
+    """A row with the log-sum-exp -inf adds nothing; a NaN row spoils the tokens it sees only."""
+    lens, d = [150, 60], 64
+    q, k, v = _prompt_inputs(20, lens, 2, 1, d, "packed")
+    q[:, :, 0] = 1.0
+    k[:40, :, 0] = -math.inf  # rows 0..39 have no finite score
+    q[100, 0] = NAN           # one row of one head
+    _, lse = _run_prompt(q, k, v, lens, 0.1)
+    assert (lse[:40] == -math.inf).all() and torch.isnan(lse[100])
+    ws = torch.empty(kvk.attention_weight_workspace_bytes(2, 1, d, lens), dtype=torch.uint8, device=DEV)
+    w = torch.full((210,), 7.0, dtype=torch.float32, device=DEV)
+    kvk.attention_weight(q, k, lse, lens, 0.1, w, ws)
+    assert torch.isnan(w[:101]).all()  # tokens that row 100 sees
+    assert torch.isfinite(w[101:]).all()
+    q[100, 0] = q[99, 0]
+    _, lse = _run_prompt(q, k, v, lens, 0.1)
+    kvk.attention_weight(q, k, lse, lens, 0.1, w, ws)
+    assert (w[:40] == 0).all() and torch.isfinite(w).all()
+    assert abs(float(w[:150].sum()) / (2 * 110) - 1) < 1e-5  # 110 rows of each head carry mass
+
+
 # --------------------------------------------------------------------------------------
 # The keep list
 # --------------------------------------------------------------------------------------
