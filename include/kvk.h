@@ -470,7 +470,8 @@ kvk_status kvk_snapkv_select(const kvk_table* table, int32_t layer, const void* 
  * s * seq + h * head + t * token (seq > 0: one place per sequence, a padded batch) or, with
  * seq = 0, at h * head + (rows of the sequences before s + t) * token (packed).  A row's
  * head_dim elements are contiguous.  Strides are non-negative multiples of 8 elements; a head
- * stride of 0 reads the same row for every head. */
+ * stride of 0 reads the same row for every head.  Rows that are written must not overlap: the
+ * strides nest (in ascending order, each spans the whole extent of those before it). */
 typedef struct {
   int64_t seq, head, token;
 } kvk_strides;

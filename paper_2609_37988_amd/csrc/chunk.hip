@@ -545,7 +545,7 @@ kvk_status lay_out(ChunkLaunch& L) {
     rec += ns > 1 ? a.Hkv * R * ns : 0;
     row += a.Hkv * R;
   }
-  if (wg > 0x7fffffffLL || rec > 0x7fffffffLL || row > 0x7ffffff0LL)
+  if (wg > 0xffffffLL || rec > 0x7fffffffLL || row > 0x7ffffff0LL)  // (a grid has less than 2^32 threads)
     return fail(KVK_ERR_UNSUPPORTED, "kvk_chunk_attention: too many query rows in one call");
   L.wgs = wg;
   L.recs = rec;

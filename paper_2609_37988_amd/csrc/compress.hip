@@ -1284,7 +1284,7 @@ extern "C" kvk_status kvk_append_chunk(const kvk_table* t, int32_t l0, int32_t l
   }
   const int per_wg = d.head_dim == 128 ? 1 : 2;  // blocks of a workgroup
   const int64_t grid = ((int64_t)a.n_streams * units + per_wg - 1) / per_wg;
-  if (grid > 0x3fffffffLL) return fail(KVK_ERR_UNSUPPORTED, "%s: grid too large", what);
+  if (grid > 0x1ffffffLL) return fail(KVK_ERR_UNSUPPORTED, "%s: grid too large", what);  // (2^32 threads)
   bool checked = false;
   int n = 0;
   const auto flush = [&]() -> kvk_status {

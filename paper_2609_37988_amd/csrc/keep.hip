@@ -25,7 +25,7 @@ namespace {
 constexpr int kThreads = 1024, kWaves = kThreads / 64;
 constexpr int kBins = 2048;                    // two per thread
 constexpr int kResident = 16;                  // keys a lane of keep_kernel keeps in registers
-constexpr int kSliceKeys = 16;                  // ... of keep_slice_kernel (two workgroups share a CU)
+constexpr int kSliceKeys = 16;                 // ... of keep_slice_kernel (two workgroups share a CU)
 constexpr int kWhole = kThreads * kResident, kSlice = kThreads * kSliceKeys;
 
 struct KeepArgs {
@@ -342,7 +342,8 @@ extern "C" kvk_status kvk_keep_heaviest(const kvk_table* t, const float* weight,
     return fail(KVK_ERR_BUFFER, "%s: workspace %zu bytes < %lld needed", what, ws_bytes,
                 (long long)(z.hist + z.above + z.state));
   if (kvk_status st = check_gpu_buffers({weight, keep_out, sliced ? workspace : nullptr}, what)) return st;
-  if (streams > (sliced ? 65535 : 0x7fffffffLL)) return fail(KVK_ERR_UNSUPPORTED, "%s: grid too large", what);
+  if (streams > (sliced ? 65535 : 0x3fffff)) return  // (a grid has less than 2^32 threads)
+    fail(KVK_ERR_UNSUPPORTED, "%s: grid too large", what);
   if (!sliced) {
     hipLaunchKernelGGL(keep_kernel, dim3((unsigned)streams), dim3(kThreads), 0, stream, a);
   } else {

@@ -5,7 +5,7 @@
 
 #include <algorithm>
 #include <cmath>
-#include <vector>
+#include <utility>
 
 #include "kvk_internal.h"
 #include "tile_device.h"
@@ -15,6 +15,7 @@ using namespace kvkd;
 namespace {
 
 constexpr int kSeqs = KVK_MAX_BATCH_PLANS;
+constexpr int64_t kMostWgs = 0xffffff;  // of 256 threads: a grid has less than 2^32 threads
 constexpr float kLog2e = 1.4426950408889634f;
 
 // The sequences of a launch, longest first, cut into blocks of rows.  The blocks with r blocks
@@ -25,7 +26,6 @@ constexpr float kLog2e = 1.4426950408889634f;
 // level and sequence follow from an entry's number by one search.
 struct SeqList {
   int32_t n;                // sequences with rows
-  int32_t blocks0;          // blocks of the longest one
   int32_t len[kSeqs];
   int32_t first[kSeqs];     // rows of the sequences before it
   int32_t begin[kSeqs];     // entries of the levels above sequence j's highest
@@ -488,14 +488,29 @@ kvk_status check_seqs(const char* what, int32_t Hq, int32_t Hkv, int32_t D, int3
   return KVK_OK;
 }
 
-// Element strides of a tensor of `heads` heads: rows are read and written in 16-byte pieces.
-kvk_status check_strides(const char* what, const char* name, const kvk_strides& s, int32_t D, bool written) {
+// Element strides of a tensor: rows are read and written in 16-byte pieces.
+kvk_status check_strides(const char* what, const char* name, const kvk_strides& s) {
   if (s.seq < 0 || s.head < 0 || s.token < 0 || s.seq % 8 || s.head % 8 || s.token % 8)
     return fail(KVK_ERR_INVALID, "%s: %s strides (%lld, %lld, %lld) must be multiples of 8 elements", what, name,
                 (long long)s.seq, (long long)s.head, (long long)s.token);
-  if (written && (s.token < D || s.head < D))
-    return fail(KVK_ERR_INVALID, "%s: %s rows overlap (head stride %lld, token stride %lld)", what, name,
-                (long long)s.head, (long long)s.token);
+  return KVK_OK;
+}
+
+// Rows that are written must not overlap: of the dimensions with more than one place, in the
+// order of their strides, each steps over all of the ones before it.
+kvk_status check_apart(const char* what, const char* name, const kvk_strides& s, int32_t D, int32_t heads, int32_t n_seqs,
+                       const int32_t* seq_tokens, int64_t total) {
+  const int64_t longest = *std::max_element(seq_tokens, seq_tokens + n_seqs);
+  std::pair<int64_t, int64_t> dims[3] = {{s.token, s.seq ? longest : total}, {s.head, heads}, {s.seq, s.seq ? n_seqs : 1}};
+  std::sort(dims, dims + 3);
+  __int128 extent = D;
+  for (const auto& [stride, count] : dims) {
+    if (count < 2) continue;
+    if (stride < extent)
+      return fail(KVK_ERR_INVALID, "%s: %s rows overlap (strides %lld, %lld, %lld)", what, name, (long long)s.seq,
+                  (long long)s.head, (long long)s.token);
+    extent += (__int128)stride * (count - 1);
+  }
   return KVK_OK;
 }
 
@@ -513,7 +528,6 @@ int64_t make_list(SeqList& sl, int32_t n_seqs, const int32_t* seq_tokens, int ro
   std::sort(s, s + n, [](const Seq& x, const Seq& y) { return x.len != y.len ? x.len > y.len : x.index < y.index; });
   const auto blocks = [&](int j) { return j < n ? (s[j].len - 1) / rows + 1 : 0; };
   sl.n = n;
-  sl.blocks0 = blocks(0);
   int64_t entries = 0;
   for (int j = 0; j < n; ++j) {
     sl.len[j] = s[j].len;
@@ -551,7 +565,8 @@ extern "C" kvk_status kvk_prompt_attention(int32_t Hq, int32_t Hkv, int32_t D, i
   const kvk_strides* s = strides ? strides : packed;
   static const char* const names[4] = {"q", "k", "v", "out"};
   for (int i = 0; i < 4; ++i)
-    if (kvk_status st = check_strides(what, names[i], s[i], D, i == 3)) return st;
+    if (kvk_status st = check_strides(what, names[i], s[i])) return st;
+  if (kvk_status st = check_apart(what, "out", s[3], D, Hq, n_seqs, seq_tokens, total)) return st;
   if (misaligned(q, 16) || misaligned(k, 16) || misaligned(v, 16) || misaligned(out, 16) || misaligned(lse, 4))
     return fail(KVK_ERR_INVALID, "%s: misaligned buffer (q, k, v, out 16 B, lse 4 B)", what);
   if (kvk_status st = check_gpu_buffers({q, k, v, out, lse}, what)) return st;
@@ -569,7 +584,7 @@ extern "C" kvk_status kvk_prompt_attention(int32_t Hq, int32_t Hkv, int32_t D, i
   a.G = Hq / Hkv;
   split_scale(scale, a.qsign, a.c);
   const int64_t grid = make_list(a.sl, n_seqs, seq_tokens, kRows) * Hq;
-  if (grid > 0x7fffffffLL) return fail(KVK_ERR_UNSUPPORTED, "%s: grid too large", what);
+  if (grid > kMostWgs) return fail(KVK_ERR_UNSUPPORTED, "%s: grid too large", what);
   if (D == 128) hipLaunchKernelGGL(prompt_kernel<128>, dim3((unsigned)grid), dim3(256), 0, stream, a);
   else hipLaunchKernelGGL(prompt_kernel<64>, dim3((unsigned)grid), dim3(256), 0, stream, a);
   const hipError_t e = hipGetLastError();
@@ -602,7 +617,7 @@ extern "C" kvk_status kvk_attention_weight(int32_t Hq, int32_t Hkv, int32_t D, i
   const kvk_strides packed[2] = {{0, D, (int64_t)Hq * D}, {0, D, (int64_t)Hkv * D}};
   const kvk_strides* s = strides ? strides : packed;
   for (int i = 0; i < 2; ++i)
-    if (kvk_status st = check_strides(what, i ? "k" : "q", s[i], D, false)) return st;
+    if (kvk_status st = check_strides(what, i ? "k" : "q", s[i])) return st;
   if (misaligned(q, 16) || misaligned(k, 16) || misaligned(lse, 4) || misaligned(weight, 4) ||
       (need && misaligned(workspace, 256)))
     return fail(KVK_ERR_INVALID, "%s: misaligned buffer (q, k 16 B, lse, weight 4 B, workspace 256 B)", what);
@@ -621,7 +636,7 @@ extern "C" kvk_status kvk_attention_weight(int32_t Hq, int32_t Hkv, int32_t D, i
   a.G = Hq / Hkv;
   split_scale(scale, a.qsign, a.c);
   const int64_t grid = make_list(a.sl, n_seqs, seq_tokens, kKeys) * Hq;
-  if (grid > 0x7fffffffLL) return fail(KVK_ERR_UNSUPPORTED, "%s: grid too large", what);
+  if (grid > kMostWgs) return fail(KVK_ERR_UNSUPPORTED, "%s: grid too large", what);
   if (D == 128) hipLaunchKernelGGL(weight_kernel<128>, dim3((unsigned)grid), dim3(256), 0, stream, a);
   else hipLaunchKernelGGL(weight_kernel<64>, dim3((unsigned)grid), dim3(256), 0, stream, a);
   if (a.G > 1)

@@ -524,7 +524,7 @@ def _here(*tensors):
 
 def _lengths(n, count: int, name: str):
     """A host int32 array of `count` lengths from one number or one per sequence."""
-    vals = [n] * count if isinstance(n, int) else [int(x) for x in n]
+    vals = [int(n)] * count if hasattr(n, "__index__") and not getattr(n, "shape", ()) else [int(x) for x in n]
     if len(vals) != count:
         raise ValueError(f"{name} must hold one length per sequence ({count})")
     if vals and not (-2**31 <= min(vals) and max(vals) < 2**31):
@@ -630,9 +630,8 @@ def keep_heaviest(t: Table, weight: torch.Tensor, n_tokens: int, n_recent: int, 
     if keep_out.dtype != torch.int32 or not keep_out.is_contiguous() or keep_out.numel() != streams * d.keep_tokens:
         raise ValueError("keep_out must be contiguous int32, streams*keep_tokens")
     if workspace is None and n_tokens > KEEP_RESIDENT:
-        workspace = torch.empty(keep_workspace_bytes(t, n_tokens), dtype=torch.uint8, device=weight.device)
-        if stream is not None:
-            workspace.record_stream(stream)
+        with torch.cuda.stream(stream):  # memory of the stream that uses it
+            workspace = torch.empty(keep_workspace_bytes(t, n_tokens), dtype=torch.uint8, device=weight.device)
     _here(workspace)
     _check(load().kvk_keep_heaviest(t.handle, weight.data_ptr(), n_tokens, n_recent, keep_out.data_ptr(),
                                     None if workspace is None else workspace.data_ptr(),

@@ -277,6 +277,25 @@ def test_keep_heaviest(n, keep, recent, kind):
     assert np.array_equal(out.cpu().numpy().reshape(6, keep), _keep_ref(w, keep, recent))
 
 
+def test_keep_heaviest_on_a_stream():
+    """A long list on a side stream, whose workspace the call brings itself, and in one of exactly
+    the size asked for."""
+    n, keep, recent = 50000, 700, 32
+    dims = kvk.make_dims(kvk.GQA, 1, 2, 2, 64, batch=2, max_tokens=n, keep_tokens=keep)
+    t = kvk.layer_table(dims, kvk.make_plan([(0, 8)]))
+    w = torch.rand(2, 2, n, device=DEV)
+    want = _keep_ref(w.cpu().numpy(), keep, recent)
+    outs = [torch.full((2, 2, keep), -1, dtype=torch.int32, device=DEV) for _ in range(2)]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    kvk.keep_heaviest(t, w, n, recent, outs[0], stream=side)
+    side.synchronize()
+    ws = torch.full((kvk.keep_workspace_bytes(t, n),), 0xFF, dtype=torch.uint8, device=DEV)
+    kvk.keep_heaviest(t, w, n, recent, outs[1], ws)
+    for out in outs:
+        assert np.array_equal(out.cpu().numpy().reshape(4, keep), want)
+
+
 def test_keep_heaviest_mla():
     dims = kvk.make_dims(kvk.MLA, 1, 8, 1, 128, latent_dim=256, rope_dim=64, nope_dim=128, v_dim=128, batch=3,
                          max_tokens=500, keep_tokens=100)
@@ -489,6 +508,92 @@ def test_chunk_attention_long(bits):
     for new in ([1, 1, 1], [4, 2, 13], [200, 40, 33], [1000, 0, 5]):
         q, out = _run_chunk(c, 0, 1, stored, new, 0.09)
         _check_chunk(c, 0, 1, stored, new, 0.09, q, out)
+
+
+@pytest.mark.parametrize("scheme", SCHEMES)
+@pytest.mark.parametrize("bits", [16, 8, 4, 2])
+@pytest.mark.parametrize("d", [64, 128])
+def test_chunk_attention_splits(bits, scheme, d):
+    """Split contexts in every row shape, ten query heads to a KV head."""
+    c = Streams([(0, bits)], 20, 2, d, 2, 2900, scheme, seed=20)
+    stored = [2881, 1600]
+    c.append([0] * 2, stored)
+    for new in ([1, 2], [4, 6], [9, 33]):
+        q, out = _run_chunk(c, 0, 1, stored, new, 0.7 / math.sqrt(d))
+        _check_chunk(c, 0, 1, stored, new, 0.7 / math.sqrt(d), q, out)
+
+
+def test_chunk_many_sequences_and_layers():
+    """More sequences than one attention launch takes, more anchors than one append launch."""
+    B, L = 203, 60
+    rng = np.random.default_rng(21)
+    plan = [(0, (4, 8, 2, 16)[l % 4]) for l in range(L)]
+    c = Streams(plan, 2, 1, 64, B, 80, kvk.KIVI32, seed=21)
+    first = [int(x) for x in rng.integers(0, 41, B)]
+    new = [int(x) for x in rng.integers(0, 40, B)]
+    stored = [a + b for a, b in zip(first, new)]
+    c.append([0] * B, first)
+    c.append(first, new)
+    q, out = _run_chunk(c, 56, 58, stored, new, 0.1)
+    some = [0, 1, 95, 96, 97, 150, 191, 192, 202]
+    for b in some:
+        n, m = stored[b], new[b]
+        assert (out[:, b, :, m:] == 7.0).all()
+        for l in (56, 57) if m else ():
+            K, V, _ = c.values(l, b, 0, n)
+            o, _, tol, _ = _attend(q[l - 56, b, :, :m], K, V, 0.1, torch.arange(n - m, n, device=DEV), 2.0**-11, 2.0**-11, 2.0**-11)
+            _check(out[l - 56, b, :, :m], o, tol, f"layer {l} sequence {b}")
+
+
+def test_append_chunk_many_equal_sequences():
+    """Sequences of one length beyond the limit of ragged ones."""
+    B = 300
+    c = Streams([(0, 4)], 1, 1, 64, B, 40, kvk.KIVI32, seed=22)
+    c.append([0] * B, [33] * B)
+    one = c.new_arena()
+    for n in range(33):
+        kvk.append_token(c.t, 0, 1, c.k[:, :, :, n].contiguous(), c.v[:, :, :, n].contiguous(), n, one)
+    _same(c.streams(c.arena, [33] * B), c.streams(one, [33] * B))
+
+
+def test_chunk_few_rows_in_a_large_workspace():
+    """A call whose rows are few beside n_chunk fits the workspace asked for n_chunk; rows that
+    are not new, and a call without new rows, leave the output alone."""
+    c = Streams([(0, 8), (1, 8)], 4, 1, 128, 3, 9000, kvk.KIVI32, seed=23)
+    stored = [8999, 5000, 64]
+    c.append([0] * 3, stored)
+    m = 300
+    g = _gen(24)
+    q = _randn(g, 2, 3, 4, m, 128).bfloat16()
+    ws = torch.empty(kvk.chunk_workspace_bytes(c.t, 0, 2, m), dtype=torch.uint8, device=DEV)
+    for new in ([1, 0, 1], [3, 5, 8], [20, 1, 30], [0, 0, 0]):
+        out = torch.full(q.shape, 7.0, dtype=torch.bfloat16, device=DEV)
+        kvk.chunk_attention(c.t, 0, 2, q, stored, new, 0.09, c.arena, out, ws)
+        _check_chunk(c, 0, 2, stored, new, 0.09, q, out)
+
+
+def test_chunk_beyond_32_bits():
+    """Caches, inputs and arena offsets past 4 GiB (16-bit layers hold the bf16 inputs)."""
+    B, hkv, n, d = 16, 8, 131000, 128
+    dims = kvk.make_dims(kvk.GQA, 1, 16, hkv, d, batch=B, max_tokens=131072)
+    t = kvk.layer_table(dims, kvk.make_plan([(0, 16)]))
+    arena = torch.empty(kvk.table_query(t).arena_bytes, dtype=torch.uint8, device=DEV)
+    assert arena.numel() > 2**32
+    k, v = (torch.zeros((1, B, hkv, n, d), dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    g = _gen(25)
+    for x in (k, v):
+        x[0, -1, -1] = _randn(g, n, d).bfloat16()
+        x[0, 0, 0] = _randn(g, n, d).bfloat16()
+    kvk.append_chunk(t, 0, 1, k, v, 0, None, arena)
+    q = _randn(g, 1, B, 16, 3, d).bfloat16()
+    out = torch.empty_like(q)
+    ws = torch.empty(kvk.chunk_workspace_bytes(t, 0, 1, 3), dtype=torch.uint8, device=DEV)
+    kvk.chunk_attention(t, 0, 1, q, n, None, 0.1, arena, out, ws)
+    last = torch.arange(n - 3, n, device=DEV)
+    for b, h in ((0, 0), (B - 1, hkv - 1)):
+        o, _, tol, _ = _attend(q[0, b, 2 * h:2 * h + 2], k[0, b, h], v[0, b, h], 0.1, last, 0.0, 2.0**-8, 0.0)
+        _check(out[0, b, 2 * h:2 * h + 2], o, tol, f"sequence {b}")
+    assert (out[0, 1:-1] == 0).all()
 
 
 @pytest.mark.parametrize("scale", [-0.1, 0.0])

@@ -65,6 +65,25 @@ def test_prompt_buffers_and_strides():
     _refused(_prompt(strides=_strides((0, 0, 0), ok, ok, ok)), kvk.ERR_INVALID, "not GPU-accessible")  # inputs may repeat
 
 
+def test_prompt_rows_written_do_not_overlap():
+    """out strides of 4 heads of 64 and sequences of 5 and 3 tokens, or one head."""
+    ok = (0, 64, 256)
+
+    def out(*s, **kw):
+        return _prompt(strides=_strides(ok, ok, ok, s), **kw)
+
+    for bad in ((0, 64, 64), (0, 64, 192), (0, 504, 64), (64, 64, 512), (504, 64, 256), (1272, 320, 64), (256, 64, 256)):
+        _refused(out(*bad), kvk.ERR_INVALID, "out rows overlap")
+    # token-major, head-major, sequence-major, head above sequence, token above both
+    for fine in ((0, 64, 256), (0, 512, 64), (1280, 64, 256), (1280, 320, 64), (320, 640, 64), (64, 128, 512)):
+        _refused(out(*fine), kvk.ERR_INVALID, "not GPU-accessible")
+    _refused(out(0, 0, 64, hq=2, hkv=2), kvk.ERR_INVALID, "out rows overlap")
+    _refused(out(0, 0, 64, hq=1, hkv=1), kvk.ERR_INVALID, "not GPU-accessible")          # one head: its stride is not taken
+    _refused(out(0, 64, 0, lens=(1,)), kvk.ERR_INVALID, "not GPU-accessible")            # one token
+    _refused(out(0, 64, 0, lens=(1, 1)), kvk.ERR_INVALID, "out rows overlap")
+    _refused(out(2**62, 2**61, 64), kvk.ERR_INVALID, "out rows overlap")
+
+
 def test_weight_buffers():
     for name in ("q", "k", "lse", "weight", "ws"):
         _refused(_weight(**{name: None}), kvk.ERR_INVALID, "NULL")
