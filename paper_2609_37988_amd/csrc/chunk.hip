@@ -5,11 +5,11 @@
 // rows of an anchor's stream (sequence, KV head) are its new tokens x the layers that read it x
 // the G query heads of the KV head, in this order, so that rows of one token sit together.
 //
-// One workgroup of four waves takes 32 WR rows and a range of the context, in tiles of TB
-// 32-token blocks.  All waves dequantise a tile into LDS, once, in the operand order that the
+// One workgroup of four waves (eight for WR = 8) takes 32 WR rows and a range of the context, in
+// tiles of TB 32-token blocks.  All waves dequantise a tile into LDS, once, in the operand order that the
 // arena's layout has already (16-byte units of eight values), bf16 for 16-bit layers and fp16
 // for quantised ones; then wave (wr, wt) attends with row group wr to the tile's wt-th share of
-// the tokens.  Many rows: WR = 4, every wave reads the whole tile.  Few rows (a draft, single
+// the tokens.  Many rows: WR = 4 or 8, every wave reads the whole tile.  Few rows (a draft, single
 // tokens): WR = 1, the waves share the tokens, and their states meet in LDS at the end.  Where
 // the rows alone leave the GPU idle the context is split over workgroups too; chunk_merge_kernel
 // joins the partial results.
@@ -58,10 +58,12 @@ static_assert(sizeof(ChunkArgs) <= 4096, "kernel arguments");
 template <int WR>
 struct Shape {
   static constexpr int kRowsWg = 32 * WR;
-  static constexpr int kWt = 4 / WR;            // waves over the tokens
+  static constexpr int kWaves = WR == 8 ? 8 : 4;
+  static constexpr int kWt = kWaves / WR;       // waves over the tokens
   static constexpr int kTb = WR == 1 ? 4 : 2;
   static constexpr int kBuffers = WR == 1 ? 1 : 2;  // tiles in LDS
   static constexpr int kNt = kTb / kWt;
+  static constexpr int kOwn = 4 * kTb / kWaves;  // blocks of which a wave dequantises a part
 };
 
 __host__ __device__ inline int splits_of(int stored, int tb, int split_tiles) {
@@ -199,20 +201,21 @@ __device__ __forceinline__ constexpr int subtile_token(int e, int h) {
 }
 
 template <int D, int BITS, int QS, int WR>
-__global__ __launch_bounds__(256, 2) void chunk_kernel(ChunkArgs a) {
+__global__ __launch_bounds__(64 * Shape<WR>::kWaves, 2) void chunk_kernel(ChunkArgs a) {
   using S = Shape<WR>;
   using P = Part<D, BITS, QS>;
   constexpr bool HALF = BITS != 16;
-  constexpr int NM = D / 32, NK = D / 16, TB = S::kTb, NT = S::kNt, WT = S::kWt;
+  constexpr int NM = D / 32, NK = D / 16, TB = S::kTb, NT = S::kNt, WT = S::kWt, OWN = S::kOwn;
   constexpr int kBlk = 128 * D;  // LDS bytes of a block: keys, then values
   constexpr int kSlot = P::MBYTES > 0 ? P::MBYTES / 4 : 1;
   constexpr int kTile = S::kBuffers * TB * kBlk, kJoin = (WT - 1) * WR * 64 * NM * 64;
   __shared__ __align__(16) uint8_t img[kTile > kJoin ? kTile : kJoin];
-  __shared__ __align__(16) uint32_t slots[4][kSlot];
+  __shared__ __align__(16) uint32_t slots[S::kWaves][kSlot];
   __shared__ float2 stats[4][32];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int col = lane & 31, h = lane >> 5;
   const int wr = wave % WR, wt = wave / WR;
+  const int role = wave & 3, own0 = (wave >> 2) * OWN;  // the wave's part, of blocks own0 .. of a tile
 
   const int sj = find_seq(a.wg0, a.n_seq, blockIdx.x, lane);
   const int stored = a.stored[sj], fresh = a.fresh[sj], seq = a.index[sj];
@@ -239,13 +242,14 @@ __global__ __launch_bounds__(256, 2) void chunk_kernel(ChunkArgs a) {
   const int tile1 = min(tiles, seen_by_any / (32 * TB) + 1);                  // one past the last one seen
   const bool tail = split == nsplit - 1 && stored % 32 && 32 * nbf <= seen_by_any;
 
-  P part[TB];
+  P part[OWN];
   const auto load = [&](int tile) {
 #pragma unroll
-    for (int i = 0; i < TB; ++i) part[i].template load<(WR < 4)>(stream + (int64_t)min(tile * TB + i, nbf - 1) * a.block_bytes, wave, lane);
+    for (int i = 0; i < OWN; ++i)
+      part[i].template load<(WR < 4)>(stream + (int64_t)min(tile * TB + own0 + i, nbf - 1) * a.block_bytes, role, lane);
   };
   uint8_t* buf = img;  // the tile in work
-  const auto place = [&](int blk) { return buf + blk * kBlk + (wave < 2 ? wave * 32 * D : 64 * D + (wave - 2) * 1024 * P::UN); };
+  const auto place = [&](int blk) { return buf + blk * kBlk + (role < 2 ? role * 32 * D : 64 * D + (role - 2) * 1024 * P::UN); };
   if (tile0 < tile1) load(tile0);
 
   u4v qf[NK];
@@ -282,29 +286,36 @@ __global__ __launch_bounds__(256, 2) void chunk_kernel(ChunkArgs a) {
     const int bound = window ? stored - 1 : 32 * nbf - 1;  // the last position that holds a token of it
     if (!window) {
 #pragma unroll
-      for (int k = 0; k < TB; ++k) {
-        if (tile * TB + k < nbf) {
-          part[k].store(place(k), slots[wave], wave, lane);
-        } else if (wave >= 2) {  // past the full blocks: no value may enter a product
+      for (int k = 0; k < OWN; ++k) {
+        if (tile * TB + own0 + k < nbf) {
+          part[k].store(place(own0 + k), slots[wave], role, lane);
+        } else if (role >= 2) {  // past the full blocks: no value may enter a product
 #pragma unroll
-          for (int u = 0; u < P::UN; ++u) reinterpret_cast<u4v*>(place(k) + 16 * lane)[64 * u] = u4v{0, 0, 0, 0};
+          for (int u = 0; u < P::UN; ++u) reinterpret_cast<u4v*>(place(own0 + k) + 16 * lane)[64 * u] = u4v{0, 0, 0, 0};
         }
       }
       if (tile + 1 < tile1) load(tile + 1);
     } else {
       const uint8_t* tb = stream + (int64_t)a.nb_cap * a.block_bytes;
-      const u4v* in = reinterpret_cast<const u4v*>(tb + (wave < 2 ? wave * 32 * D : 64 * D + (wave - 2) * 1024 * P::UN)) + lane;
+      const u4v* in = reinterpret_cast<const u4v*>(tb + (role < 2 ? role * 32 * D : 64 * D + (role - 2) * 1024 * P::UN)) + lane;
 #pragma unroll
-      for (int u = 0; u < P::UN; ++u) {
-        u4v x = in[64 * u];
-        if (wave >= 2) {  // slots past the tokens hold anything
+      for (int k = 0; k < OWN; ++k) {
+        u4v* to = reinterpret_cast<u4v*>(place(own0 + k) + 16 * lane);
+        if (own0 + k == 0) {
 #pragma unroll
-          for (int n = 0; n < 8; ++n)
-            if (16 * (n >> 2) + 4 * (lane >> 4) + (n & 3) >= stored % 32) x[n >> 1] &= n & 1 ? 0x0000ffffu : 0xffff0000u;
+          for (int u = 0; u < P::UN; ++u) {
+            u4v x = in[64 * u];
+            if (role >= 2) {  // slots past the tokens hold anything
 #pragma unroll
-          for (int k = 1; k < TB; ++k) reinterpret_cast<u4v*>(place(k) + 16 * lane)[64 * u] = u4v{0, 0, 0, 0};
+              for (int n = 0; n < 8; ++n)
+                if (16 * (n >> 2) + 4 * (lane >> 4) + (n & 3) >= stored % 32) x[n >> 1] &= n & 1 ? 0x0000ffffu : 0xffff0000u;
+            }
+            to[64 * u] = HALF ? bf16_to_half_unit(x) : x;
+          }
+        } else if (role >= 2) {
+#pragma unroll
+          for (int u = 0; u < P::UN; ++u) to[64 * u] = u4v{0, 0, 0, 0};
         }
-        reinterpret_cast<u4v*>(place(0) + 16 * lane)[64 * u] = HALF ? bf16_to_half_unit(x) : x;
       }
     }
     // A tile that some row does not see wholly: masked scores, and a look for infinities and NaN
@@ -314,8 +325,8 @@ __global__ __launch_bounds__(256, 2) void chunk_kernel(ChunkArgs a) {
     const int last = min(limit, bound) - p0 - 32 * b0;  // the last token of them that the row sees
     if (masked) {
       bool bad = false;
-      if (wave >= 2) {
-        for (int k = 0; k < TB; ++k) {
+      if (role >= 2) {
+        for (int k = own0; k < own0 + OWN; ++k) {
           const u4v* u = reinterpret_cast<const u4v*>(place(k) + 16 * lane);
           for (int y = 0; y < P::UN; ++y) bad |= any_nonfinite<HALF>(u[64 * y]);
         }
@@ -325,8 +336,8 @@ __global__ __launch_bounds__(256, 2) void chunk_kernel(ChunkArgs a) {
         take_nonfinite<NM, NT, HALF>(st, [&](int k, int x, int m) { return value_unit(b0 + k, x, m); },
                                      [&](int k, int e) { return (uint32_t)((last - 32 * k - subtile_token(e, h)) >> 31); });
         __syncthreads();
-        if (wave >= 2) {
-          for (int k = 0; k < TB; ++k) {
+        if (role >= 2) {
+          for (int k = own0; k < own0 + OWN; ++k) {
             u4v* u = reinterpret_cast<u4v*>(place(k) + 16 * lane);
             for (int y = 0; y < P::UN; ++y) u[64 * y] = only_finite<HALF>(u[64 * y]);
           }
@@ -487,27 +498,37 @@ namespace {
 
 // Workgroups that a launch's splits aim at: four per CU, so that the last ones to end leave
 // little idle, or the two that a CU holds at once where four would be short (a split pays its
-// start, and a record per row written and read).  4-bit, 64 streams of 8192 tokens, one new
-// token: two per CU 37 us, four 42; 8-bit, 256 streams, four new tokens: 131 and 122.
+// start, and a record per row written and read), or two of those of eight waves.  4-bit, 64
+// streams of 8192 tokens, one new token: two per CU 37 us, four 42; 8-bit, 256 streams, four new
+// tokens: 131 and 122.
 constexpr int64_t kAimWgs = 1024;
 constexpr int kLongSplit = 16;  // tiles
 constexpr int kMinTiles = 2;
 
-int waves_over_rows(int64_t rows) { return rows <= 32 ? 1 : (rows <= 64 ? 2 : 4); }
+// Eight waves halve the dequantisation per row but leave a CU one workgroup, whose barriers
+// nothing covers, and wide row blocks part empty.  4-bit, one sequence of 8192 tokens, query rows
+// per KV head and times with four and eight waves: 1280 76 and 89 us, 2560 131 and 125, 5120
+// 225 and 206; 12345 tokens, 10240 rows 594 and 545.
+constexpr int64_t kManyRows = 2048;
+
+int waves_over_rows(int64_t rows) { return rows <= 32 ? 1 : (rows <= 64 ? 2 : (rows < kManyRows ? 4 : 8)); }
+int64_t aim_of(int wr, int64_t work) { return wr < 8 && work / kAimWgs >= kLongSplit ? kAimWgs : kAimWgs / 2; }
 int blocks_of_tile(int wr) { return wr == 1 ? 4 : 2; }
 
 // Split records of a launch at most, for up to rows_of_stream rows in each of up to `streams`
-// streams.  The splits of all row blocks are at most kAimWgs and one more for each block, and a
-// launch with kAimWgs row blocks does not split; a row has at most the splits of a full stream.
+// streams.  The splits of all row blocks are at most the number aimed at and one more for each
+// block, and a launch with that many row blocks does not split; a row has at most the splits
+// of a full stream.
 int64_t most_records(const kvk_table* t, int64_t rows_of_stream, int64_t streams) {
   int64_t most = 0;
   for (int w = waves_over_rows(rows_of_stream); w >= 1; w /= 2) {  // (fewer new tokens take narrower blocks)
-    const int64_t rows = w < 4 ? std::min<int64_t>(rows_of_stream, 32 * w) : rows_of_stream;
+    const int64_t rows = std::min<int64_t>(rows_of_stream, w < 4 ? 32 * w : (w == 4 ? kManyRows - 1 : rows_of_stream));
+    const int64_t aim = w < 8 ? kAimWgs : kAimWgs / 2;  // (at most)
     const int64_t blocks = streams * ((rows + 32 * w - 1) / (32 * w));
     const int64_t tiles = (t->nb_cap + blocks_of_tile(w) - 1) / blocks_of_tile(w);
     const int64_t splits = (tiles + kMinTiles - 1) / kMinTiles;
     if (splits > 1)
-      most = std::max(most, std::min((kAimWgs + std::min(blocks, kAimWgs)) * 32 * w, streams * rows * splits));
+      most = std::max(most, std::min((aim + std::min(blocks, aim)) * 32 * w, streams * rows * splits));
   }
   return most;
 }
@@ -531,7 +552,7 @@ kvk_status lay_out(ChunkLaunch& L) {
     wgs += n;
     work += n * ((a.stored[j] / 32 + tb - 1) / tb);
   }
-  const int64_t aim = work / kAimWgs >= kLongSplit ? kAimWgs : kAimWgs / 2;
+  const int64_t aim = aim_of(L.wr, work);
   a.split_tiles = wgs >= aim ? 0x7fffffff : (int32_t)std::max<int64_t>(kMinTiles, (work + aim - 1) / aim);
   int64_t wg = 0, rec = 0, row = 0;
   for (int j = 0; j < a.n_seq; ++j) {
@@ -558,7 +579,8 @@ void launch_rows(const ChunkLaunch& L, hipStream_t st) {
   const dim3 g((unsigned)L.wgs), b(256);
   if (L.wr == 1) hipLaunchKernelGGL((chunk_kernel<D, BITS, QS, 1>), g, b, 0, st, L.a);
   else if (L.wr == 2) hipLaunchKernelGGL((chunk_kernel<D, BITS, QS, 2>), g, b, 0, st, L.a);
-  else hipLaunchKernelGGL((chunk_kernel<D, BITS, QS, 4>), g, b, 0, st, L.a);
+  else if (L.wr == 4) hipLaunchKernelGGL((chunk_kernel<D, BITS, QS, 4>), g, b, 0, st, L.a);
+  else hipLaunchKernelGGL((chunk_kernel<D, BITS, QS, 8>), g, dim3(512), 0, st, L.a);
 }
 template <int D, int QS>
 void launch_bits(const ChunkLaunch& L, hipStream_t st) {

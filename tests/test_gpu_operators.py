@@ -639,6 +639,38 @@ def test_chunk_attention_hides_later_infinities():
         assert torch.isnan(out[:, 38:]).all()
 
 
+@pytest.mark.parametrize("scheme", SCHEMES)
+@pytest.mark.parametrize("bits", [16, 8, 4, 2])
+@pytest.mark.parametrize("d", [64, 128])
+def test_chunk_attention_wide(bits, scheme, d):
+    """Many rows (sixty-four query heads to a KV head), the widest workgroups."""
+    c = Streams([(0, bits)], 64, 1, d, 3, 400, scheme, seed=26)
+    stored = [390, 33, 96]
+    c.append([0] * 3, stored)
+    new = [41, 33, 7]
+    q, out = _run_chunk(c, 0, 1, stored, new, 0.9 / math.sqrt(d))
+    _check_chunk(c, 0, 1, stored, new, 0.9 / math.sqrt(d), q, out)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_chunk_attention_wide_hides_later_infinities(d):
+    """As above in the widest workgroups: in full blocks, in the window, and past its tokens."""
+    hq, n, m = 64, 170, 40
+    c = Streams([(0, 16)], hq, 1, d, 1, 200, kvk.KIVI32, seed=27)
+    c.append([0], [n])
+    q, ref = _run_chunk(c, 0, 1, [n], [m], 0.1)
+    c.v[0, 0, 0, 150, 3], c.v[0, 0, 0, 165, 4] = math.inf, NAN
+    c.v[0, 0, 0, n:] = NAN
+    c.append([0], [192])  # (the slots past token 170 of the window hold NaN, then block 5 is full)
+    c.append([0], [n])
+    _, out = _run_chunk(c, 0, 1, [n], [m], 0.1, q=q)
+    out, ref = out[0, 0], ref[0, 0]  # row i is token 130 + i
+    keep = [x for x in range(d) if x not in (3, 4)]
+    assert torch.equal(out[:, :, keep], ref[:, :, keep])
+    assert torch.equal(out[:, :20, 3], ref[:, :20, 3]) and (out[:, 20:, 3] == math.inf).all()
+    assert torch.equal(out[:, :35, 4], ref[:, :35, 4]) and torch.isnan(out[:, 35:, 4]).all()
+
+
 def test_chunk_attention_one_token_matches_decode():
     """With one new token the chunk attention is the decode step."""
     c = Streams([(0, 4), (1, 4), (0, 16)], 10, 2, 128, 2, 400, kvk.KIVI32, seed=17)
