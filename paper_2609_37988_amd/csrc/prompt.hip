@@ -15,7 +15,7 @@ using namespace kvkd;
 namespace {
 
 constexpr int kSeqs = KVK_MAX_BATCH_PLANS;
-constexpr int64_t kMostWgs = 0xffffff;  // of 256 threads: a grid has less than 2^32 threads
+constexpr int64_t kMostWgs = 0xffffff;  // workgroups of 256 threads: a grid has less than 2^32 threads
 constexpr float kLog2e = 1.4426950408889634f;
 
 // The sequences of a launch, longest first, cut into blocks of rows.  The blocks with r blocks
@@ -337,21 +337,22 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(PromptArgs a) {
 // The weight each position collects over the queries
 // ---------------------------------------------------------------------------
 
-constexpr int kKeys = 256;  // keys of a workgroup: 64 per wave, in registers
-constexpr int kWq = 64;     // query rows of a staged tile
+constexpr int kKeys = 256;  // keys of a workgroup of eight waves: 32 per wave, in registers
+constexpr int kWq = 128;    // query rows of a staged tile
 
 // One workgroup: 256 keys against the later query rows of one query head,
 //   part[t] = sum_{i >= t} exp(scale q_i . k_t - lse_i).
 // S^T tiles with the keys as product rows: a lane adds its columns' probabilities up, and the
 // lanes of a key meet once at the end.
 // Bound: the vector units, 24 clocks per wave-wide probability (a product, an exponential of 16
-// clocks, a sum) beside 16 of the matrix unit: 40 / 8 heads over 8192 tokens 371 us, of which
-// the exponentials and sums alone take about 220.  Forming the next scores between the
-// exponentials of the last ones within a wave spilled registers (479 and 656 us); the other
-// wave of the SIMD fills some of the gaps.
+// clocks, a sum) beside 16 of the matrix unit: 40 / 8 heads over 8192 tokens 350 us, of which
+// the exponentials and sums alone take about 220.  Four waves share a SIMD, so that one's
+// products run beside another's exponentials (64 keys per wave and two waves, half the query
+// reads: 371).  Forming the next scores between the exponentials of the last ones within a wave
+// spilled registers (479 and 656), priorities of the waves changed nothing.
 template <int D>
-__global__ __launch_bounds__(256, 2) void weight_kernel(WeightArgs a) {
-  constexpr int NK = D / 16, kOct = D / 8, kPieces = kWq * kOct / 256;
+__global__ __launch_bounds__(512, 4) void weight_kernel(WeightArgs a) {
+  constexpr int NK = D / 16, kOct = D / 8, kPieces = kWq * kOct / 512;
   __shared__ __align__(16) uint8_t qimg[2][kWq * kPitchK<D>];
   __shared__ float lse2[2][kWq];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -361,7 +362,7 @@ __global__ __launch_bounds__(256, 2) void weight_kernel(WeightArgs a) {
   const Entry en = find_entry<kKeys>(a.sl, blockIdx.x / a.Hq, lane);
   const int len = a.sl.len[en.j];
   const int k0 = ((len + kKeys - 1) / kKeys - en.r) * kKeys;  // the block's first key
-  const int kw = k0 + 64 * wave;                              // the wave's
+  const int kw = k0 + 32 * wave;                              // the wave's
   const uint16_t* qb = a.q + row_base(a.sq, a.sl, en.j, head);
   const float* lse = a.lse + (int64_t)a.sl.first[en.j] * a.Hq + (int64_t)head * len;
 
@@ -370,7 +371,7 @@ __global__ __launch_bounds__(256, 2) void weight_kernel(WeightArgs a) {
   const auto load = [&](int first) {
 #pragma unroll
     for (int i = 0; i < kPieces; ++i) {
-      const int u = tid + 256 * i, r = min(first + u / kOct, len - 1);
+      const int u = tid + 512 * i, r = min(first + u / kOct, len - 1);
       w[i] = *reinterpret_cast<const u4v*>(qb + (int64_t)r * a.sq.token + 8 * (u % kOct));
     }
     if (tid < kWq) {
@@ -381,28 +382,27 @@ __global__ __launch_bounds__(256, 2) void weight_kernel(WeightArgs a) {
   const auto store = [&](int buf) {
 #pragma unroll
     for (int i = 0; i < kPieces; ++i) {
-      const int u = tid + 256 * i;
+      const int u = tid + 512 * i;
       *reinterpret_cast<u4v*>(qimg[buf] + (u / kOct) * kPitchK<D> + 16 * (u % kOct)) = w[i];
     }
     if (tid < kWq) lse2[buf][tid] = ls;
   };
 
   load(k0);
-  u4v kf[2][NK];
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const int r = min(kw + 32 * i + col, len - 1);
+  u4v kf[NK];
+  {
+    const int r = min(kw + col, len - 1);
     const uint16_t* kp = a.k + row_base(a.sk, a.sl, en.j, kvh) + (int64_t)r * a.sk.token + 8 * h;
 #pragma unroll
     for (int j = 0; j < NK; ++j) {
-      kf[i][j] = *reinterpret_cast<const u4v*>(kp + 16 * j);
+      kf[j] = *reinterpret_cast<const u4v*>(kp + 16 * j);
       if (a.qsign <= 0) {
 #pragma unroll
-        for (int x = 0; x < 4; ++x) kf[i][j][x] = a.qsign < 0 ? kf[i][j][x] ^ 0x80008000u : 0u;
+        for (int x = 0; x < 4; ++x) kf[j][x] = a.qsign < 0 ? kf[j][x] ^ 0x80008000u : 0u;
       }
     }
   }
-  f16v acc[2] = {zero16(), zero16()};
+  f16v acc = zero16();
   store(0);
   if (k0 + kWq < len) load(k0 + kWq);
   __syncthreads();
@@ -411,30 +411,22 @@ __global__ __launch_bounds__(256, 2) void weight_kernel(WeightArgs a) {
     if (q0 + 2 * kWq < len) load(q0 + 2 * kWq);
     if (q0 + kWq > kw && kw < len) {
 #pragma unroll
-      for (int y = 0; y < 2; ++y) {
+      for (int y = 0; y < kWq / 32; ++y) {
         const uint8_t* qp = qimg[buf] + (32 * y + col) * kPitchK<D> + 16 * h;
-        f16v s[2] = {zero16(), zero16()};
+        f16v s = zero16();
 #pragma unroll
-        for (int j = 0; j < NK; ++j) {
-          const u4v qf = *reinterpret_cast<const u4v*>(qp + 32 * j);
-          s[0] = mfma32<false>(kf[0][j], qf, s[0]);
-          s[1] = mfma32<false>(kf[1][j], qf, s[1]);
-        }
+        for (int j = 0; j < NK; ++j) s = mfma32<false>(kf[j], *reinterpret_cast<const u4v*>(qp + 32 * j), s);
         const float l2 = lse2[buf][32 * y + col];
         const int row = q0 + 32 * y + col;
-        if (q0 + 32 * y >= kw + 63) {  // every row of the subtile sees every key of the wave
+        if (q0 + 32 * y >= kw + 31) {  // every row of the subtile sees every key of the wave
 #pragma unroll
-          for (int i = 0; i < 2; ++i)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) acc[i][e] += __builtin_amdgcn_exp2f(__builtin_fmaf(s[i][e], a.c, -l2));
+          for (int e = 0; e < 16; ++e) acc[e] += __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], a.c, -l2));
         } else {
 #pragma unroll
-          for (int i = 0; i < 2; ++i)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-              const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i][e], a.c, -l2));
-              acc[i][e] += kw + 32 * i + tile_row(e, h) <= row ? p : 0.0f;  // (p of a hidden place may be NaN)
-            }
+          for (int e = 0; e < 16; ++e) {
+            const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], a.c, -l2));
+            acc[e] += kw + tile_row(e, h) <= row ? p : 0.0f;  // (p of a hidden place may be NaN)
+          }
         }
       }
     }
@@ -442,15 +434,13 @@ __global__ __launch_bounds__(256, 2) void weight_kernel(WeightArgs a) {
   }
   float* out = (a.G > 1 ? a.part : a.weight) + (int64_t)a.sl.first[en.j] * a.Hq + (int64_t)head * len;
 #pragma unroll
-  for (int i = 0; i < 2; ++i)
-#pragma unroll
-    for (int e = 0; e < 16; ++e) {  // over the 32 columns
-      float x = sum16(acc[i][e]);
-      const auto y = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-      x = __uint_as_float(y[0]) + __uint_as_float(y[1]);
-      const int t = kw + 32 * i + tile_row(e, h);
-      if (col == 0 && t < len) out[t] = x;
-    }
+  for (int e = 0; e < 16; ++e) {  // over the 32 columns
+    float x = sum16(acc[e]);
+    const auto y = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = __uint_as_float(y[0]) + __uint_as_float(y[1]);
+    const int t = kw + tile_row(e, h);
+    if (col == 0 && t < len) out[t] = x;
+  }
 }
 
 // weight[h][t] = the sum over the query heads of KV head h, in order.
@@ -636,9 +626,9 @@ extern "C" kvk_status kvk_attention_weight(int32_t Hq, int32_t Hkv, int32_t D, i
   a.G = Hq / Hkv;
   split_scale(scale, a.qsign, a.c);
   const int64_t grid = make_list(a.sl, n_seqs, seq_tokens, kKeys) * Hq;
-  if (grid > kMostWgs) return fail(KVK_ERR_UNSUPPORTED, "%s: grid too large", what);
-  if (D == 128) hipLaunchKernelGGL(weight_kernel<128>, dim3((unsigned)grid), dim3(256), 0, stream, a);
-  else hipLaunchKernelGGL(weight_kernel<64>, dim3((unsigned)grid), dim3(256), 0, stream, a);
+  if (grid > kMostWgs / 2) return fail(KVK_ERR_UNSUPPORTED, "%s: grid too large", what);
+  if (D == 128) hipLaunchKernelGGL(weight_kernel<128>, dim3((unsigned)grid), dim3(512), 0, stream, a);
+  else hipLaunchKernelGGL(weight_kernel<64>, dim3((unsigned)grid), dim3(512), 0, stream, a);
   if (a.G > 1)
     hipLaunchKernelGGL(weight_sum_kernel, dim3((unsigned)((a.sl.len[0] + 255) / 256), (unsigned)Hkv, (unsigned)a.sl.n),
                        dim3(256), 0, stream, a);
