@@ -5,17 +5,26 @@
 // rows of an anchor's stream (sequence, KV head) are its new tokens x the layers that read it x
 // the G query heads of the KV head, in this order, so that rows of one token sit together.
 //
-// One workgroup of four waves (eight for WR = 8) takes 32 WR rows and a range of the context, in
-// tiles of TB 32-token blocks.  All waves dequantise a tile into LDS, once, in the operand order that the
-// arena's layout has already (16-byte units of eight values), bf16 for 16-bit layers and fp16
-// for quantised ones; then wave (wr, wt) attends with row group wr to the tile's wt-th share of
+// One workgroup of four waves (eight for WR = 8) takes 32 WR rows and a range of the context,
+// in tiles of TB 32-token blocks.  All waves dequantise a tile into LDS, once, in the operand
+// order that the arena's layout has already (16-byte units of eight values), bf16 for 16-bit
+// layers and fp16 for quantised ones; then wave (wr, wt) attends with row group wr to the tile's wt-th share of
 // the tokens.  Many rows: WR = 4 or 8, every wave reads the whole tile.  Few rows (a draft, single
 // tokens): WR = 1, the waves share the tokens, and their states meet in LDS at the end.  Where
 // the rows alone leave the GPU idle the context is split over workgroups too; chunk_merge_kernel
 // joins the partial results.
 //
-// Precision: fp16 holds a dequantised value to 2^-12 relative, the queries (bf16) exactly, and
-// the probabilities, kept between 2^-24 and 2^15, to 2^-12; scores, sums and outputs are fp32.
+// Precision: fp16 holds a dequantised value to 2^-11 relative (bf16 would to 2^-8), the queries
+// (bf16) exactly, and the probabilities, kept between 2^-24 and 2^15, to 2^-11; scores, sums and
+// partial outputs are fp32, the outputs are rounded once, to bf16.
+//
+// Bound.  Few rows: the latency of a tile after another (8 ragged sequences up to 7000 tokens,
+// one new token each, int4, 32 streams: 17 us for up to ten tiles, merge 7).  A draft of 40 rows per
+// stream: the caches' bytes and the dequantisation (256 streams of 8192 tokens, int8: 142 us
+// for 604 MB; the loads alone take 100 to 110; two tiles in flight, three workgroups per CU or
+// tiles of four blocks for two row groups were slower, by spills).  Many rows: as
+// prompt_kernel, power and issue, with the dequantisation on top (2048 new of 12345 tokens, 40 /
+// 8 heads, int4: 565 us with its merge, 840 TFLOP/s).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -435,8 +444,8 @@ __global__ __launch_bounds__(64 * Shape<WR>::kWaves, 2) void chunk_kernel(ChunkA
 }
 
 // The splits of every row joined, half a wave per row, D / 32 channels a lane, eight records at a
-// time with a running maximum.  Bound: latency where rows are few (256 rows of up to six splits 7 us, most of it the launch),
-// else the records' bytes (81920 rows of two: 86 MB, 36 us).
+// time with a running maximum.  Bound: latency where rows are few (224 rows of up to 28 splits
+// 7 us, most of it the launch), else the records' bytes (81920 rows of two: 86 MB, 36 us).
 template <int D>
 __global__ __launch_bounds__(256) void chunk_merge_kernel(ChunkArgs a, int tb) {
   constexpr int V = D / 32;

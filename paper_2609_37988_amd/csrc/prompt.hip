@@ -168,6 +168,10 @@ struct Stage {
 // after M(2 t - 1): the barrier after M(2 t - 2) lies behind the last reads of t - 1, the one
 // after M(2 t) before the first ones of t + 1.
 //
+// Precision: scores, statistics and output sums are fp32; the probabilities enter the second
+// product in bf16 (2^-8 relative each, of either sign), the type of the values, and the
+// outputs are rounded to bf16 once.
+//
 // Bound: power, then issue.  With both matrix and vector units busy the clock falls to about 1.9
 // GHz; 40 / 8 heads of 128 over 8192 tokens take 730 us (940 TFLOP/s; an 8192-wide bf16 library
 // product reaches 1400 to 1550).  Of a step's 2100 clocks per wave (two waves share a SIMD) the
