@@ -19,7 +19,7 @@
 // partial outputs are fp32, the outputs are rounded once, to bf16.
 //
 // Bound.  Few rows: the latency of a tile after another (8 ragged sequences up to 7000 tokens,
-// one new token each, int4, 32 streams: 17 us for up to ten tiles, merge 7).  A draft of 40 rows per
+// one new token each, int4, 32 streams: 17 us for two tiles each, merge 7).  A draft of 40 rows per
 // stream: the caches' bytes and the dequantisation (256 streams of 8192 tokens, int8: 142 us
 // for 604 MB; the loads alone take 100 to 110; two tiles in flight, three workgroups per CU or
 // tiles of four blocks for two row groups were slower, by spills).  Many rows: as
@@ -29,6 +29,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "kvk_internal.h"
 #include "tile_device.h"
@@ -444,8 +445,9 @@ __global__ __launch_bounds__(64 * Shape<WR>::kWaves, 2) void chunk_kernel(ChunkA
 }
 
 // The splits of every row joined, half a wave per row, D / 32 channels a lane, eight records at a
-// time with a running maximum.  Bound: latency where rows are few (224 rows of up to 28 splits
-// 7 us, most of it the launch), else the records' bytes (81920 rows of two: 86 MB, 36 us).
+// time (two, where no more are left: a record read twice costs like another) with a running
+// maximum.  Bound: latency where rows are few (224 rows of up to 28 splits 7 us, most of it the
+// launch), else the records' bytes (81920 rows of two: 86 MB, 30 us).
 template <int D>
 __global__ __launch_bounds__(256) void chunk_merge_kernel(ChunkArgs a, int tb) {
   constexpr int V = D / 32;
@@ -466,12 +468,12 @@ __global__ __launch_bounds__(256) void chunk_merge_kernel(ChunkArgs a, int tb) {
   fv o;
 #pragma unroll
   for (int k = 0; k < V; ++k) o[k] = 0.0f;
-  for (int i0 = 0; i0 < n; i0 += 8) {
-    fv v[8];
-    float2 ml[8];
+  const auto take = [&]<int N>(std::integral_constant<int, N>, int i0) {  // records i0 .. i0 + N - 1
+    fv v[N];
+    float2 ml[N];
     float m = M;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < N; ++i) {
       const float* p = rec + min(i0 + i, n - 1) * step;
       v[i] = *reinterpret_cast<const fv*>(p + V * l32);
       ml[i] = *reinterpret_cast<const float2*>(p + D);
@@ -482,14 +484,17 @@ __global__ __launch_bounds__(256) void chunk_merge_kernel(ChunkArgs a, int tb) {
     l *= f;
     o *= f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < N; ++i) {
       if (i0 + i < n) {
         const float w = ml[i].x == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(ml[i].x - M);  // (no mass, or NaN)
         l += ml[i].y * w;
         o += v[i] * w;
       }
     }
-  }
+  };
+  int i0 = 0;
+  for (; n - i0 > 2; i0 += 8) take(std::integral_constant<int, 8>(), i0);
+  if (i0 < n) take(std::integral_constant<int, 2>(), i0);
   if (!live) return;
   const float inv = 1.0f / l;
   const int tok = row / a.geff, rl = (row - tok * a.geff) / a.G, g = row - tok * a.geff - rl * a.G;
