@@ -505,7 +505,8 @@ kvk_status kvk_prompt_attention(int32_t n_q_heads, int32_t n_kv_heads, int32_t h
  *   lse       : device fp32, as kvk_prompt_attention returns it (same scale).
  *   weight    : device fp32, per sequence [Hkv][tokens], one sequence after another.
  *   workspace : device, >= kvk_attention_weight_workspace_bytes(...), 256-byte aligned (NULL
- *               where that is 0: one query head per KV head).
+ *               where that is 0: one query head per KV head); its contents on entry are
+ *               ignored.  Calls that overlap on one workspace race.
  * A row whose log-sum-exp is -inf (no score above -inf) adds nothing; one that is NaN makes the
  * weights of the tokens it sees NaN.  Sums are fp32 in a fixed order (two calls give the same
  * bits).
@@ -528,7 +529,8 @@ kvk_status kvk_attention_weight(int32_t n_q_heads, int32_t n_kv_heads, int32_t h
  *   n_recent : 0 .. keep_tokens.
  *   keep_out : device int32 [streams][keep_tokens].
  *   workspace: device, >= kvk_keep_workspace_bytes(table, n_tokens), 256-byte aligned; NULL
- *              where that is 0 (up to 16384 tokens).
+ *              where that is 0 (up to 16384 tokens).  Its contents on entry are ignored; calls
+ *              that overlap on one workspace race.
  * Errors: KVK_ERR_INVALID (table without eviction, sizes, NULL pointers, misalignment, host
  *         memory), KVK_ERR_BUFFER (workspace), KVK_ERR_UNSUPPORTED (more than 65535 streams of
  *         over 16384 tokens), KVK_ERR_DEVICE. */

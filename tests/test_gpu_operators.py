@@ -574,11 +574,11 @@ def test_chunk_few_rows_in_a_large_workspace():
 
 def test_chunk_beyond_32_bits():
     """Caches, inputs and arena offsets past 4 GiB (16-bit layers hold the bf16 inputs)."""
-    B, hkv, n, d = 16, 8, 131000, 128
+    B, hkv, n, d = 17, 8, 131000, 128
     dims = kvk.make_dims(kvk.GQA, 1, 16, hkv, d, batch=B, max_tokens=131072)
     t = kvk.layer_table(dims, kvk.make_plan([(0, 16)]))
     arena = torch.empty(kvk.table_query(t).arena_bytes, dtype=torch.uint8, device=DEV)
-    assert arena.numel() > 2**32
+    assert arena.numel() > 2**32 and B * hkv * n * d > 2**31
     k, v = (torch.zeros((1, B, hkv, n, d), dtype=torch.bfloat16, device=DEV) for _ in range(2))
     g = _gen(25)
     for x in (k, v):
