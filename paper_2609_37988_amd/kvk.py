@@ -547,6 +547,8 @@ def _row_strides(x: torch.Tensor, name: str, rank: int, width: int, total: int, 
     b, h, n, d = shape
     if b != count or n < longest:
         raise ValueError(f"{name} must hold every sequence's tokens")
+    if b > 1 and st[0] == 0:  # (the library reads a sequence stride of 0 as packed rows)
+        raise ValueError(f"{name} must have a place per sequence: copy a broadcast batch")
     return st[0] if b > 1 else h * n * d, st[1] if h > 1 else n * d, st[2] if n > 1 else d
 
 

@@ -204,6 +204,18 @@ def test_chunk_workspace():
     _refused(call(_table(kvk.MLA).handle, 0, 1, 1, ctypes.byref(out)), kvk.ERR_UNSUPPORTED)
 
 
+def test_binding_refuses_a_broadcast_batch():
+    """A padded batch whose sequences share one place (stride 0) has no packed meaning."""
+    q, k = torch.zeros(2, 4, 8, 64, dtype=torch.bfloat16), torch.zeros(1, 2, 8, 64, dtype=torch.bfloat16)
+    kv, lse = torch.zeros(2, 2, 8, 64, dtype=torch.bfloat16), torch.zeros(64)
+    shared = k.expand(2, 2, 8, 64)
+    for args in ((q, shared, kv, q), (q, kv, shared, q), (q, kv, kv, q[:1].expand(2, 4, 8, 64)), (q[:1].expand(2, 4, 8, 64), kv, kv, q)):
+        with pytest.raises(ValueError, match="broadcast"):
+            kvk.prompt_attention(*args[:3], [8, 8], 0.1, args[3])
+    with pytest.raises(ValueError, match="broadcast"):
+        kvk.attention_weight(q, shared, lse, [8, 8], 0.1, torch.zeros(32))
+
+
 def test_binding_refuses():
     """Tensors of the wrong type, layout or size, and tensors on the host."""
     x = torch.zeros(8, 4, 64, dtype=torch.bfloat16)
