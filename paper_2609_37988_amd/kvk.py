@@ -8,6 +8,7 @@ with an error (there is no fallback path).
 """
 import ctypes
 import os
+from array import array
 from dataclasses import dataclass
 from typing import List, Optional, Sequence
 
@@ -522,14 +523,20 @@ def _here(*tensors):
             raise ValueError("buffers must be GPU tensors on the current device")
 
 
-def _lengths(n, count: int, name: str):
-    """A host int32 array of `count` lengths from one number or one per sequence."""
+def _lengths(n, count: int, name: str) -> array:
+    """A host int32 array of `count` lengths from one number or one per sequence.  (A plain
+    array, whose address the calls take: ctypes' arrays cost a fifth of a call's host time.)"""
     vals = [int(n)] * count if hasattr(n, "__index__") and not getattr(n, "shape", ()) else [int(x) for x in n]
     if len(vals) != count:
         raise ValueError(f"{name} must hold one length per sequence ({count})")
-    if vals and not (-2**31 <= min(vals) and max(vals) < 2**31):
-        raise ValueError(f"{name} beyond 32 bits")
-    return (ctypes.c_int32 * count)(*vals)
+    try:
+        return array("i", vals)
+    except OverflowError:
+        raise ValueError(f"{name} beyond 32 bits") from None
+
+
+def _address(a: Optional[array]):
+    return None if a is None else a.buffer_info()[0]
 
 
 def _row_strides(x: torch.Tensor, name: str, rank: int, width: int, total: int, count: int, longest: int):
@@ -556,14 +563,13 @@ def _prompt_args(q: torch.Tensor, others, seq_tokens: Sequence[int]):
     """The sequences' count, total and C array of lengths, and the C array of strides."""
     lens = [int(n) for n in seq_tokens]
     total, count, longest, rank = sum(lens), len(lens), max(lens, default=0), q.dim()
-    if rank not in (3, 4) or min(lens, default=0) < 0:
-        raise ValueError("q must be [tokens, heads, d] or [B, heads, n, d], and sequence lengths not negative")
+    if rank not in (3, 4) or min(lens, default=0) < 0 or longest >= 2**31:
+        raise ValueError("q must be [tokens, heads, d] or [B, heads, n, d], and sequence lengths 0 to 2^31 - 1")
     width = q.shape[-1]
     flat = [*_row_strides(q, "q", rank, width, total, count, longest)]
     for name, x in others:
         flat += _row_strides(x, name, rank, width, total, count, longest)
-    # kvk_strides entries are three 64-bit numbers each
-    return count, total, _lengths(lens, count, "seq_tokens"), (ctypes.c_int64 * len(flat))(*flat)
+    return count, total, array("i", lens), array("q", flat)  # (kvk_strides: three 64-bit numbers)
 
 
 def prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, seq_tokens: Sequence[int], scale: float,
@@ -579,15 +585,16 @@ def prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, seq_toke
     _here(q, k, v, out, lse)
     if lse is not None and (lse.dtype != torch.float32 or not lse.is_contiguous() or lse.numel() != Hq * total):
         raise ValueError("lse must be contiguous fp32, Hq values per token")
-    _check(load().kvk_prompt_attention(Hq, Hkv, q.shape[-1], count, lens, q.data_ptr(), k.data_ptr(), v.data_ptr(), strides,
-                                       scale, out.data_ptr(), None if lse is None else lse.data_ptr(), _stream(stream)))
+    _check(load().kvk_prompt_attention(Hq, Hkv, q.shape[-1], count, _address(lens), q.data_ptr(), k.data_ptr(), v.data_ptr(),
+                                       _address(strides), scale, out.data_ptr(), None if lse is None else lse.data_ptr(),
+                                       _stream(stream)))
 
 
 def attention_weight_workspace_bytes(n_q_heads: int, n_kv_heads: int, head_dim: int, seq_tokens: Sequence[int]) -> int:
     out = ctypes.c_size_t(0)
-    n = len(seq_tokens)
-    _check(load().kvk_attention_weight_workspace_bytes(n_q_heads, n_kv_heads, head_dim, n,
-                                                       _lengths(seq_tokens, n, "seq_tokens"), ctypes.byref(out)))
+    lens = _lengths(seq_tokens, len(seq_tokens), "seq_tokens")
+    _check(load().kvk_attention_weight_workspace_bytes(n_q_heads, n_kv_heads, head_dim, len(lens), _address(lens),
+                                                       ctypes.byref(out)))
     return out.value
 
 
@@ -603,8 +610,8 @@ def attention_weight(q: torch.Tensor, k: torch.Tensor, lse: torch.Tensor, seq_to
         raise ValueError("lse must be contiguous fp32, Hq values per token")
     if weight.dtype != torch.float32 or not weight.is_contiguous() or weight.numel() != Hkv * total:
         raise ValueError("weight must be contiguous fp32, Hkv values per token")
-    _check(load().kvk_attention_weight(Hq, Hkv, q.shape[-1], count, lens, q.data_ptr(), k.data_ptr(), strides,
-                                       lse.data_ptr(), scale, weight.data_ptr(),
+    _check(load().kvk_attention_weight(Hq, Hkv, q.shape[-1], count, _address(lens), q.data_ptr(), k.data_ptr(),
+                                       _address(strides), lse.data_ptr(), scale, weight.data_ptr(),
                                        None if workspace is None else workspace.data_ptr(),
                                        0 if workspace is None else _nbytes(workspace), _stream(stream)))
 
@@ -655,9 +662,9 @@ def append_chunk(t: Table, layer_begin: int, layer_end: int, k: torch.Tensor, v:
     _here(k, v, arena)
     if _nbytes(arena) < t.arena_bytes:
         raise ValueError("arena smaller than arena_bytes")
+    stored, new = _lengths(n_stored, B, "n_stored"), None if n_new is None else _lengths(n_new, B, "n_new")
     _check(load().kvk_append_chunk(t.handle, layer_begin, layer_end, k.data_ptr(), v.data_ptr(), _dtype_code(k), shape[3],
-                                   _lengths(n_stored, B, "n_stored"), None if n_new is None else _lengths(n_new, B, "n_new"),
-                                   arena.data_ptr(), _stream(stream)))
+                                   _address(stored), _address(new), arena.data_ptr(), _stream(stream)))
 
 
 def chunk_workspace_bytes(t: Table, layer_begin: int, layer_end: int, n_chunk: int) -> int:
@@ -682,10 +689,10 @@ def chunk_attention(t: Table, layer_begin: int, layer_end: int, q: torch.Tensor,
     _here(q, arena, out, workspace)
     if _nbytes(arena) < t.arena_bytes:
         raise ValueError("arena smaller than arena_bytes")
-    _check(load().kvk_chunk_attention(t.handle, layer_begin, layer_end, q.data_ptr(), shape[3],
-                                      _lengths(n_stored, B, "n_stored"), None if n_new is None else _lengths(n_new, B, "n_new"),
-                                      scale, arena.data_ptr(), out.data_ptr(), workspace.data_ptr(), _nbytes(workspace),
-                                      _stream(stream)))
+    stored, new = _lengths(n_stored, B, "n_stored"), None if n_new is None else _lengths(n_new, B, "n_new")
+    _check(load().kvk_chunk_attention(t.handle, layer_begin, layer_end, q.data_ptr(), shape[3], _address(stored),
+                                      _address(new), scale, arena.data_ptr(), out.data_ptr(), workspace.data_ptr(),
+                                      _nbytes(workspace), _stream(stream)))
 
 
 def decode_attention(t: Table, layer_begin: int, layer_end: int, q: torch.Tensor, n_stored: int,
