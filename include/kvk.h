@@ -488,7 +488,9 @@ typedef struct {
  * Scores and sums are fp32; the probabilities enter the second product in bf16, hence the
  * bf16 output.  Later tokens of a sequence (and whatever lies past it) do not reach a row,
  * infinities and NaN among them.  A row whose visible scores are all -inf yields NaN and the
- * log-sum-exp -inf, a row that sees a NaN score yields NaN.
+ * log-sum-exp -inf, a row that sees a NaN score yields NaN.  An infinite value at a visible token
+ * of probability 0 (a score of -inf, or underflow) gives NaN in its channel, as 0 times
+ * infinity does; at any other visible token the infinity.
  * Errors: KVK_ERR_INVALID (sizes, strides, NULL, misalignment: q, k, v and out 16 B, lse 4 B;
  *         a scale that is not finite; host memory), KVK_ERR_UNSUPPORTED (head_dim, n_seqs),
  *         KVK_ERR_DEVICE. */
@@ -698,7 +700,8 @@ kvk_status kvk_decode_attention_noalloc(const kvk_table* table, int32_t layer_be
  * Per-sequence tables need no set-up.  Quantised layers are dequantised to fp16: their values
  * and the queries on them must lie in the fp16 range.  Scores, sums and outputs are
  * accumulated in fp32.  Tokens a row does not see (and stale slots) do not reach it,
- * infinities and NaN among them.  The host arrays are read before the call returns.
+ * infinities and NaN among them; infinite values at visible tokens count as in
+ * kvk_prompt_attention.  The host arrays are read before the call returns.
  * Errors: KVK_ERR_INVALID (range, lengths, scale, NULL pointers, misalignment: q, arena and out
  *         16 B, workspace 256 B; host memory), KVK_ERR_UNSUPPORTED (MLA table; a batch beyond
  *         65535), KVK_ERR_BUFFER (workspace), KVK_ERR_DEVICE. */

@@ -333,6 +333,17 @@ __global__ __launch_bounds__(64 * Shape<WR>::kWaves, 2) void chunk_kernel(ChunkA
     const bool masked = p0 + 32 * TB - 1 > min(seen_by_all, bound);
     const int b0 = wt * NT;  // the wave's blocks
     const int last = min(limit, bound) - p0 - 32 * b0;  // the last token of them that the row sees
+    const auto scores = [&](int k) {
+      f16v s = zero16();
+#pragma unroll
+      for (int j = 0; j < NK; ++j) s = mfma32<HALF>(key_unit(b0 + k, j), qf[j], s);
+      if (masked) {
+        asm volatile("");  // a branch: as selects these would cost every tile vector work
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s[e] = 32 * k + subtile_token(e, h) <= last ? s[e] : -INFINITY;
+      }
+      return s;
+    };
     if (masked) {
       bool bad = false;
       if (role >= 2) {
@@ -343,8 +354,13 @@ __global__ __launch_bounds__(64 * Shape<WR>::kWaves, 2) void chunk_kernel(ChunkA
       }
       if (__syncthreads_or(bad)) {
         asm volatile("");
-        take_nonfinite<NM, NT, HALF>(st, [&](int k, int x, int m) { return value_unit(b0 + k, x, m); },
-                                     [&](int k, int e) { return (uint32_t)((last - 32 * k - subtile_token(e, h)) >> 31); });
+        float m = st.m;
+#pragma unroll 1
+        for (int k = 0; k < NT; ++k) {
+          if (p0 + 32 * (b0 + k) > min(bound, seen_by_any)) break;
+          m = take_nonfinite<NM, HALF>(st, m, scores(k), a.c, kBias, [&](int x, int t) { return value_unit(b0 + k, x, t); },
+                                       [&](int e) { return (uint32_t)((last - 32 * k - subtile_token(e, h)) >> 31); });
+        }
         __syncthreads();
         if (role >= 2) {
           for (int k = own0; k < own0 + OWN; ++k) {
@@ -360,20 +376,13 @@ __global__ __launch_bounds__(64 * Shape<WR>::kWaves, 2) void chunk_kernel(ChunkA
 #pragma unroll
     for (int k = 0; k < NT; ++k) {
       if (p0 + 32 * (b0 + k) > min(bound, seen_by_any)) break;
-      f16v s[1] = {zero16()};
-#pragma unroll
-      for (int j = 0; j < NK; ++j) s[0] = mfma32<HALF>(key_unit(b0 + k, j), qf[j], s[0]);
-      if (masked) {
-        asm volatile("");  // a branch: as selects these would cost every tile vector work
-#pragma unroll
-        for (int e = 0; e < 16; ++e) s[0][e] = 32 * k + subtile_token(e, h) <= last ? s[0][e] : -INFINITY;
-      }
-      u4v p[1][2];
-      softmax_step<NM, 1, HALF>(st, s, a.c, kBias, p);
+      const f16v s = scores(k);
+      u4v p[2];
+      softmax_step<NM, HALF>(st, s, a.c, kBias, p);
 #pragma unroll
       for (int x = 0; x < 2; ++x)
 #pragma unroll
-        for (int m = 0; m < NM; ++m) st.o[m] = mfma32<HALF>(value_unit(b0 + k, x, m), p[0][x], st.o[m]);
+        for (int m = 0; m < NM; ++m) st.o[m] = mfma32<HALF>(value_unit(b0 + k, x, m), p[x], st.o[m]);
     }
     if constexpr (S::kBuffers == 1) __syncthreads();
     else buf = buf == img ? img + TB * kBlk : img;  // (its last readers are behind this tile's barrier)

@@ -255,13 +255,13 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(PromptArgs a) {
     return u4v{lo[0], lo[1], hi[0], hi[1]};
   };
 
-  f16v sc[1] = {zero16()};
+  f16v sc = zero16();
   u4v vf[2][NM];
   if (live > 0) {
 #pragma unroll
     for (int j = 0; j < NK; ++j) kf[j] = key_unit(0, j);
 #pragma unroll
-    for (int j = 0; j < NK; ++j) sc[0] = mfma32<false>(kf[j], qf[j], sc[0]);
+    for (int j = 0; j < NK; ++j) sc = mfma32<false>(kf[j], qf[j], sc);
 #pragma unroll
     for (int x = 0; x < 2; ++x)
 #pragma unroll
@@ -271,39 +271,39 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(PromptArgs a) {
   if (nt > 2) load(2);
   __syncthreads();
   for (int s = 0; s < 2 * nt; ++s) {
-    u4v p[1][2];
+    u4v p[2];
     // V(s)
     if (s < live) {
       if (32 * s + 31 > w0) {
         asm volatile("");
 #pragma unroll
-        for (int k = 0; k < 16; ++k) sc[0][k] = 32 * s + tile_row(k, h) <= w0 + col ? sc[0][k] : -INFINITY;
+        for (int k = 0; k < 16; ++k) sc[k] = 32 * s + tile_row(k, h) <= w0 + col ? sc[k] : -INFINITY;
       }
-      softmax_step<NM, 1, false>(st, sc, a.c, 0.0f, p);
       if (masked(s >> 1) && odd_tile[(s >> 1) & 3] == (s >> 1) + 1) {
         asm volatile("");
-        take_nonfinite<NM, 1, false>(
-            st, [&](int, int x, int m) { return vf[x][m]; },
-            [&](int, int k) { return (uint32_t)((row - 32 * s - tile_row(k, h)) >> 31); });
+        take_nonfinite<NM, false>(
+            st, st.m, sc, a.c, 0.0f, [&](int x, int m) { return vf[x][m]; },
+            [&](int k) { return (uint32_t)((row - 32 * s - tile_row(k, h)) >> 31); });
 #pragma unroll
         for (int x = 0; x < 2; ++x)
 #pragma unroll
           for (int m = 0; m < NM; ++m) vf[x][m] = only_finite<false>(vf[x][m]);
       }
+      softmax_step<NM, false>(st, sc, a.c, 0.0f, p);
       __builtin_amdgcn_sched_barrier(0);
       // M(s)
       const int sn = min(s + 1, 2 * nt - 1);  // (past the last step: the last one's operands again, not used)
 #pragma unroll
       for (int i = 0; i < 2 * NM; ++i) {
-        st.o[i % NM] = mfma32<false>(vf[i / NM][i % NM], p[0][i / NM], st.o[i % NM]);
+        st.o[i % NM] = mfma32<false>(vf[i / NM][i % NM], p[i / NM], st.o[i % NM]);
 #pragma unroll
         for (int j = i * NK / (2 * NM); j < (i + 1) * NK / (2 * NM); ++j) kf[j] = key_unit(sn, j);
         __builtin_amdgcn_sched_barrier(0);
       }
-      sc[0] = zero16();
+      sc = zero16();
 #pragma unroll
       for (int j = 0; j < NK; ++j) {
-        sc[0] = mfma32<false>(kf[j], qf[j], sc[0]);
+        sc = mfma32<false>(kf[j], qf[j], sc);
 #pragma unroll
         for (int i = j * 2 * NM / NK; i < (j + 1) * 2 * NM / NK; ++i) vf[i / NM][i % NM] = value_unit(sn, i / NM, i % NM);
         __builtin_amdgcn_sched_barrier(0);

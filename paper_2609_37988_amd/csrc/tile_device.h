@@ -84,42 +84,49 @@ struct RowState {
 // and most steps need no rescaling.
 constexpr float kSlack = 8.0f;
 
-// One online-softmax step over NT subtiles: scores s (times c = log2-scale: base-2 logits)
-// become probabilities 2^(c s - m + BIAS), packed for the second product in p.  c > 0.  A
+// The largest base-2 logit of a row's scores s (times c = log2-scale, c > 0).
+__device__ __forceinline__ float top_logit(const f16v& s, float c) {
+  float mx = s[0];
+#pragma unroll
+  for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[e]);
+  return halves_max(mx) * c;
+}
+// What a reference that moves from m to mnew leaves of the sums.  (A row without mass has outputs
+// of 0, or infinities and NaN by take_nonfinite: they stay.)
+__device__ __forceinline__ float rescale(float m, float mnew) {
+  return m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - mnew);
+}
+// Probabilities 2^(c s - m + bias) of scores s, packed for the second product in p; their sum.  A
 // row whose logits have all been -inf so far keeps the reference -inf, and its probabilities
 // 2^(-inf) = 0 are formed against 0.
-template <int NM, int NT, bool HALF>
-__device__ __forceinline__ void softmax_step(RowState<NM>& st, f16v (&s)[NT], float c, float bias, u4v (&p)[NT][2]) {
-  float mx = s[0][0];
+template <bool HALF>
+__device__ __forceinline__ float probabilities(float m, const f16v& s, float c, float bias, u4v (&p)[2]) {
+  const float ref = (m == -INFINITY ? 0.0f : m) - bias;
+  float sum = 0.0f;
 #pragma unroll
-  for (int i = 0; i < NT; ++i)
+  for (int x = 0; x < 2; ++x)
 #pragma unroll
-    for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[i][e]);
-  mx = halves_max(mx) * c;
+    for (int w = 0; w < 4; ++w) {
+      const int e = 8 * x + 2 * w;
+      const float a = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], c, -ref));
+      const float b = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e + 1], c, -ref));
+      sum += a + b;
+      p[x][w] = pack2<HALF>(a, b);
+    }
+  return sum;
+}
+// One online-softmax step over a subtile.
+template <int NM, bool HALF>
+__device__ __forceinline__ void softmax_step(RowState<NM>& st, const f16v& s, float c, float bias, u4v (&p)[2]) {
+  const float mx = top_logit(s, c);
   if (__any(mx > st.m + kSlack)) {
-    const float mnew = fmaxf(st.m, mx);
-    // (a row without mass has outputs of 0, or infinities and NaN by take_nonfinite: they stay)
-    const float alpha = st.m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(st.m - mnew);
+    const float mnew = fmaxf(st.m, mx), alpha = rescale(st.m, mnew);
     st.m = mnew;
     st.l *= alpha;
 #pragma unroll
     for (int i = 0; i < NM; ++i) st.o[i] *= alpha;
   }
-  const float ref = (st.m == -INFINITY ? 0.0f : st.m) - bias;
-  float sum = 0.0f;
-#pragma unroll
-  for (int i = 0; i < NT; ++i)
-#pragma unroll
-    for (int x = 0; x < 2; ++x)
-#pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        const int e = 8 * x + 2 * w;
-        const float a = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i][e], c, -ref));
-        const float b = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i][e + 1], c, -ref));
-        sum += a + b;
-        p[i][x][w] = pack2<HALF>(a, b);
-      }
-  st.l += sum;
+  st.l += probabilities<HALF>(st.m, s, c, bias, p);
 }
 
 // Whether any of the eight bf16 / fp16 values of a 16-byte unit is infinite or NaN.
@@ -143,41 +150,61 @@ __device__ __forceinline__ u4v only_finite(u4v w) {
   return w;
 }
 
-// Infinite and NaN values in a tile that some rows may not see wholly: a masked place has
-// probability 0, and 0 times infinity would reach every row of the product.  The values a row
-// does see are counted by kind in products of indicators, and each kind present is added to
-// the row's outputs (p > 0 times an infinity or a NaN is that value); the caller then takes the
-// product over the finite ones.  unit(i, x, m): the value operand of subtile i, k-step x, channel
-// tile m; hidden(i, e): all ones where the row does not see element e of subtile i, else 0.  Rare.
-template <int NM, int NT, bool HALF, class Unit, class Hidden>
-__device__ __forceinline__ void take_nonfinite(RowState<NM>& st, Unit unit, Hidden hidden) {
+// Infinite and NaN values in a subtile that some rows may not see wholly: a masked place has
+// probability 0, and 0 times infinity would reach every row of the product.  Before the subtile's
+// softmax_step the values a row does see are counted by kind in products of indicators, and each
+// kind present is added to the row's outputs, as the plain product would: a probability p > 0 times
+// an infinity or a NaN is that value, p = 0 (a score of -inf, or underflow) times an infinity is
+// NaN.  The caller then takes its steps with the finite values.  m: the reference before the
+// subtile, st.m or what this call returned for the subtile before it; returns the one after it.
+// unit(x, t): the value operand of k-step x, channel tile t; hidden(e): all ones where the row does
+// not see element e, else 0.  Rare.
+template <int NM, bool HALF, class Unit, class Hidden>
+__device__ __forceinline__ float take_nonfinite(RowState<NM>& st, float m, const f16v& s, float c, float bias, Unit unit,
+                                                Hidden hidden) {
   constexpr uint32_t kOne = HALF ? 0x3c00u : 0x3f80u, kExp = HALF ? 0x7c00u : 0x7f80u;
-#pragma unroll 1
-  for (int kind = 0; kind < 3; ++kind) {  // +infinity, -infinity, NaN
-    // a 16-bit value b is of the kind if (b & keep) - lo < span (unsigned)
-    const uint32_t keep = kind == 2 ? 0x7fffu : 0xffffu, lo = kind == 0 ? kExp : (kind == 1 ? kExp | 0x8000u : kExp + 1);
-    const uint32_t span = kind == 2 ? 0x8000u - (kExp + 1) : 1u;
+  const float mx = top_logit(s, c);
+  if (__any(mx > m + kSlack)) {
+    const float mnew = fmaxf(m, mx), alpha = rescale(m, mnew);
+    if (__any(alpha == 0.0f)) {  // now: after what is added here it would make NaN of it
+      st.m = mnew;
+      st.l *= alpha;
 #pragma unroll
-    for (int m = 0; m < NM; ++m) {
+      for (int i = 0; i < NM; ++i) st.o[i] *= alpha;
+    }
+    m = mnew;
+  }
+  u4v p[2];
+  probabilities<HALF>(m, s, c, bias, p);
+#pragma unroll 1
+  for (int kind = 0; kind < 4; ++kind) {  // +infinity and -infinity (p > 0), NaN, either infinity (p = 0)
+    asm volatile("" ::: "memory");  // (units read again for each kind, not held in registers)
+    // a 16-bit value b is of the kind if (b & keep) - lo < span (unsigned)
+    const uint32_t keep = kind >= 2 ? 0x7fffu : 0xffffu;
+    const uint32_t lo = kind == 1 ? kExp | 0x8000u : (kind == 2 ? kExp + 1 : kExp);
+    const uint32_t span = kind == 2 ? 0x8000u - (kExp + 1) : 1u;
+    const bool some = kind != 3, none = kind >= 2;  // the probabilities that count: p > 0, p = 0
+#pragma unroll
+    for (int t = 0; t < NM; ++t) {
       f16v n = zero16();
 #pragma unroll
-      for (int i = 0; i < NT; ++i)
+      for (int x = 0; x < 2; ++x) {
+        u4v v = unit(x, t), seen;
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          u4v v = unit(i, x, m), seen;
-#pragma unroll
-          for (int w = 0; w < 4; ++w) {
-            const int e = 8 * x + 2 * w;
-            seen[w] = (kOne & ~hidden(i, e)) | ((kOne << 16) & ~hidden(i, e + 1));
-            v[w] = ((v[w] & keep) - lo < span ? kOne : 0u) | (((v[w] >> 16) & keep) - lo < span ? kOne << 16 : 0u);
-          }
-          n = mfma32<HALF>(v, seen, n);
+        for (int w = 0; w < 4; ++w) {
+          const int e = 8 * x + 2 * w;
+          const bool lo_counts = (p[x][w] & 0xffffu) ? some : none, hi_counts = (p[x][w] >> 16) ? some : none;
+          seen[w] = (lo_counts ? kOne & ~hidden(e) : 0u) | (hi_counts ? (kOne << 16) & ~hidden(e + 1) : 0u);
+          v[w] = ((v[w] & keep) - lo < span ? kOne : 0u) | (((v[w] >> 16) & keep) - lo < span ? kOne << 16 : 0u);
         }
+        n = mfma32<HALF>(v, seen, n);
+      }
       const float add = kind == 0 ? INFINITY : (kind == 1 ? -INFINITY : __builtin_nanf(""));
 #pragma unroll
-      for (int e = 0; e < 16; ++e) st.o[m][e] = n[e] > 0.0f ? st.o[m][e] + add : st.o[m][e];
+      for (int e = 0; e < 16; ++e) st.o[t][e] = n[e] > 0.0f ? st.o[t][e] + add : st.o[t][e];
     }
   }
+  return m;
 }
 
 }  // namespace kvkd

@@ -1,0 +1,75 @@
+"""The multi-token operators at the edges of what they accept: infinite values at visible
+tokens, with and without mass.
+"""
+import math
+
+import pytest
+import torch
+
+from paper_2609_37988_amd import kvk
+from gpu_common import DEV
+from test_gpu_operators import Streams, _prompt_inputs, _run_chunk, _run_prompt
+
+pytestmark = pytest.mark.gpu
+NAN = float("nan")
+
+
+# --------------------------------------------------------------------------------------
+# Infinite values at visible tokens
+# --------------------------------------------------------------------------------------
+
+# Score of the token that holds the infinities, relative to the others' (of order 1), and what an
+# infinite value there gives: probability 0 times infinity is NaN, a positive one leaves infinity.
+SCALE = 0.1
+SCORES = [(-math.inf, NAN), (-30000.0, NAN), (-50.0, math.inf), (400.0, math.inf)]
+
+
+def _spoil(q, k, v, t, score):
+    """Channel 0 of the keys decides the score of token t; channels 5 to 7 of its values are not finite."""
+    q[..., 0], k[..., 0] = 1.0, 0.0
+    k[..., t, :] = 0.0
+    k[..., t, 0] = score / SCALE
+    v[..., t, 5], v[..., t, 6], v[..., t, 7] = math.inf, -math.inf, NAN
+
+
+def _check_spoilt(out, ref, t, want):
+    """out, ref [rows, heads, d], row i that of token i; ref without the infinities."""
+    d = out.shape[-1]
+    clean = [c for c in range(d) if c not in (5, 6, 7)]
+    assert torch.equal(out[:, :, clean], ref[:, :, clean]) and torch.equal(out[:t], ref[:t])
+    for ch, x in ((5, want), (6, -want), (7, NAN)):
+        got = out[t:, :, ch].float()
+        wrong = ~(torch.isnan(got) if math.isnan(x) else got == x).all(-1)
+        assert not wrong.any(), f"channel {ch}: rows {(wrong.nonzero().flatten() + t).tolist()} are not {x}"
+
+
+@pytest.mark.parametrize("score,want", SCORES)
+@pytest.mark.parametrize("d", [64, 128])
+def test_prompt_infinite_values_agree(d, score, want):
+    """Rows that see the token in the tile of the diagonal, and rows that see it in a tile which
+    the whole workgroup sees."""
+    n, t = 500, 150
+    q, k, v = _prompt_inputs(30, [n], 2, 1, d, "padded")
+    _spoil(q, k, v, t, score)
+    out, _ = _run_prompt(q, k, v, [n], SCALE)
+    v[..., t, 5:8] = 0.0
+    ref, _ = _run_prompt(q, k, v, [n], SCALE)
+    _check_spoilt(out[0, :, :n].transpose(0, 1), ref[0, :, :n].transpose(0, 1), t, want)
+
+
+@pytest.mark.parametrize("score,want", SCORES)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("hq", [3, 20, 64])
+def test_chunk_infinite_values_agree(hq, d, score, want):
+    """The same for chunks of a 16-bit layer, in narrow and wide workgroups, and in the window."""
+    n, t = 430, 150
+    for start, m, at in ((0, n, t), (n - 5, 5, t), (n - 12, 12, 425)):
+        c = Streams([(0, 16)], hq, 1, d, 1, n, kvk.KIVI32, seed=31)
+        q = torch.randn(1, 1, hq, m, d, device=DEV).bfloat16()
+        _spoil(q, c.k, c.v, at, score)
+        c.append([0], [n])
+        _, out = _run_chunk(c, 0, 1, [n], [m], SCALE, q=q)
+        c.v[..., at, 5:8] = 0.0
+        c.append([0], [n])
+        _, ref = _run_chunk(c, 0, 1, [n], [m], SCALE, q=q)
+        _check_spoilt(out[0, 0].transpose(0, 1), ref[0, 0].transpose(0, 1), max(at - start, 0), want)
