@@ -178,7 +178,10 @@ __device__ __forceinline__ Group make_group(float mn, float mx) {
   constexpr float levels = (float)((1 << BITS) - 1), inv = 1.0f / levels;
   const float d = mx - mn;
   const float q = fminf(d * inv, 3.402823466e38f);
-  const float sc = __builtin_fmaf(__builtin_fmaf(-levels, q, d), inv, q);
+  float sc = __builtin_fmaf(__builtin_fmaf(-levels, q, d), inv, q);
+  // An fp32 value of its own: fused with the conversion the step would be rounded once, to
+  // fp16, and a quotient halfway between two of those would go by the error of inv.
+  asm("" : "+v"(sc));
   const _Float16 s16 = (_Float16)sc, z16 = (_Float16)mn;
   Group g;
   const float s = (float)s16;

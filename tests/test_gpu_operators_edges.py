@@ -1,5 +1,5 @@
 """The multi-token operators at the edges of what they accept: infinite values at visible
-tokens, with and without mass.
+tokens, with and without mass, and group scales halfway between two fp16 values.
 """
 import math
 
@@ -73,3 +73,53 @@ def test_chunk_infinite_values_agree(hq, d, score, want):
         c.append([0], [n])
         _, ref = _run_chunk(c, 0, 1, [n], [m], SCALE, q=q)
         _check_spoilt(out[0, 0].transpose(0, 1), ref[0, 0].transpose(0, 1), max(at - start, 0), want)
+
+
+# --------------------------------------------------------------------------------------
+# Group scales halfway between two fp16 values
+# --------------------------------------------------------------------------------------
+
+
+def _tied_ranges(levels):
+    """(lowest, highest) bf16 values whose difference is `levels` times a 12-bit odd number (times
+    2^-10): the scale lies halfway between two fp16 values."""
+    out = []
+    for odd in range(2049, 4096, 2):
+        d = levels * odd
+        for k in range(4, 13):
+            hi, lo = d >> k << k, d & ((1 << k) - 1)
+            if hi >> k < 256 and lo < 256 and hi >> k:
+                out.append((-lo / 1024, hi / 1024))
+                break
+    assert len(out) >= 64
+    return out[::len(out) // 64][:64]
+
+
+@pytest.mark.parametrize("bits", [8, 4, 2])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("scheme", [kvk.KIVI32, kvk.GROUP64])
+def test_group_scales_round_twice_as_documented(scheme, d, bits):
+    """The scale is the fp32 quotient rounded to fp16 (the oracle's chain), in ties too: by the
+    chunk append and by the prefill write."""
+    n = 64
+    ranges = _tied_ranges((1 << bits) - 1)
+    c = Streams([(0, bits)], 1, 1, d, 1, n, scheme, seed=35)
+    for x, per_channel in ((c.k, scheme == kvk.KIVI32), (c.v, False)):
+        u = x.float().sigmoid()
+        for i in range(n if not per_channel else d):
+            lo, hi = ranges[i % len(ranges)]
+            g = u[0, 0, 0, :, i] if per_channel else u[0, 0, 0, i]
+            g.mul_(hi - lo).add_(lo)
+            g[0::32], g[1::32] = lo, hi
+        x.copy_(u)
+    c.append([0], [n])
+    want = c.values(0, 0, 0, n)
+    for write in ("append", "prefill"):
+        if write == "prefill":
+            c.arena.fill_(0xFF)
+            kvk.compress_layer(c.t, 0, c.k[0], c.v[0], n, None, c.arena)
+        got = [torch.empty((1, 1, n, d), dtype=torch.float32, device=DEV) for _ in range(2)]
+        kvk.debug_dequantize(c.t, 0, n, c.arena, *got)
+        for g, w, name in zip(got, want, "kv"):
+            wrong = (g[0, 0] != w.float()).sum()
+            assert wrong == 0, f"{write}: {int(wrong)} of {n * d} {name} values differ"
