@@ -697,9 +697,9 @@ kvk_status kvk_decode_attention_noalloc(const kvk_table* table, int32_t layer_be
  *   workspace: device, >= kvk_chunk_workspace_bytes of the range and n_chunk, 256-byte
  *              aligned; its contents on entry are ignored.  Calls that overlap on one
  *              workspace race.
- * Per-sequence tables need no set-up.  Quantised layers are dequantised to fp16: their values
- * and the queries on them must lie in the fp16 range.  Scores, sums and outputs are
- * accumulated in fp32.  Tokens a row does not see (and stale slots) do not reach it,
+ * Per-sequence tables need no set-up.  The full groups of quantised layers are dequantised to
+ * fp16: their values must lie in the fp16 range (the queries and the window are any bf16).
+ * Scores, sums and outputs are accumulated in fp32.  Tokens a row does not see (and stale slots) do not reach it,
  * infinities and NaN among them; infinite values at visible tokens count as in
  * kvk_prompt_attention.  The host arrays are read before the call returns.
  * Errors: KVK_ERR_INVALID (range, lengths, scale, NULL pointers, misalignment: q, arena and out

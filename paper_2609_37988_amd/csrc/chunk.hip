@@ -14,9 +14,12 @@
 // the rows alone leave the GPU idle the context is split over workgroups too; chunk_merge_kernel
 // joins the partial results.
 //
-// Precision: fp16 holds a dequantised value to 2^-11 relative (bf16 would to 2^-8), the queries
-// (bf16) exactly, and the probabilities, kept between 2^-24 and 2^15, to 2^-11; scores, sums and
-// partial outputs are fp32, the outputs are rounded once, to bf16.
+// Precision: in quantised layers fp16 holds a dequantised value to 2^-11 relative (bf16 would to
+// 2^-8), the queries (bf16, each row scaled by a power of two) exactly, and the probabilities, kept
+// between 2^-24 and 2^15, to 2^-11; the bf16 window meets bf16 queries and probabilities in two
+// bf16 parts.  In 16-bit layers keys, values and queries are exact and the probabilities bf16, to
+// 2^-8: fp16 would lose small and large values.  Scores, sums and partial outputs are fp32, the
+// outputs are rounded once, to bf16.
 //
 // Bound.  Few rows: the latency of a tile after another (8 ragged sequences up to 7000 tokens,
 // one new token each, int4, 32 streams: 17 us for two tiles each, merge 7).  A draft of 40 rows per
@@ -54,6 +57,7 @@ struct ChunkArgs {
   int32_t split_tiles;   // tiles of a split
   int32_t qsign;
   float c;
+  int32_t most_lift;     // the largest power of two that a row of queries may be scaled by
   int32_t total_rows;    // rows of all streams
   int64_t region[kChunkSeqs];   // of the sequence's first stream
   int32_t stored[kChunkSeqs], fresh[kChunkSeqs];  // tokens stored, the last `fresh` of them new
@@ -194,14 +198,34 @@ struct Part {
   }
 };
 
-__device__ __forceinline__ u4v bf16_to_half_unit(u4v w) {
-  half8 r;
+// A row of bf16 queries (the lane's half of it) as fp16, exactly but for values 2^29 times smaller
+// than the row's largest: fp16 has bf16's digits but fewer exponents, so the row is scaled by
+// the power of two that brings its largest value to 2^15 (at most 2^most), and c, the scores'
+// factor, takes it back.  Rows of zeros, and with infinities or NaN, are left as they are.
+template <int NK>
+__device__ __forceinline__ float queries_to_half(u4v (&q)[NK], float c, int most) {
+  typedef uint16_t us2 __attribute__((ext_vector_type(2)));
+  us2 top = {0, 0};
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    r[2 * i] = (_Float16)__uint_as_float(w[i] << 16);
-    r[2 * i + 1] = (_Float16)__uint_as_float(w[i] & 0xffff0000u);
+  for (int j = 0; j < NK; ++j)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) top = __builtin_elementwise_max(top, bitcast<us2>(q[j][i] & 0x7fff7fffu));
+  // (positive bf16 values order as their bits do, NaN above infinity)
+  const float mx = halves_max(__uint_as_float((uint32_t)max(top[0], top[1]) << 16));
+  const int ex = (int)(__float_as_uint(mx) >> 23);
+  const int up = mx == 0.0f || ex == 255 ? 0 : min(127 + 15 - ex, most);
+  const float f = __uint_as_float((uint32_t)(127 + up) << 23);
+#pragma unroll
+  for (int j = 0; j < NK; ++j) {
+    half8 r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      r[2 * i] = (_Float16)(__uint_as_float(q[j][i] << 16) * f);
+      r[2 * i + 1] = (_Float16)(__uint_as_float(q[j][i] & 0xffff0000u) * f);
+    }
+    q[j] = bitcast<u4v>(r);
   }
-  return bitcast<u4v>(r);
+  return __builtin_ldexpf(c, -up);
 }
 
 // Token of element e in half h of a 32-token subtile: the key rows of the first product are
@@ -262,16 +286,20 @@ __global__ __launch_bounds__(64 * Shape<WR>::kWaves, 2) void chunk_kernel(ChunkA
   const auto place = [&](int blk) { return buf + blk * kBlk + (role < 2 ? role * 32 * D : 64 * D + (role - 2) * 1024 * P::UN); };
   if (tile0 < tile1) load(tile0);
 
-  u4v qf[NK];
+  const auto load_queries = [&](u4v (&x)[NK]) {
 #pragma unroll
-  for (int j = 0; j < NK; ++j) {
-    u4v x = *reinterpret_cast<const u4v*>(a.q + qrow + 16 * j + 8 * h);
-    if (a.qsign <= 0) {
+    for (int j = 0; j < NK; ++j) {
+      x[j] = *reinterpret_cast<const u4v*>(a.q + qrow + 16 * j + 8 * h);
+      if (a.qsign <= 0) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) x[i] = a.qsign < 0 ? x[i] ^ 0x80008000u : 0u;
+        for (int i = 0; i < 4; ++i) x[j][i] = a.qsign < 0 ? x[j][i] ^ 0x80008000u : 0u;
+      }
     }
-    qf[j] = HALF ? bf16_to_half_unit(x) : x;
-  }
+  };
+  u4v qf[NK];
+  load_queries(qf);
+  float c = a.c;
+  if constexpr (HALF) c = queries_to_half(qf, a.c, a.most_lift);
   RowState<NM> st;
   st.clear();
   constexpr float kBias = HALF ? 7.0f : 0.0f;  // 2^(kBias + kSlack) is the largest probability
@@ -287,87 +315,68 @@ __global__ __launch_bounds__(64 * Shape<WR>::kWaves, 2) void chunk_kernel(ChunkA
     return *reinterpret_cast<const u4v*>(buf + vat + blk * kBlk + 2048 * m + 512 * x);
   };
 
-  // Tiles of full blocks, then the bf16 window (one block) as one more.
-  const int n_tiles = max(tile1 - tile0, 0) + (tail ? 1 : 0);
-  for (int i = 0; i < n_tiles; ++i) {
-    const int tile = tile0 + i;
-    const bool window = tile >= tile1;
-    const int p0 = window ? 32 * nbf : 32 * TB * tile;   // the first token's position
-    const int bound = window ? stored - 1 : 32 * nbf - 1;  // the last position that holds a token of it
-    if (!window) {
+  // Whether a value of the blocks [k0, k1) of the tile is infinite or NaN (the wave's part of
+  // them), and those values replaced by zero.
+  const auto nonfinite = [&]<bool H>(std::bool_constant<H>, int k0, int k1) {
+    bool bad = false;
+    for (int k = k0; k < k1 && role >= 2; ++k) {
+      const u4v* u = reinterpret_cast<const u4v*>(place(k) + 16 * lane);
+      for (int y = 0; y < P::UN; ++y) bad |= any_nonfinite<H>(u[64 * y]);
+    }
+    return bad;
+  };
+  const auto clean = [&]<bool H>(std::bool_constant<H>, int k0, int k1) {
+    for (int k = k0; k < k1 && role >= 2; ++k) {
+      u4v* u = reinterpret_cast<u4v*>(place(k) + 16 * lane);
+      for (int y = 0; y < P::UN; ++y) u[64 * y] = only_finite<H>(u[64 * y]);
+    }
+  };
+  // Scores of block blk; of a masked tile -inf where the row does not see them: past token `last`
+  // of the block.
+  const auto scores = [&]<bool H>(std::bool_constant<H>, const u4v (&q)[NK], int blk, bool masked, int last) {
+    f16v s = zero16();
 #pragma unroll
-      for (int k = 0; k < OWN; ++k) {
-        if (tile * TB + own0 + k < nbf) {
-          part[k].store(place(own0 + k), slots[wave], role, lane);
-        } else if (role >= 2) {  // past the full blocks: no value may enter a product
+    for (int j = 0; j < NK; ++j) s = mfma32<H>(key_unit(blk, j), q[j], s);
+    if (masked) {
+      asm volatile("");  // a branch: as selects these would cost every tile vector work
 #pragma unroll
-          for (int u = 0; u < P::UN; ++u) reinterpret_cast<u4v*>(place(own0 + k) + 16 * lane)[64 * u] = u4v{0, 0, 0, 0};
-        }
-      }
-      if (tile + 1 < tile1) load(tile + 1);
-    } else {
-      const uint8_t* tb = stream + (int64_t)a.nb_cap * a.block_bytes;
-      const u4v* in = reinterpret_cast<const u4v*>(tb + (role < 2 ? role * 32 * D : 64 * D + (role - 2) * 1024 * P::UN)) + lane;
+      for (int e = 0; e < 16; ++e) s[e] = subtile_token(e, h) <= last ? s[e] : -INFINITY;
+    }
+    return s;
+  };
+  const auto hidden = [&](int last, int e) { return (uint32_t)((last - subtile_token(e, h)) >> 31); };
+  constexpr std::bool_constant<HALF> kTileType;
+
+  for (int tile = tile0; tile < tile1; ++tile) {
+    const int p0 = 32 * TB * tile, bound = 32 * nbf - 1;  // the first token's position; the last full block's
 #pragma unroll
-      for (int k = 0; k < OWN; ++k) {
-        u4v* to = reinterpret_cast<u4v*>(place(own0 + k) + 16 * lane);
-        if (own0 + k == 0) {
+    for (int k = 0; k < OWN; ++k) {
+      if (tile * TB + own0 + k < nbf) {
+        part[k].store(place(own0 + k), slots[wave], role, lane);
+      } else if (role >= 2) {  // past the full blocks: no value may enter a product
 #pragma unroll
-          for (int u = 0; u < P::UN; ++u) {
-            u4v x = in[64 * u];
-            if (role >= 2) {  // slots past the tokens hold anything
-#pragma unroll
-              for (int n = 0; n < 8; ++n)
-                if (16 * (n >> 2) + 4 * (lane >> 4) + (n & 3) >= stored % 32) x[n >> 1] &= n & 1 ? 0x0000ffffu : 0xffff0000u;
-            }
-            to[64 * u] = HALF ? bf16_to_half_unit(x) : x;
-          }
-        } else if (role >= 2) {
-#pragma unroll
-          for (int u = 0; u < P::UN; ++u) to[64 * u] = u4v{0, 0, 0, 0};
-        }
+        for (int u = 0; u < P::UN; ++u) reinterpret_cast<u4v*>(place(own0 + k) + 16 * lane)[64 * u] = u4v{0, 0, 0, 0};
       }
     }
+    if (tile + 1 < tile1) load(tile + 1);
     // A tile that some row does not see wholly: masked scores, and a look for infinities and NaN
     // among its values (see take_nonfinite).
     const bool masked = p0 + 32 * TB - 1 > min(seen_by_all, bound);
     const int b0 = wt * NT;  // the wave's blocks
     const int last = min(limit, bound) - p0 - 32 * b0;  // the last token of them that the row sees
-    const auto scores = [&](int k) {
-      f16v s = zero16();
-#pragma unroll
-      for (int j = 0; j < NK; ++j) s = mfma32<HALF>(key_unit(b0 + k, j), qf[j], s);
-      if (masked) {
-        asm volatile("");  // a branch: as selects these would cost every tile vector work
-#pragma unroll
-        for (int e = 0; e < 16; ++e) s[e] = 32 * k + subtile_token(e, h) <= last ? s[e] : -INFINITY;
-      }
-      return s;
-    };
     if (masked) {
-      bool bad = false;
-      if (role >= 2) {
-        for (int k = own0; k < own0 + OWN; ++k) {
-          const u4v* u = reinterpret_cast<const u4v*>(place(k) + 16 * lane);
-          for (int y = 0; y < P::UN; ++y) bad |= any_nonfinite<HALF>(u[64 * y]);
-        }
-      }
-      if (__syncthreads_or(bad)) {
+      if (__syncthreads_or(nonfinite(kTileType, own0, own0 + OWN))) {
         asm volatile("");
         float m = st.m;
 #pragma unroll 1
         for (int k = 0; k < NT; ++k) {
           if (p0 + 32 * (b0 + k) > min(bound, seen_by_any)) break;
-          m = take_nonfinite<NM, HALF>(st, m, scores(k), a.c, kBias, [&](int x, int t) { return value_unit(b0 + k, x, t); },
-                                       [&](int e) { return (uint32_t)((last - 32 * k - subtile_token(e, h)) >> 31); });
+          m = take_nonfinite<NM, HALF>(st, m, scores(kTileType, qf, b0 + k, true, last - 32 * k), c, kBias,
+                                       [&](int x, int t) { return value_unit(b0 + k, x, t); },
+                                       [&](int e) { return hidden(last - 32 * k, e); });
         }
         __syncthreads();
-        if (role >= 2) {
-          for (int k = own0; k < own0 + OWN; ++k) {
-            u4v* u = reinterpret_cast<u4v*>(place(k) + 16 * lane);
-            for (int y = 0; y < P::UN; ++y) u[64 * y] = only_finite<HALF>(u[64 * y]);
-          }
-        }
+        clean(kTileType, own0, own0 + OWN);
         __syncthreads();
       }
     } else {
@@ -376,9 +385,9 @@ __global__ __launch_bounds__(64 * Shape<WR>::kWaves, 2) void chunk_kernel(ChunkA
 #pragma unroll
     for (int k = 0; k < NT; ++k) {
       if (p0 + 32 * (b0 + k) > min(bound, seen_by_any)) break;
-      const f16v s = scores(k);
+      const f16v s = scores(kTileType, qf, b0 + k, masked, last - 32 * k);
       u4v p[2];
-      softmax_step<NM, HALF>(st, s, a.c, kBias, p);
+      softmax_step<NM, HALF>(st, s, c, kBias, p);
 #pragma unroll
       for (int x = 0; x < 2; ++x)
 #pragma unroll
@@ -386,6 +395,54 @@ __global__ __launch_bounds__(64 * Shape<WR>::kWaves, 2) void chunk_kernel(ChunkA
     }
     if constexpr (S::kBuffers == 1) __syncthreads();
     else buf = buf == img ? img + TB * kBlk : img;  // (its last readers are behind this tile's barrier)
+  }
+
+  // The window, one block of bf16 tokens, in bf16 products for every layer (its values are any
+  // bf16; fp16 would lose the small ones).  Quantised layers keep their probabilities' precision
+  // by a second product with what the rounding left.  The waves of the first share take it.
+  if (tail) {
+    if (own0 == 0) {
+      const uint8_t* tb = stream + (int64_t)a.nb_cap * a.block_bytes;
+      const u4v* in = reinterpret_cast<const u4v*>(tb + (role < 2 ? role * 32 * D : 64 * D + (role - 2) * 1024 * P::UN)) + lane;
+#pragma unroll
+      for (int u = 0; u < P::UN; ++u) {
+        u4v x = in[64 * u];
+        if (role >= 2) {  // slots past the tokens hold anything
+#pragma unroll
+          for (int n = 0; n < 8; ++n)
+            if (16 * (n >> 2) + 4 * (lane >> 4) + (n & 3) >= stored % 32) x[n >> 1] &= n & 1 ? 0x0000ffffu : 0xffff0000u;
+        }
+        reinterpret_cast<u4v*>(place(0) + 16 * lane)[64 * u] = x;
+      }
+    }
+    const int k1 = own0 == 0 ? 1 : 0, last = limit - 32 * nbf;
+    const bool odd = __syncthreads_or(nonfinite(std::false_type(), 0, k1));
+    f16v s;
+    if (wt == 0) {
+      if constexpr (HALF) load_queries(qf);
+      s = scores(std::false_type(), qf, 0, true, last);
+    }
+    if (odd) {
+      asm volatile("");
+      if (wt == 0)
+        take_nonfinite<NM, false>(st, st.m, s, a.c, kBias, [&](int x, int t) { return value_unit(0, x, t); },
+                                  [&](int e) { return hidden(last, e); });
+      __syncthreads();
+      clean(std::false_type(), 0, k1);
+      __syncthreads();
+    }
+    if (wt == 0) {
+      u4v p[2], rest[2];
+      softmax_step<NM, false>(st, s, a.c, kBias, p, HALF ? rest : nullptr);
+#pragma unroll
+      for (int x = 0; x < 2; ++x)
+#pragma unroll
+        for (int m = 0; m < NM; ++m) {
+          const u4v v = value_unit(0, x, m);
+          st.o[m] = mfma32<false>(v, p[x], st.o[m]);
+          if constexpr (HALF) st.o[m] = mfma32<false>(v, rest[x], st.o[m]);
+        }
+    }
   }
   __syncthreads();
 
@@ -690,6 +747,7 @@ extern "C" kvk_status kvk_chunk_attention(const kvk_table* t, int32_t l0, int32_
   a.nb_cap = t->nb_cap;
   a.qsign = scale > 0.0f ? 1 : (scale < 0.0f ? -1 : 0);
   a.c = a.qsign ? std::fabs(scale) * kLog2e : 1.0f;
+  a.most_lift = std::min(60, std::ilogb(a.c) + 60);  // (c / 2^most_lift stays a normal number)
   // One launch for the sequences that read the same layers from an anchor of one bit-width (one
   // plan: all of them), in groups of kChunkSeqs.  Two passes: every launch is laid out and
   // checked before the first one is made.

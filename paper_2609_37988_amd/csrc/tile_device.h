@@ -98,9 +98,11 @@ __device__ __forceinline__ float rescale(float m, float mnew) {
 }
 // Probabilities 2^(c s - m + bias) of scores s, packed for the second product in p; their sum.  A
 // row whose logits have all been -inf so far keeps the reference -inf, and its probabilities
-// 2^(-inf) = 0 are formed against 0.
+// 2^(-inf) = 0 are formed against 0.  rest: NULL, or what the rounding to bf16 left of them (p and
+// rest together hold 16 bits).
 template <bool HALF>
-__device__ __forceinline__ float probabilities(float m, const f16v& s, float c, float bias, u4v (&p)[2]) {
+__device__ __forceinline__ float probabilities(float m, const f16v& s, float c, float bias, u4v (&p)[2],
+                                               u4v* rest = nullptr) {
   const float ref = (m == -INFINITY ? 0.0f : m) - bias;
   float sum = 0.0f;
 #pragma unroll
@@ -112,12 +114,15 @@ __device__ __forceinline__ float probabilities(float m, const f16v& s, float c, 
       const float b = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e + 1], c, -ref));
       sum += a + b;
       p[x][w] = pack2<HALF>(a, b);
+      if (rest)
+        rest[x][w] = pack2<HALF>(a - __uint_as_float(p[x][w] << 16), b - __uint_as_float(p[x][w] & 0xffff0000u));
     }
   return sum;
 }
 // One online-softmax step over a subtile.
 template <int NM, bool HALF>
-__device__ __forceinline__ void softmax_step(RowState<NM>& st, const f16v& s, float c, float bias, u4v (&p)[2]) {
+__device__ __forceinline__ void softmax_step(RowState<NM>& st, const f16v& s, float c, float bias, u4v (&p)[2],
+                                             u4v* rest = nullptr) {
   const float mx = top_logit(s, c);
   if (__any(mx > st.m + kSlack)) {
     const float mnew = fmaxf(st.m, mx), alpha = rescale(st.m, mnew);
@@ -126,7 +131,7 @@ __device__ __forceinline__ void softmax_step(RowState<NM>& st, const f16v& s, fl
 #pragma unroll
     for (int i = 0; i < NM; ++i) st.o[i] *= alpha;
   }
-  st.l += probabilities<HALF>(st.m, s, c, bias, p);
+  st.l += probabilities<HALF>(st.m, s, c, bias, p, rest);
 }
 
 // Whether any of the eight bf16 / fp16 values of a 16-byte unit is infinite or NaN.

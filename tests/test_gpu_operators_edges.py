@@ -1,5 +1,6 @@
 """The multi-token operators at the edges of what they accept: infinite values at visible
-tokens, with and without mass, and group scales halfway between two fp16 values.
+tokens, with and without mass, small values and queries, and group scales halfway between two
+fp16 values.
 """
 import math
 
@@ -8,7 +9,7 @@ import torch
 
 from paper_2609_37988_amd import kvk
 from gpu_common import DEV
-from test_gpu_operators import Streams, _prompt_inputs, _run_chunk, _run_prompt
+from test_gpu_operators import Streams, _check_chunk, _prompt_inputs, _run_chunk, _run_prompt
 
 pytestmark = pytest.mark.gpu
 NAN = float("nan")
@@ -73,6 +74,51 @@ def test_chunk_infinite_values_agree(hq, d, score, want):
         c.append([0], [n])
         _, ref = _run_chunk(c, 0, 1, [n], [m], SCALE, q=q)
         _check_spoilt(out[0, 0].transpose(0, 1), ref[0, 0].transpose(0, 1), max(at - start, 0), want)
+
+
+@pytest.mark.parametrize("score,want", SCORES)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("hq", [3, 20, 64])
+def test_chunk_infinite_values_in_the_window_of_a_quantised_layer(hq, d, score, want):
+    n, m, at = 430, 12, 425
+    c = Streams([(0, 4)], hq, 1, d, 1, n, kvk.KIVI32, seed=36)
+    q = torch.randn(1, 1, hq, m, d, device=DEV).bfloat16()
+    _spoil(q, c.k, c.v, at, score)
+    c.append([0], [n])
+    _, out = _run_chunk(c, 0, 1, [n], [m], SCALE, q=q)
+    c.v[..., at, 5:8] = 0.0
+    c.append([0], [n])
+    _, ref = _run_chunk(c, 0, 1, [n], [m], SCALE, q=q)
+    _check_spoilt(out[0, 0].transpose(0, 1), ref[0, 0].transpose(0, 1), at - (n - m), want)
+
+
+# --------------------------------------------------------------------------------------
+# Small values
+# --------------------------------------------------------------------------------------
+
+STORED = [1, 20, 33, 64, 129, 200, 517, 97]
+NEW = [[1] * 8, [1, 20, 33, 4, 6, 7, 3, 1], [1, 11, 20, 33, 60, 100, 0, 40]]
+
+
+def _small(scheme, d, bits, hq, kv, qf):
+    """Keys and values scaled by kv, queries by qf, the softmax scale to match."""
+    c = Streams([(0, bits)], hq, 1, d, 8, 520, scheme, seed=32)
+    c.k, c.v = c.k * kv, c.v * kv
+    c.append([0] * 8, STORED)
+    scale = 0.8 / math.sqrt(d) / (kv * qf)
+    for new in NEW:
+        q = (torch.randn(1, 8, hq, max(new), d, device=DEV) * qf).bfloat16()
+        _, out = _run_chunk(c, 0, 1, STORED, new, scale, q=q)
+        _check_chunk(c, 0, 1, STORED, new, scale, q, out)
+
+
+@pytest.mark.parametrize("scheme", [kvk.KIVI32, kvk.GROUP64])
+@pytest.mark.parametrize("bits", [16, 8, 4, 2])
+@pytest.mark.parametrize("d,hq", [(64, 64), (128, 5)])
+@pytest.mark.parametrize("kv,qf", [(2.0**-12, 1.0), (2.0**-18, 1.0), (1.0, 2.0**-12), (1.0, 2.0**-30), (2.0**-18, 2.0**12)])
+def test_chunk_small_values(kv, qf, d, hq, bits, scheme):
+    """Values and queries below fp16's normal range, in full blocks and in the window."""
+    _small(scheme, d, bits, hq, kv, qf)
 
 
 # --------------------------------------------------------------------------------------
