@@ -15,7 +15,8 @@
 // joins the partial results.
 //
 // Precision: in quantised layers fp16 holds a dequantised value to 2^-11 relative (bf16 would to
-// 2^-8), the queries (bf16, each row scaled by a power of two) exactly, and the probabilities, kept
+// 2^-8; SYMROW's blocks are scaled by a power of two each, as their bf16 scales reach further than
+// fp16: see Part::lift), the queries (bf16, each row scaled by a power of two) exactly, and the probabilities, kept
 // between 2^-24 and 2^15, to 2^-11; the bf16 window meets bf16 queries and probabilities in two
 // bf16 parts.  In 16-bit layers keys, values and queries are exact and the probabilities bf16, to
 // 2^-8: fp16 would lose small and large values.  Scores, sums and partial outputs are fp32, the
@@ -43,6 +44,7 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kChunkSeqs = 96;  // sequences of a launch
+constexpr int kMostLift = 60;   // largest power of two that scales a block or a row of queries
 
 struct ChunkArgs {
   const uint8_t* arena;
@@ -96,6 +98,8 @@ __device__ __forceinline__ int find_seq(const int32_t* start, int n, int x, int 
   return __builtin_amdgcn_readfirstlane(at);
 }
 
+__device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((uint32_t)(127 + e) << 23); }  // |e| < 127
+
 // A wave's part of a block: the keys of 16 tokens (roles 0, 1) or half the channels' values
 // (roles 2, 3), D / 32 units of eight values per lane.  Raw codes as loaded ahead of use, and
 // the part's scales and zeros, which go through a slot of LDS that is the wave's own.
@@ -148,28 +152,54 @@ struct Part {
     else return unpack2_half(w[u >> 1] >> (8 * (u & 1)), off);
   }
 
-  // The units' values to their places (1 KiB apart) at dst.
-  __device__ __forceinline__ void store(uint8_t* dst, uint32_t* slot, int role, int lane) const {
+  // The power of two that a SYMROW block's values are stored multiplied by: it brings the largest
+  // scale of the part's 32 tokens to [2^7, 2^8), so that every product with a code is in fp16's
+  // range and the scales (bf16) are exact down to 2^-24 of the largest.  scales: the lane's two of
+  // them so multiplied, in fp16.
+  __device__ __forceinline__ int lift(int lane, uint32_t& scales) const {
+    const uint32_t w = lane < 16 ? meta[0] : 0u, lo = w << 16, hi = w & 0xffff0000u;
+    // (positive fp32 values order as their bits do; infinite scales do not count)
+    uint32_t top = max(lo < 0x7f800000u ? lo : 0u, hi < 0x7f800000u ? hi : 0u);
+    top = max(top, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, kQuadXor1, 0xF, 0xF, false));
+    top = max(top, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, kQuadXor2, 0xF, 0xF, false));
+    top = max(top, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, kHalfRowMirror, 0xF, 0xF, false));
+    top = max(top, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, kRowMirror, 0xF, 0xF, false));
+    const int ex = __builtin_amdgcn_readfirstlane((int)(top >> 23));
+    const int up = ex == 0 ? 0 : max(min(127 + 7 - ex, kMostLift), -kMostLift);
+    const float f = power_of_two(up);
+    scales = bitcast<uint32_t>(h2(__uint_as_float(lo) * f, __uint_as_float(hi) * f));
+    return up;
+  }
+
+  // The units' values to their places (1 KiB apart) at dst; SYMROW: times 2^up, the result.
+  __device__ __forceinline__ int store(uint8_t* dst, uint32_t* slot, int role, int lane) const {
+    int up = 0;
     u4v* out = reinterpret_cast<u4v*>(dst + 16 * lane);
     if constexpr (BITS == 16) {
 #pragma unroll
       for (int u = 0; u < UN; ++u) out[64 * u] = u4v{w[4 * u], w[4 * u + 1], w[4 * u + 2], w[4 * u + 3]};
-      return;
     } else {
       const int kg = lane >> 4, i = lane & 15;
 #pragma unroll
-      for (int j = 0; j < MW; ++j)
-        if (64 * j + lane < MBYTES / 4) slot[64 * j + lane] = meta[j];
+      for (int j = 0; j < MW; ++j) {
+        uint32_t word = meta[j];
+        if constexpr (QS == kQsSym) up = lift(lane, word);
+        if (64 * j + lane < MBYTES / 4) slot[64 * j + lane] = word;
+      }
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       __builtin_amdgcn_wave_barrier();
       const half8* h8 = reinterpret_cast<const half8*>(slot);
       const _Float16* h1 = reinterpret_cast<const _Float16*>(slot);
       if constexpr (QS == kQsSym) {
-        const uint16_t* b1 = reinterpret_cast<const uint16_t*>(slot);
         half8 s;
-#pragma unroll
-        for (int n = 0; n < 8; ++n)
-          s[n] = (_Float16)bf16_to_f32(b1[role < 2 ? 16 * role + i : 16 * (n >> 2) + 4 * kg + (n & 3)]);
+        if (role < 2) {
+          const _Float16 x = h1[16 * role + i];
+          s = half8{x, x, x, x, x, x, x, x};
+        } else {
+          const u2v* h4 = reinterpret_cast<const u2v*>(slot);
+          const u2v x = h4[kg], y = h4[4 + kg];
+          s = bitcast<half8>(u4v{x[0], x[1], y[0], y[1]});
+        }
 #pragma unroll
         for (int u = 0; u < UN; ++u) out[64 * u] = bitcast<u4v>(codes(u, (float)(1 << (BITS - 1))) * s);
       } else {
@@ -195,6 +225,7 @@ struct Part {
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       __builtin_amdgcn_wave_barrier();
     }
+    return up;
   }
 };
 
@@ -214,7 +245,7 @@ __device__ __forceinline__ float queries_to_half(u4v (&q)[NK], float c, int most
   const float mx = halves_max(__uint_as_float((uint32_t)max(top[0], top[1]) << 16));
   const int ex = (int)(__float_as_uint(mx) >> 23);
   const int up = mx == 0.0f || ex == 255 ? 0 : min(127 + 15 - ex, most);
-  const float f = __uint_as_float((uint32_t)(127 + up) << 23);
+  const float f = power_of_two(up);
 #pragma unroll
   for (int j = 0; j < NK; ++j) {
     half8 r;
@@ -234,6 +265,11 @@ __device__ __forceinline__ constexpr int subtile_token(int e, int h) {
   return 16 * ((e >> 2) & 1) + 8 * (e >> 3) + 4 * h + (e & 3);
 }
 
+// A SYMROW block's powers of two (Part::lift): 2^-up of its keys, up and 2^up of its values.
+struct Lift {
+  float keys, drop, grow;
+};
+
 template <int D, int BITS, int QS, int WR>
 __global__ __launch_bounds__(64 * Shape<WR>::kWaves, 2) void chunk_kernel(ChunkArgs a) {
   using S = Shape<WR>;
@@ -246,6 +282,8 @@ __global__ __launch_bounds__(64 * Shape<WR>::kWaves, 2) void chunk_kernel(ChunkA
   __shared__ __align__(16) uint8_t img[kTile > kJoin ? kTile : kJoin];
   __shared__ __align__(16) uint32_t slots[S::kWaves][kSlot];
   __shared__ float2 stats[4][32];
+  constexpr bool SYM = BITS != 16 && QS == kQsSym;
+  __shared__ Lift lifts[S::kBuffers][SYM ? TB : 1];  // of a tile's blocks
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int col = lane & 31, h = lane >> 5;
   const int wr = wave % WR, wt = wave / WR;
@@ -347,12 +385,19 @@ __global__ __launch_bounds__(64 * Shape<WR>::kWaves, 2) void chunk_kernel(ChunkA
   const auto hidden = [&](int last, int e) { return (uint32_t)((last - subtile_token(e, h)) >> 31); };
   constexpr std::bool_constant<HALF> kTileType;
 
+  Lift* lift = lifts[0];  // of the tile in work
+
   for (int tile = tile0; tile < tile1; ++tile) {
     const int p0 = 32 * TB * tile, bound = 32 * nbf - 1;  // the first token's position; the last full block's
 #pragma unroll
     for (int k = 0; k < OWN; ++k) {
       if (tile * TB + own0 + k < nbf) {
-        part[k].store(place(own0 + k), slots[wave], role, lane);
+        const int up = part[k].store(place(own0 + k), slots[wave], role, lane);
+        if (SYM && role == 0 && lane == 0) lift[own0 + k].keys = power_of_two(-up);
+        if (SYM && role == 2 && lane == 0) {
+          lift[own0 + k].drop = (float)up;
+          lift[own0 + k].grow = power_of_two(up);
+        }
       } else if (role >= 2) {  // past the full blocks: no value may enter a product
 #pragma unroll
         for (int u = 0; u < P::UN; ++u) reinterpret_cast<u4v*>(place(own0 + k) + 16 * lane)[64 * u] = u4v{0, 0, 0, 0};
@@ -371,9 +416,10 @@ __global__ __launch_bounds__(64 * Shape<WR>::kWaves, 2) void chunk_kernel(ChunkA
 #pragma unroll 1
         for (int k = 0; k < NT; ++k) {
           if (p0 + 32 * (b0 + k) > min(bound, seen_by_any)) break;
-          m = take_nonfinite<NM, HALF>(st, m, scores(kTileType, qf, b0 + k, true, last - 32 * k), c, kBias,
+          const Lift x2 = SYM ? lift[b0 + k] : Lift{1.0f, 0.0f, 1.0f};
+          m = take_nonfinite<NM, HALF>(st, m, scores(kTileType, qf, b0 + k, true, last - 32 * k), c * x2.keys, kBias,
                                        [&](int x, int t) { return value_unit(b0 + k, x, t); },
-                                       [&](int e) { return hidden(last - 32 * k, e); });
+                                       [&](int e) { return hidden(last - 32 * k, e); }, x2.drop);
         }
         __syncthreads();
         clean(kTileType, own0, own0 + OWN);
@@ -385,16 +431,20 @@ __global__ __launch_bounds__(64 * Shape<WR>::kWaves, 2) void chunk_kernel(ChunkA
 #pragma unroll
     for (int k = 0; k < NT; ++k) {
       if (p0 + 32 * (b0 + k) > min(bound, seen_by_any)) break;
+      const Lift x2 = SYM ? lift[b0 + k] : Lift{1.0f, 0.0f, 1.0f};
       const f16v s = scores(kTileType, qf, b0 + k, masked, last - 32 * k);
       u4v p[2];
-      softmax_step<NM, HALF>(st, s, c, kBias, p);
+      softmax_step<NM, HALF>(st, s, c * x2.keys, kBias, p, nullptr, x2.drop, x2.grow);
 #pragma unroll
       for (int x = 0; x < 2; ++x)
 #pragma unroll
         for (int m = 0; m < NM; ++m) st.o[m] = mfma32<HALF>(value_unit(b0 + k, x, m), p[x], st.o[m]);
     }
     if constexpr (S::kBuffers == 1) __syncthreads();
-    else buf = buf == img ? img + TB * kBlk : img;  // (its last readers are behind this tile's barrier)
+    else {  // (its last readers are behind this tile's barrier)
+      buf = buf == img ? img + TB * kBlk : img;
+      lift = lift == lifts[0] ? lifts[S::kBuffers - 1] : lifts[0];
+    }
   }
 
   // The window, one block of bf16 tokens, in bf16 products for every layer (its values are any
@@ -747,7 +797,7 @@ extern "C" kvk_status kvk_chunk_attention(const kvk_table* t, int32_t l0, int32_
   a.nb_cap = t->nb_cap;
   a.qsign = scale > 0.0f ? 1 : (scale < 0.0f ? -1 : 0);
   a.c = a.qsign ? std::fabs(scale) * kLog2e : 1.0f;
-  a.most_lift = std::min(60, std::ilogb(a.c) + 60);  // (c / 2^most_lift stays a normal number)
+  a.most_lift = std::min(kMostLift, std::ilogb(a.c) + kMostLift);  // (c / 2^(2 kMostLift) stays a normal number)
   // One launch for the sequences that read the same layers from an anchor of one bit-width (one
   // plan: all of them), in groups of kChunkSeqs.  Two passes: every launch is laid out and
   // checked before the first one is made.

@@ -67,6 +67,10 @@ __device__ __forceinline__ u2v read_transposed(const uint8_t* p) {
 
 // Running state of a wave's 32 query rows: output accumulators (32 NM channels), reference
 // maximum in base-2 logits, and the lane's share of the sum.
+// Scaled values: a subtile whose values enter the product multiplied by 2^drop gets its logits
+// lowered by drop instead (softmax_step's argument), and its part of the sum multiplied by 2^drop;
+// the reference is then the maximum of the lowered logits, so that probabilities and scaled
+// values both stay in range.  (drop 0, the default, costs nothing: x - 0 and 1 x fold.)
 template <int NM>
 struct RowState {
   f16v o[NM];
@@ -85,25 +89,25 @@ struct RowState {
 constexpr float kSlack = 8.0f;
 
 // The largest base-2 logit of a row's scores s (times c = log2-scale, c > 0).
-__device__ __forceinline__ float top_logit(const f16v& s, float c) {
+__device__ __forceinline__ float top_logit(const f16v& s, float c, float drop) {
   float mx = s[0];
 #pragma unroll
   for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[e]);
-  return halves_max(mx) * c;
+  return halves_max(mx) * c - drop;
 }
 // What a reference that moves from m to mnew leaves of the sums.  (A row without mass has outputs
 // of 0, or infinities and NaN by take_nonfinite: they stay.)
 __device__ __forceinline__ float rescale(float m, float mnew) {
   return m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - mnew);
 }
-// Probabilities 2^(c s - m + bias) of scores s, packed for the second product in p; their sum.  A
+// Probabilities 2^(c s - drop - m + bias) of scores s, packed for the second product in p; their sum.  A
 // row whose logits have all been -inf so far keeps the reference -inf, and its probabilities
 // 2^(-inf) = 0 are formed against 0.  rest: NULL, or what the rounding to bf16 left of them (p and
 // rest together hold 16 bits).
 template <bool HALF>
 __device__ __forceinline__ float probabilities(float m, const f16v& s, float c, float bias, u4v (&p)[2],
-                                               u4v* rest = nullptr) {
-  const float ref = (m == -INFINITY ? 0.0f : m) - bias;
+                                               float drop, u4v* rest = nullptr) {
+  const float ref = (m == -INFINITY ? 0.0f : m) - (bias - drop);
   float sum = 0.0f;
 #pragma unroll
   for (int x = 0; x < 2; ++x)
@@ -119,11 +123,11 @@ __device__ __forceinline__ float probabilities(float m, const f16v& s, float c, 
     }
   return sum;
 }
-// One online-softmax step over a subtile.
+// One online-softmax step over a subtile; grow = 2^drop.
 template <int NM, bool HALF>
 __device__ __forceinline__ void softmax_step(RowState<NM>& st, const f16v& s, float c, float bias, u4v (&p)[2],
-                                             u4v* rest = nullptr) {
-  const float mx = top_logit(s, c);
+                                             u4v* rest = nullptr, float drop = 0.0f, float grow = 1.0f) {
+  const float mx = top_logit(s, c, drop);
   if (__any(mx > st.m + kSlack)) {
     const float mnew = fmaxf(st.m, mx), alpha = rescale(st.m, mnew);
     st.m = mnew;
@@ -131,7 +135,7 @@ __device__ __forceinline__ void softmax_step(RowState<NM>& st, const f16v& s, fl
 #pragma unroll
     for (int i = 0; i < NM; ++i) st.o[i] *= alpha;
   }
-  st.l += probabilities<HALF>(st.m, s, c, bias, p, rest);
+  st.l += grow * probabilities<HALF>(st.m, s, c, bias, p, drop, rest);
 }
 
 // Whether any of the eight bf16 / fp16 values of a 16-byte unit is infinite or NaN.
@@ -166,9 +170,9 @@ __device__ __forceinline__ u4v only_finite(u4v w) {
 // not see element e, else 0.  Rare.
 template <int NM, bool HALF, class Unit, class Hidden>
 __device__ __forceinline__ float take_nonfinite(RowState<NM>& st, float m, const f16v& s, float c, float bias, Unit unit,
-                                                Hidden hidden) {
+                                                Hidden hidden, float drop = 0.0f) {
   constexpr uint32_t kOne = HALF ? 0x3c00u : 0x3f80u, kExp = HALF ? 0x7c00u : 0x7f80u;
-  const float mx = top_logit(s, c);
+  const float mx = top_logit(s, c, drop);
   if (__any(mx > m + kSlack)) {
     const float mnew = fmaxf(m, mx), alpha = rescale(m, mnew);
     if (__any(alpha == 0.0f)) {  // now: after what is added here it would make NaN of it
@@ -180,7 +184,7 @@ __device__ __forceinline__ float take_nonfinite(RowState<NM>& st, float m, const
     m = mnew;
   }
   u4v p[2];
-  probabilities<HALF>(m, s, c, bias, p);
+  probabilities<HALF>(m, s, c, bias, p, drop);
 #pragma unroll 1
   for (int kind = 0; kind < 4; ++kind) {  // +infinity and -infinity (p > 0), NaN, either infinity (p = 0)
     asm volatile("" ::: "memory");  // (units read again for each kind, not held in registers)

@@ -1,6 +1,6 @@
 """The multi-token operators at the edges of what they accept: infinite values at visible
 tokens, with and without mass, small values and queries, and group scales halfway between two
-fp16 values.
+fp16 values.  Tolerances as in test_gpu_operators.py.
 """
 import math
 
@@ -9,7 +9,7 @@ import torch
 
 from paper_2609_37988_amd import kvk
 from gpu_common import DEV
-from test_gpu_operators import Streams, _check_chunk, _prompt_inputs, _run_chunk, _run_prompt
+from test_gpu_operators import Streams, _attend, _check, _gen, _prompt_inputs, _randn, _run_chunk, _run_prompt
 
 pytestmark = pytest.mark.gpu
 NAN = float("nan")
@@ -66,7 +66,7 @@ def test_chunk_infinite_values_agree(hq, d, score, want):
     n, t = 430, 150
     for start, m, at in ((0, n, t), (n - 5, 5, t), (n - 12, 12, 425)):
         c = Streams([(0, 16)], hq, 1, d, 1, n, kvk.KIVI32, seed=31)
-        q = torch.randn(1, 1, hq, m, d, device=DEV).bfloat16()
+        q = _randn(_gen(40), 1, 1, hq, m, d).bfloat16()
         _spoil(q, c.k, c.v, at, score)
         c.append([0], [n])
         _, out = _run_chunk(c, 0, 1, [n], [m], SCALE, q=q)
@@ -82,7 +82,7 @@ def test_chunk_infinite_values_agree(hq, d, score, want):
 def test_chunk_infinite_values_in_the_window_of_a_quantised_layer(hq, d, score, want):
     n, m, at = 430, 12, 425
     c = Streams([(0, 4)], hq, 1, d, 1, n, kvk.KIVI32, seed=36)
-    q = torch.randn(1, 1, hq, m, d, device=DEV).bfloat16()
+    q = _randn(_gen(40), 1, 1, hq, m, d).bfloat16()
     _spoil(q, c.k, c.v, at, score)
     c.append([0], [n])
     _, out = _run_chunk(c, 0, 1, [n], [m], SCALE, q=q)
@@ -100,6 +100,38 @@ STORED = [1, 20, 33, 64, 129, 200, 517, 97]
 NEW = [[1] * 8, [1, 20, 33, 4, 6, 7, 3, 1], [1, 11, 20, 33, 60, 100, 0, 40]]
 
 
+def _check_rows(c, stored, new, scale, q, out, held=None):
+    """The outputs of layer 0 with the tolerance of test_gpu_operators.py and what it leaves out:
+    probabilities beneath fp16's normal range (quantised layers).  A row's largest probability
+    enters the product as 2^7 or more and fp16 rounds small ones by at most 2^-25, so each
+    probability is off by at most 2^-32 of the largest.  SYMROW scales the values of 32 tokens by
+    the power of two of their largest scale, and the probabilities against it: there 2^-32 of the
+    largest product of a probability and its group's scale, here 2^-31 of that with the
+    group's largest value (a scale is between it and half of it, times a constant).  held: tokens
+    in the cache, where they are more than the rows' (which groups are complete goes by them)."""
+    grp = c.hq // c.hkv
+    for b, (n, m) in enumerate(zip(stored, new)):
+        assert (out[:, b, :, m:] == 7.0).all(), "rows past the new tokens"
+        last = torch.arange(n - m, n, device=DEV)
+        for h in range(c.hkv if m else 0):
+            K, V, bits = c.values(0, b, h, held or n)
+            K, V = K[:n], V[:n]
+            rows = q[0, b, h * grp:(h + 1) * grp, :m]
+            err = (0.0, 2.0**-8, 0.0) if bits == 16 else (2.0**-11, 2.0**-11, 2.0**-11)
+            o, lse, tol, _ = _attend(rows, K, V, scale, last, *err)
+            if bits != 16:
+                top = V.abs().amax(-1)
+                top = torch.cat([x.amax().clamp(min=1e-30).expand(x.numel()) for x in top.split(32)])
+                if c.dims.qscheme != kvk.SYMROW:
+                    top = torch.ones_like(top)
+                p = torch.exp((rows.double() @ K.double().t()) * scale - lse[..., None])
+                seen = torch.arange(n, device=DEV) <= last[:, None]
+                p = torch.where(seen, p, torch.zeros_like(p))
+                off = seen.double() @ (V.abs().double() / top[:, None])  # [rows, channels]
+                tol = tol + 2.0**-31 * (p * top).amax(-1, keepdim=True) * off
+            _check(out[0, b, h * grp:(h + 1) * grp, :m], o, tol, f"sequence {b} head {h}")
+
+
 def _small(scheme, d, bits, hq, kv, qf):
     """Keys and values scaled by kv, queries by qf, the softmax scale to match."""
     c = Streams([(0, bits)], hq, 1, d, 8, 520, scheme, seed=32)
@@ -107,9 +139,9 @@ def _small(scheme, d, bits, hq, kv, qf):
     c.append([0] * 8, STORED)
     scale = 0.8 / math.sqrt(d) / (kv * qf)
     for new in NEW:
-        q = (torch.randn(1, 8, hq, max(new), d, device=DEV) * qf).bfloat16()
+        q = (_randn(_gen(41), 1, 8, hq, max(new), d) * qf).bfloat16()
         _, out = _run_chunk(c, 0, 1, STORED, new, scale, q=q)
-        _check_chunk(c, 0, 1, STORED, new, scale, q, out)
+        _check_rows(c, STORED, new, scale, q, out)
 
 
 @pytest.mark.parametrize("scheme", [kvk.KIVI32, kvk.GROUP64])
@@ -119,6 +151,74 @@ def _small(scheme, d, bits, hq, kv, qf):
 def test_chunk_small_values(kv, qf, d, hq, bits, scheme):
     """Values and queries below fp16's normal range, in full blocks and in the window."""
     _small(scheme, d, bits, hq, kv, qf)
+
+
+@pytest.mark.parametrize("bits", [8, 4, 2])
+@pytest.mark.parametrize("d,hq", [(64, 64), (128, 5)])
+@pytest.mark.parametrize("kv,qf", [(2.0**-12, 1.0), (2.0**-18, 1.0), (2.0**-40, 2.0**-10), (2.0**12, 1.0)])
+def test_chunk_small_symrow_values(kv, qf, d, hq, bits):
+    """The same where a row's scale is bf16, which reaches further than fp16."""
+    _small(kvk.SYMROW, d, bits, hq, kv, qf)
+
+
+@pytest.mark.parametrize("bits", [8, 4, 2])
+@pytest.mark.parametrize("d,hq", [(64, 64), (128, 5), (128, 30)])
+def test_chunk_symrow_values_of_many_sizes(d, hq, bits):
+    """Tokens whose values, and whose keys, differ by up to 2^16 from one to the next and by 2^20
+    from one group to the next; contexts in one piece and split."""
+    cap = 3000
+    c = Streams([(0, bits)], hq, 1, d, 2, cap, kvk.SYMROW, seed=33)
+    g = _gen(34)
+    for x, top in ((c.k, 1.0), (c.v, 1.0)):
+        per_token = torch.exp2(-16 * torch.rand(1, 2, 1, cap, 1, generator=g, device=DEV))
+        per_group = torch.exp2(-20 * torch.rand(1, 2, 1, cap // 30, 1, generator=g, device=DEV)).repeat_interleave(32, 3)[:, :, :, :cap]
+        x.copy_(x.float() * per_token * per_group)
+    c.k[:, :, :, ::7] = (c.k[:, :, :, ::7].float() * 2.0**10).bfloat16()
+    stored = [2990, 96]
+    c.append([0, 0], stored)
+    for new in ([1, 96], [7, 40], [33, 1]):
+        q, out = _run_chunk(c, 0, 1, stored, new, 0.1)
+        _check_rows(c, stored, new, 0.1, q, out)
+
+
+@pytest.mark.parametrize("bits", [8, 4, 2])
+@pytest.mark.parametrize("d,hq", [(64, 64), (128, 5), (128, 20)])
+def test_chunk_symrow_infinite_token(d, hq, bits):
+    """A token with infinities has an infinite scale: its group's earlier tokens, and their rows, do
+    not notice; the rows that see it are NaN."""
+    n, t = 70, 40
+    c = Streams([(0, bits)], hq, 1, d, 1, n, kvk.SYMROW, seed=37)
+    c.k[..., t, 3], c.v[..., t, 4] = math.inf, -math.inf
+    c.append([0], [n])
+    q, out = _run_chunk(c, 0, 1, [n], [n], 0.1)
+    assert torch.isnan(out[..., t:, :]).all()
+    c.k[..., t, 3], c.v[..., t, 4] = 0.0, 0.0  # (hidden from the rows before it)
+    _check_rows(c, [t], [t], 0.1, q[..., :t, :].contiguous(), out[..., :t, :].contiguous(), held=n)
+
+
+@pytest.mark.parametrize("scheme", [kvk.SYMROW, kvk.GROUP64])
+@pytest.mark.parametrize("bits", [8, 4, 2])
+def test_chunk_one_token_matches_decode_element_by_element(bits, scheme):
+    """The decode step rounds less than what the tolerance of a chunk's row counts (codes are exact
+    in its products), but GROUP64's codes and zeros enter apart: each of the two is at most twice
+    the group's largest value."""
+    hq, d, n = 10, 128, 333
+    c = Streams([(0, bits)], hq, 2, d, 2, 400, scheme, seed=17)
+    c.append([0, 0], [n, n])
+    q, out = _run_chunk(c, 0, 1, [n, n], [1, 1], 0.09)
+    ws = torch.empty(kvk.workspace_bytes(c.t, 0, 1), dtype=torch.uint8, device=DEV)
+    dec = torch.empty((1, 2, hq, d), dtype=torch.float32, device=DEV)
+    kvk.decode_attention(c.t, 0, 1, q[:, :, :, 0].contiguous(), n, 0.09, c.arena, dec, ws)
+    last = torch.tensor([n - 1], device=DEV)
+    for b in range(2):
+        for h in range(2):
+            rows = slice(5 * h, 5 * h + 5)
+            K, V, _ = c.values(0, b, h, n)
+            o, _, tol, _ = _attend(q[0, b, rows], K, V, 0.09, last, 2.0**-11, 2.0**-11, 2.0**-11)
+            wide = V.abs().reshape(n, d // 64, 64).amax(-1, keepdim=True).expand(n, d // 64, 64).reshape(n, d)
+            _, _, more, _ = _attend(q[0, b, rows], K, 4 * wide, 0.09, last, 2.0**-11, 2.0**-11, 2.0**-11)
+            _check(out[0, b, rows], o, tol, "chunk")
+            _check(dec[0, b, rows][:, None], o, tol + (more if scheme == kvk.GROUP64 else 0), "decode")
 
 
 # --------------------------------------------------------------------------------------
