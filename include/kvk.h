@@ -400,6 +400,11 @@ kvk_status kvk_append_token(const kvk_table* table, int32_t layer_begin, int32_t
  *              the tails are written.  Tail slots past the last token are left undefined.
  * Sequences of different lengths: at most KVK_MAX_BATCH_PLANS (any number of equal ones).  The
  * host arrays are read before the call returns.
+ * Taking tokens back (rejected drafts), to S stored tokens of a sequence: while S / 32 full blocks
+ * are all there are, later calls just pass S; the slots past it count for nothing.  Where a later
+ * block has been completed since, the tokens S / 32 * 32 .. S - 1 are bf16 nowhere in the arena
+ * any more: append them again, n_stored = S / 32 * 32 and n_new = S % 32, which writes the tail
+ * alone.  A caller who takes tokens back therefore keeps the keys and values of the last 31.
  * Errors: KVK_ERR_INVALID (range, lengths, NULL pointers, dtype, misalignment: k, v and arena
  *         16 B, host memory), KVK_ERR_UNSUPPORTED (MLA table: kvk_append_token; sequences of
  *         different lengths beyond the limit), KVK_ERR_DEVICE. */
@@ -687,7 +692,11 @@ kvk_status kvk_decode_attention_noalloc(const kvk_table* table, int32_t layer_be
  * with one token each, decoding of sequences of different lengths.  Row i of the n_new[b] rows
  * of sequence b is its stored token n_stored[b] - n_new[b] + i and attends to the stored tokens
  * up to itself, as they are stored: a token whose 32-token group is complete in its quantised
- * form, for the group's own rows too.  Layers of [layer_begin, layer_end) that share an anchor
+ * form, for the group's own rows too.  Where token-by-token decoding would still read such a
+ * group in bf16 (rows before its last token), the two differ by the quantisation, and KIVI32's
+ * keys, whose scale and zero are one per channel of the group, let a later token of the group (a
+ * draft that may yet be rejected) into the form of an earlier one.  A chunk that ends before
+ * the last token of a group, which then goes by itself, gives the token-by-token results.  Layers of [layer_begin, layer_end) that share an anchor
  * are served by one read of it.
  *   q        : device bf16 [layer_end-layer_begin][B][Hq][n_chunk][d_h]; n_chunk 1..capacity.
  *   n_stored : host [B], tokens stored per stream of each sequence, the chunk among them.
@@ -702,7 +711,7 @@ kvk_status kvk_decode_attention_noalloc(const kvk_table* table, int32_t layer_be
  * group (exact to fp16's 2^-11 from 2^-60 to 2^60, for tokens whose scale is at least 2^-24 of the
  * group's largest).  The queries and the window are any bf16.
  * Scores, sums and outputs are accumulated in fp32.  Tokens a row does not see (and stale slots) do not reach it,
- * infinities and NaN among them; infinite values at visible tokens count as in
+ * infinities and NaN among them, but through that scale and zero of KIVI32's keys; infinite values at visible tokens count as in
  * kvk_prompt_attention.  The host arrays are read before the call returns.
  * Errors: KVK_ERR_INVALID (range, lengths, scale, NULL pointers, misalignment: q, arena and out
  *         16 B, workspace 256 B; host memory), KVK_ERR_UNSUPPORTED (MLA table; a batch beyond

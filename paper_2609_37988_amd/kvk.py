@@ -651,7 +651,9 @@ def append_chunk(t: Table, layer_begin: int, layer_end: int, k: torch.Tensor, v:
                  arena: torch.Tensor, stream=None):
     """Append a chunk of new tokens to every anchor in [layer_begin, layer_end).  k, v
     [layers, B, Hkv, chunk, d_h], contiguous bf16/fp32; n_stored (before the call) and n_new
-    (None: the whole chunk): one length, or one per sequence, on the host."""
+    (None: the whole chunk): one length, or one per sequence, on the host.  Tokens are taken back
+    by passing fewer stored ones; into a group completed since, by appending the group's kept
+    tokens again from its start (see kvk.h)."""
     d = t.dims
     shape = k.shape
     if k.dtype != v.dtype or not k.is_contiguous() or not v.is_contiguous() or len(shape) != 5 or shape != v.shape:

@@ -1,6 +1,6 @@
 """The multi-token operators at the edges of what they accept: infinite values at visible
-tokens, with and without mass, small values and queries, and group scales halfway between two
-fp16 values.  Tolerances as in test_gpu_operators.py.
+tokens, with and without mass, small values and queries, drafts that are taken back or complete
+a group, and group scales halfway between two fp16 values.  Tolerances as in test_gpu_operators.py.
 """
 import math
 
@@ -9,7 +9,7 @@ import torch
 
 from paper_2609_37988_amd import kvk
 from gpu_common import DEV
-from test_gpu_operators import Streams, _attend, _check, _gen, _prompt_inputs, _randn, _run_chunk, _run_prompt
+from test_gpu_operators import Streams, _attend, _check, _gen, _prompt_inputs, _randn, _run_chunk, _run_prompt, _same
 
 pytestmark = pytest.mark.gpu
 NAN = float("nan")
@@ -219,6 +219,84 @@ def test_chunk_one_token_matches_decode_element_by_element(bits, scheme):
             _, _, more, _ = _attend(q[0, b, rows], K, 4 * wide, 0.09, last, 2.0**-11, 2.0**-11, 2.0**-11)
             _check(out[0, b, rows], o, tol, "chunk")
             _check(dec[0, b, rows][:, None], o, tol + (more if scheme == kvk.GROUP64 else 0), "decode")
+
+
+# --------------------------------------------------------------------------------------
+# Drafts: taken back, and in a group that they complete
+# --------------------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("scheme", [kvk.KIVI32, kvk.SYMROW, kvk.GROUP64])
+@pytest.mark.parametrize("d", [64, 128])
+def test_chunk_drafts_taken_back(d, scheme):
+    """Sequences whose drafts are rejected in part, inside a group and after completing one (or
+    two): the streams go on as those that never held the drafts."""
+    L, B, hkv = 3, 5, 2
+    plan = [(0, 16), (0, 8), (0, 2)]
+    c = Streams(plan, 4, hkv, d, B, 200, scheme, seed=38)
+    never = c.new_arena()
+    start, drafts, kept = [60, 62, 30, 64, 5], [3, 6, 70, 4, 20], [1, 1, 1, 0, 20]
+    c.append([0] * B, start)
+    c.append([0] * B, start, arena=never)
+    other = Streams(plan, 4, hkv, d, B, 200, scheme, seed=39)  # rejected tokens: other values after the kept ones
+    for b in range(B):
+        at = start[b] + kept[b]
+        other.k[:, b, :, :at], other.v[:, b, :, :at] = c.k[:, b, :, :at], c.v[:, b, :, :at]
+    other.append(start, drafts, arena=c.arena)
+    now = [s + n for s, n in zip(start, kept)]
+    again = [n % 32 if n // 32 < (s + m) // 32 else 0 for n, s, m in zip(now, start, drafts)]
+    assert again == [0, 31, 31, 0, 0]
+    c.append([n // 32 * 32 if a else n for n, a in zip(now, again)], again)
+    c.append(start, kept, arena=never)
+    _same(c.streams(c.arena, now), c.streams(never, now))
+    for l in (0, 2):
+        q, out = _run_chunk(c, l, l + 1, now, [5, 3, 1, 2, 7], 0.1)
+        c.arena, never = never, c.arena
+        _, ref = _run_chunk(c, l, l + 1, now, [5, 3, 1, 2, 7], 0.1, q=q)
+        c.arena, never = never, c.arena
+        assert torch.equal(out, ref)
+    more = [40, 1, 5, 33, 64]
+    c.append(now, more)
+    c.append(now, more, arena=never)
+    now = [n + m for n, m in zip(now, more)]
+    _same(c.streams(c.arena, now), c.streams(never, now))
+
+
+@pytest.mark.parametrize("scheme", [kvk.KIVI32, kvk.SYMROW, kvk.GROUP64])
+@pytest.mark.parametrize("bits", [8, 4, 2])
+@pytest.mark.parametrize("d,hq", [(64, 64), (128, 5)])
+def test_chunk_rows_of_a_completed_group_with_a_late_outlier(d, hq, bits, scheme):
+    """Rows of a group that the chunk completes attend to its quantised form, whose scales a later
+    token of it may have set."""
+    c = Streams([(0, bits)], hq, 1, d, 2, 100, scheme, seed=42)
+    for x in (c.k, c.v):
+        x[:, 0, :, 60] *= 50.0
+        x[:, 1, :, 31] *= 50.0
+    stored, new = [64, 40], [20, 40]
+    c.append([0, 0], [44, 0])
+    c.append([44, 0], new)
+    q, out = _run_chunk(c, 0, 1, stored, new, 0.02)
+    _check_rows(c, stored, new, 0.02, q, out)
+
+
+@pytest.mark.parametrize("scheme,keys", [(kvk.KIVI32, False), (kvk.GROUP64, True)])
+@pytest.mark.parametrize("bits", [8, 4, 2])
+@pytest.mark.parametrize("d,hq", [(64, 64), (128, 5), (128, 20)])
+def test_chunk_infinite_token_of_a_group(d, hq, bits, scheme, keys):
+    """As for SYMROW, where the scales are each token's own: GROUP64, and the values of KIVI32."""
+    n, t = 70, 40
+    c = Streams([(0, bits)], hq, 1, d, 1, n, scheme, seed=43)
+    c.v[..., t, 4] = math.inf
+    if keys:
+        c.k[..., t, 3] = math.inf
+    c.append([0], [n])
+    q, out = _run_chunk(c, 0, 1, [n], [n], 0.1)
+    group = slice(0, 32 if scheme == kvk.KIVI32 else 64)  # the channels that share the infinite scale
+    assert not torch.isfinite(out[..., t:, group]).any()
+    c.v[..., t, 4] = 0.0
+    if keys:
+        c.k[..., t, 3] = 0.0
+    _check_rows(c, [t], [t], 0.1, q[..., :t, :].contiguous(), out[..., :t, :].contiguous(), held=n)
 
 
 # --------------------------------------------------------------------------------------
