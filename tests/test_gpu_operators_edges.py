@@ -1,14 +1,17 @@
 """The multi-token operators at the edges of what they accept: infinite values at visible
 tokens, with and without mass, small values and queries, drafts that are taken back or complete
-a group, and group scales halfway between two fp16 values.  Tolerances as in test_gpu_operators.py.
+a group, group scales halfway between two fp16 values, launches of many sequences, repeated inputs
+and captured calls of the long forms.  Tolerances as in test_gpu_operators.py.
 """
 import math
 
+import numpy as np
 import pytest
 import torch
 
 from paper_2609_37988_amd import kvk
 from gpu_common import DEV
+import test_gpu_operators as base
 from test_gpu_operators import Streams, _attend, _check, _gen, _prompt_inputs, _randn, _run_chunk, _run_prompt, _same
 
 pytestmark = pytest.mark.gpu
@@ -347,3 +350,98 @@ def test_group_scales_round_twice_as_documented(scheme, d, bits):
         for g, w, name in zip(got, want, "kv"):
             wrong = (g[0, 0] != w.float()).sum()
             assert wrong == 0, f"{write}: {int(wrong)} of {n * d} {name} values differ"
+
+
+# --------------------------------------------------------------------------------------
+# Launches of many sequences, long prompts, repeated inputs, unlike row counts
+# --------------------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("d,hq,hkv", [(64, 2, 1), (128, 3, 3)])
+@pytest.mark.parametrize("count", [65, 128, 256])
+def test_prompt_and_weight_many_sequences(count, d, hq, hkv):
+    """More sequences than a wave has lanes, up to the limit, of lengths that repeat and end
+    inside blocks of either kernel, empty ones among them."""
+    rng = np.random.default_rng(count)
+    lens = [int(x) for x in rng.choice([0, 1, 17, 64, 127, 128, 129, 256, 257, 300], count)]
+    base.test_prompt_attention(lens, hq, hkv, d, "packed")
+    base.test_attention_weight(lens, hq, hkv, d, "packed")
+
+
+@pytest.mark.parametrize("lens,hq,hkv,d", [([5003], 2, 1, 64), ([2049, 4100], 3, 1, 128)])
+def test_prompt_and_weight_long(lens, hq, hkv, d):
+    base.test_prompt_attention(lens, hq, hkv, d, "fused")
+    base.test_attention_weight(lens, hq, hkv, d, "padded")
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_prompt_repeated_inputs(d):
+    """Heads, and tokens, that share one place (strides of 0), without the log-sum-exps."""
+    lens, scale = [150, 33], 0.2
+    q, k, v = _prompt_inputs(44, lens, 4, 2, d, "packed")
+    k, v = k[:, :1].expand(-1, 2, -1), v[:, 1:].expand(-1, 2, -1)
+    q = q[5:6].expand(183, -1, -1)
+    out, lse = _run_prompt(q, k, v, lens, scale)
+    base._check_prompt(q, k, v, lens, scale, out, lse)
+    again = torch.full_like(out, NAN)
+    kvk.prompt_attention(q, k, v, lens, scale, again)
+    assert torch.equal(out, again)
+
+
+@pytest.mark.parametrize("scheme", [kvk.KIVI32, kvk.SYMROW])
+def test_chunk_of_a_prompt_beside_single_tokens(scheme):
+    """One long chunk sets the launch's row blocks; the other sequences have one row per head, or
+    a few, or none."""
+    stored = [1500] + [1, 700, 32, 64, 95, 1024, 5, 333, 64, 31]
+    new = [600] + [1, 1, 1, 4, 2, 1, 5, 1, 0, 31]
+    c = Streams([(0, 8)], 5, 1, 128, len(stored), 1500, scheme, seed=45)
+    c.append([0] * len(stored), stored)
+    q, out = _run_chunk(c, 0, 1, stored, new, 0.08)
+    _check_rows(c, stored, new, 0.08, q, out)
+
+
+def test_keep_heaviest_long_and_all_recent():
+    n, keep = 40000, 333
+    t = kvk.layer_table(kvk.make_dims(kvk.GQA, 1, 2, 2, 64, batch=1, max_tokens=n, keep_tokens=keep), kvk.make_plan([(0, 8)]))
+    out = torch.full((1, 2, keep), -1, dtype=torch.int32, device=DEV)
+    kvk.keep_heaviest(t, torch.rand(1, 2, n, device=DEV), n, keep, out)
+    assert torch.equal(out, torch.arange(n - keep, n, dtype=torch.int32, device=DEV).expand(1, 2, keep))
+
+
+def test_long_forms_captured():
+    """The keep list of a long prompt and a chunk whose context is split, captured into one graph
+    with workspaces of their own and replayed on new inputs, eager calls in between."""
+    B, hq, hkv, d, n, keep = 2, 4, 2, 128, 20000, 5000
+    c = Streams([(0, 4), (1, 4)], hq, hkv, d, B, n, kvk.KIVI32, seed=46)
+    stored, new = [19990, 7001], [3, 2]
+    c.append([0, 0], stored)
+    dims = kvk.make_dims(kvk.GQA, 1, hq, hkv, d, batch=B, max_tokens=n, keep_tokens=keep)
+    te = kvk.layer_table(dims, kvk.make_plan([(0, 8)]))
+    g = _gen(47)
+    w, q = _randn(g, B, hkv, n).exp(), _randn(g, 2, B, hq, 3, d).bfloat16()
+    idx = torch.full((B, hkv, keep), -1, dtype=torch.int32, device=DEV)
+    out = torch.full(q.shape, 7.0, dtype=torch.bfloat16, device=DEV)
+    ws = torch.full((kvk.chunk_workspace_bytes(c.t, 0, 2, 3),), 0xFF, dtype=torch.uint8, device=DEV)
+    kws = torch.full((kvk.keep_workspace_bytes(te, n),), 0xFF, dtype=torch.uint8, device=DEV)
+    assert kws.numel() > 0 and ws.numel() > 256
+
+    def path():
+        kvk.keep_heaviest(te, w, n, 32, idx, kws)
+        kvk.chunk_attention(c.t, 0, 2, q, stored, new, 0.09, c.arena, out, ws)
+
+    path()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        path()
+    for _ in range(3):
+        w.copy_(_randn(g, *w.shape).exp()), q.copy_(_randn(g, *q.shape))
+        path()
+        eager = idx.clone(), out.clone()
+        idx.fill_(-1), out.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(idx, eager[0]) and torch.equal(out, eager[1])
+        assert np.array_equal(idx.cpu().numpy().reshape(-1, keep), base._keep_ref(w.cpu().numpy(), keep, 32))
+        assert (out[:, 1, :, 2:] == 7.0).all()
+    base._check_chunk(c, 0, 2, stored, new, 0.09, q, out)
