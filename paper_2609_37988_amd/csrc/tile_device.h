@@ -176,10 +176,11 @@ __device__ __forceinline__ float take_nonfinite(RowState<NM>& st, float m, const
   if (__any(mx > m + kSlack)) {
     const float mnew = fmaxf(m, mx), alpha = rescale(m, mnew);
     if (__any(alpha == 0.0f)) {  // now: after what is added here it would make NaN of it
+      const float before = rescale(st.m, m);  // of the subtiles before, whose steps are yet to come
       st.m = mnew;
-      st.l *= alpha;
+      st.l = st.l * before * alpha;
 #pragma unroll
-      for (int i = 0; i < NM; ++i) st.o[i] *= alpha;
+      for (int i = 0; i < NM; ++i) st.o[i] = st.o[i] * before * alpha;
     }
     m = mnew;
   }

@@ -79,6 +79,32 @@ def test_chunk_infinite_values_agree(hq, d, score, want):
         _check_spoilt(out[0, 0].transpose(0, 1), ref[0, 0].transpose(0, 1), max(at - start, 0), want)
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("hq", [3, 20])
+@pytest.mark.parametrize("first", [0.0, 20.0, 60.0])
+def test_chunk_infinite_values_after_two_jumps(first, hq, d):
+    """A partly seen tile whose first half raises the rows' logits a little and whose second one by
+    more than fp32's range, for some rows of a wave."""
+    n, low, t = 430, 200, 240  # (the second tile of its split)
+    c = Streams([(0, 16)], hq, 1, d, 1, n, kvk.KIVI32, seed=48)
+    q = _randn(_gen(49), 1, 1, hq, n, d).bfloat16()
+    _spoil(q, c.k, c.v, t, 400.0)
+    c.k[..., low, :] = 0.0
+    c.k[..., low, 0] = first / SCALE
+    c.append([0], [n])
+    _, out = _run_chunk(c, 0, 1, [n], [n], SCALE, q=q)
+    c.v[..., t, 5:8] = 0.0
+    c.append([0], [n])
+    _, ref = _run_chunk(c, 0, 1, [n], [n], SCALE, q=q)
+    # the reference maximum moves earlier for the wave's other rows: rounding, not bits (each side
+    # is off by its own rounding and the probabilities', 2^-8 of the largest value each)
+    _check_rows(c, [n], [n], SCALE, q, ref)
+    clean = [x for x in range(d) if x not in (5, 6, 7)]
+    assert ((out - ref).abs()[..., clean] <= 2.0**-6 * c.v.abs().max()).all()
+    assert (out[0, 0, :, t:, 5] == math.inf).all() and (out[0, 0, :, t:, 6] == -math.inf).all()
+    assert torch.isnan(out[0, 0, :, t:, 7]).all() and torch.isfinite(out[0, 0, :, :t]).all()
+
+
 @pytest.mark.parametrize("score,want", SCORES)
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("hq", [3, 20, 64])
