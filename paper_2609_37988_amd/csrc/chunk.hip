@@ -8,27 +8,30 @@
 // One workgroup of four waves (eight for WR = 8) takes 32 WR rows and a range of the context,
 // in tiles of TB 32-token blocks.  All waves dequantise a tile into LDS, once, in the operand
 // order that the arena's layout has already (16-byte units of eight values), bf16 for 16-bit
-// layers and fp16 for quantised ones; then wave (wr, wt) attends with row group wr to the tile's wt-th share of
-// the tokens.  Many rows: WR = 4 or 8, every wave reads the whole tile.  Few rows (a draft, single
-// tokens): WR = 1, the waves share the tokens, and their states meet in LDS at the end.  Where
-// the rows alone leave the GPU idle the context is split over workgroups too; chunk_merge_kernel
-// joins the partial results.
+// layers and fp16 for quantised ones; then wave (wr, wt) attends with row group wr to the tile's
+// wt-th share of the tokens.  Many rows: WR = 4 or 8, every wave reads the whole tile.  Few rows (a
+// draft, single tokens): WR = 1, the waves share the tokens, and their states meet in LDS at the
+// end.  The bf16 window comes last, as one block of its own.  Where the rows alone leave the GPU
+// idle the context is split over workgroups too; chunk_merge_kernel joins the partial results.
 //
 // Precision: in quantised layers fp16 holds a dequantised value to 2^-11 relative (bf16 would to
 // 2^-8; SYMROW's blocks are scaled by a power of two each, as their bf16 scales reach further than
-// fp16: see Part::lift), the queries (bf16, each row scaled by a power of two) exactly, and the probabilities, kept
-// between 2^-24 and 2^15, to 2^-11; the bf16 window meets bf16 queries and probabilities in two
-// bf16 parts.  In 16-bit layers keys, values and queries are exact and the probabilities bf16, to
-// 2^-8: fp16 would lose small and large values.  Scores, sums and partial outputs are fp32, the
-// outputs are rounded once, to bf16.
+// fp16: see Part::lift), the queries (bf16, each row scaled by a power of two) exactly, and the
+// probabilities, kept between 2^-24 and 2^15, to 2^-11; the window's probabilities enter as two
+// bf16 parts, 16 bits.  In 16-bit layers keys, values and queries are exact and the probabilities
+// bf16, to 2^-8: fp16 would lose small and large values.  Scores, sums and partial outputs are
+// fp32, the outputs are rounded once, to bf16.
 //
 // Bound.  Few rows: the latency of a tile after another (8 ragged sequences up to 7000 tokens,
-// one new token each, int4, 32 streams: 17 us for two tiles each, merge 7).  A draft of 40 rows per
-// stream: the caches' bytes and the dequantisation (256 streams of 8192 tokens, int8: 142 us
-// for 604 MB; the loads alone take 100 to 110; two tiles in flight, three workgroups per CU or
-// tiles of four blocks for two row groups were slower, by spills).  Many rows: as
-// prompt_kernel, power and issue, with the dequantisation on top (2048 new of 12345 tokens, 40 /
-// 8 heads, int4: 565 us with its merge, 840 TFLOP/s).
+// one new token each, int4, 32 streams: 15 us for two tiles each, merge 7).  A draft of 40 rows per
+// stream: the dequantisation beside the caches' loads (256 streams of 8192 tokens, int8: 145 us
+// for 604 MB, 4.2 TB/s; vector units active 40 %, matrix units 21 %, LDS 33 %, a wave waits for
+// data 37 % of its time; two tiles in flight, three workgroups per CU or tiles of four blocks for two
+// row groups were slower, as built with spills).  Many rows: the chain of a step as in
+// prompt_kernel, with the dequantisation before it and one workgroup per CU (2048 new of 12345
+// tokens, 40 / 8 heads, int4: 558 us with its merge, 850 TFLOP/s; matrix units busy 38 %, vector
+// units 45 %, a wave waits for data 39 % of its time, for issue 25 %).  SYMROW's powers of two cost
+// 6 % there (int8, 583 us) and 2 % in the draft.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>

@@ -840,8 +840,9 @@ static_assert(sizeof(ChunkWriteArgs) <= 4096, "kernel arguments");
 // from its bf16 tokens, the first one's from the tail and the chunk together; its wave also
 // writes what is left over to the tail, after it has read it.  A chunk that stays in the tail
 // only adds its tokens to it.
-// Bound: the chain of one wave where blocks are few (4 tokens, 32 sequences of 8 KV heads, 4
-// layers: 5.4 us), else HBM (1000 tokens, 4 sequences, 2 layers: 16 to 18 us for 47 MB).
+// Bound: the chain of one wave from its loads to its stores, also where it is a round of 16 waves
+// per CU (4 tokens, 32 sequences of 8 KV heads, 4 layers: 4.8 us; 1000 tokens, 4 sequences, 2
+// layers: 17.5 us for 47 MB, 2.7 TB/s, where a copy reaches 4.7).
 template <int D, int QS>
 __global__ __launch_bounds__(128) void chunk_write_kernel(ChunkWriteArgs a) {
   using L = Lanes<D>;

@@ -10,9 +10,10 @@
 //                      slice's histogram, and one that writes the lists.  (One workgroup per
 //                      stream that reads its keys again for every digit is bound by that CU's
 //                      vector instructions: 32 streams of 131072 positions 127 us, sliced 38.)
-// Bound: latency.  8 streams of 1024 positions take 6.5 us, 4 of it the launch.  Of the 38 the four
-// launches take 8 to 13 each: the keys' loads (from the caches after the first), a histogram in
-// LDS, and the sum of the slices' histograms, which every slice forms for itself.  Slices of half
+// Bound: latency.  8 streams of 1024 positions take 6.5 us, 4 of it the launch.  The four launches
+// of the long list take 7.5, 9.5, 9.5 and 12.7 us in a kernel trace (38.5 in all without one): the
+// keys' loads (from the caches after the first), a histogram in LDS, and the sum of the slices'
+// histograms, which every slice forms for itself.  Slices of half
 // the size have twice as many of those to read (45 us), of twice the size leave CUs idle (42).
 #include <hip/hip_runtime.h>
 

@@ -172,13 +172,14 @@ struct Stage {
 // product in bf16 (2^-8 relative each, of either sign), the type of the values, and the
 // outputs are rounded to bf16 once.
 //
-// Bound: power, then issue.  With both matrix and vector units busy the clock falls to about 1.9
-// GHz; 40 / 8 heads of 128 over 8192 tokens take 730 us (940 TFLOP/s; an 8192-wide bf16 library
-// product reaches 1400 to 1550).  Of a step's 2100 clocks per wave (two waves share a SIMD) the
-// softmax takes 860, the products 670 (512 at the full rate), staging 510, the barrier 80.
+// Bound: the chain of a step at two waves per SIMD.  40 / 8 heads of 128 over 8192 tokens take 724
+// us (950 TFLOP/s; an 8192-wide bf16 library product reaches 1400 to 1550).  By the counters the
+// matrix units are busy 43 % of that and the vector units active 43 %, hardly at the same time;
+// a wave waits for issue 36 % of its time and for data 22 % (LDS bandwidth is used to 32 %), and the
+// clock is 1.83 GHz.
 // Measured and not kept: eight waves with the last four a phase behind (barriers between
-// phases, 760 us), rows of 64 per wave at one wave per SIMD (accumulator copies, 1120), direct
-// loads to LDS in a ring of four steps (790), staging between the products too (787).
+// phases, 760 us), rows of 64 per wave at one wave per SIMD (1120: as built, with accumulator
+// copies), direct loads to LDS in a ring of four steps (790), staging between the products (787).
 template <int D>
 __global__ __launch_bounds__(256, 2) void prompt_kernel(PromptArgs a) {
   constexpr int NM = D / 32, NK = D / 16;
@@ -349,11 +350,13 @@ constexpr int kWq = 128;    // query rows of a staged tile
 // S^T tiles with the keys as product rows: a lane adds its columns' probabilities up, and the
 // lanes of a key meet once at the end.
 // Bound: the vector units, 24 clocks per wave-wide probability (a product, an exponential of 16
-// clocks, a sum) beside 16 of the matrix unit: 40 / 8 heads over 8192 tokens 350 us, of which
-// the exponentials and sums alone take about 220.  Four waves share a SIMD, so that one's
-// products run beside another's exponentials (64 keys per wave and two waves, half the query
-// reads: 371).  Forming the next scores between the exponentials of the last ones within a wave
-// spilled registers (479 and 656), priorities of the waves changed nothing.
+// clocks, a sum) beside 16 of the matrix unit: 40 / 8 heads over 8192 tokens 356 us.  The counters
+// show 7.1e5 clocks (1.91 GHz), of which the 24 add up to 4.9e5; vector units active 63 %, matrix
+// units busy 47 %.  Four waves share a SIMD, so that one's products run beside another's
+// exponentials (64 keys per wave and two waves, half the query reads: 371); the 128 registers that
+// this leaves are two too few at d_h 128 (spilled).  Forming the next scores between the
+// exponentials of the last ones within a wave spilled more (479 and 656), priorities of the waves
+// changed nothing.
 template <int D>
 __global__ __launch_bounds__(512, 4) void weight_kernel(WeightArgs a) {
   constexpr int NK = D / 16, kOct = D / 8, kPieces = kWq * kOct / 512;

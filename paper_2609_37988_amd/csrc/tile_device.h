@@ -100,9 +100,9 @@ __device__ __forceinline__ float top_logit(const f16v& s, float c, float drop) {
 __device__ __forceinline__ float rescale(float m, float mnew) {
   return m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - mnew);
 }
-// Probabilities 2^(c s - drop - m + bias) of scores s, packed for the second product in p; their sum.  A
-// row whose logits have all been -inf so far keeps the reference -inf, and its probabilities
-// 2^(-inf) = 0 are formed against 0.  rest: NULL, or what the rounding to bf16 left of them (p and
+// Probabilities 2^(c s - drop - m + bias) of scores s, packed for the second product in p; their
+// sum.  A row whose logits have all been -inf so far keeps the reference -inf, and its
+// probabilities 2^(-inf) = 0 are formed against 0.  rest: NULL, or what the rounding to bf16 left of them (p and
 // rest together hold 16 bits).
 template <bool HALF>
 __device__ __forceinline__ float probabilities(float m, const f16v& s, float c, float bias, u4v (&p)[2],
