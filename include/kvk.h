@@ -708,7 +708,7 @@ kvk_status kvk_decode_attention_noalloc(const kvk_table* table, int32_t layer_be
  *              workspace race.
  * Per-sequence tables need no set-up.  The full groups of quantised layers are dequantised to
  * fp16: KIVI32's and GROUP64's values must lie in its range, SYMROW's are scaled into it group by
- * group (exact to fp16's 2^-11 from 2^-60 to 2^60, for tokens whose scale is at least 2^-24 of the
+ * group (exact to fp16's 2^-11 from 2^-40 to 2^40, for tokens whose scale is at least 2^-24 of the
  * group's largest).  The queries and the window are any bf16.
  * Scores, sums and outputs are accumulated in fp32.  Tokens a row does not see (and stale slots) do not reach it,
  * infinities and NaN among them, but through that scale and zero of KIVI32's keys; infinite values at visible tokens count as in

@@ -47,7 +47,9 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kChunkSeqs = 96;  // sequences of a launch
-constexpr int kMostLift = 60;   // largest power of two that scales a block or a row of queries
+// Largest power of two that scales a block, either way: a probability against values 2^80 apart is
+// still a normal fp32 number, and counts in the sum.
+constexpr int kBlockLift = 40;
 
 struct ChunkArgs {
   const uint8_t* arena;
@@ -168,7 +170,7 @@ struct Part {
     top = max(top, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, kHalfRowMirror, 0xF, 0xF, false));
     top = max(top, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, kRowMirror, 0xF, 0xF, false));
     const int ex = __builtin_amdgcn_readfirstlane((int)(top >> 23));
-    const int up = ex == 0 ? 0 : max(min(127 + 7 - ex, kMostLift), -kMostLift);
+    const int up = ex == 0 ? 0 : max(min(127 + 7 - ex, kBlockLift), -kBlockLift);
     const float f = power_of_two(up);
     scales = bitcast<uint32_t>(h2(__uint_as_float(lo) * f, __uint_as_float(hi) * f));
     return up;
@@ -800,7 +802,9 @@ extern "C" kvk_status kvk_chunk_attention(const kvk_table* t, int32_t l0, int32_
   a.nb_cap = t->nb_cap;
   a.qsign = scale > 0.0f ? 1 : (scale < 0.0f ? -1 : 0);
   a.c = a.qsign ? std::fabs(scale) * kLog2e : 1.0f;
-  a.most_lift = std::min(kMostLift, std::ilogb(a.c) + kMostLift);  // (c / 2^(2 kMostLift) stays a normal number)
+  // c / 2^(most_lift + kBlockLift) stays a normal number; queries so small that this binds give
+  // logits that do not count.  (c itself may have overflowed)
+  a.most_lift = std::isinf(a.c) ? 120 : std::min(120, std::ilogb(a.c) + 60);
   // One launch for the sequences that read the same layers from an anchor of one bit-width (one
   // plan: all of them), in groups of kChunkSeqs.  Two passes: every launch is laid out and
   // checked before the first one is made.

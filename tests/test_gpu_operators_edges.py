@@ -210,6 +210,25 @@ def test_chunk_symrow_values_of_many_sizes(d, hq, bits):
         _check_rows(c, stored, new, 0.1, q, out)
 
 
+@pytest.mark.parametrize("d,hq", [(64, 64), (128, 5), (128, 20)])
+@pytest.mark.parametrize("scale", [0.25, -0.25, 1e30, 1e-38])
+def test_chunk_symrow_values_2_to_80_apart(scale, d, hq):
+    """One token with values of 2^40 among many of 2^-40 that together weigh a fifth of it: they count
+    in the sum.  Softmax scales to both ends, the queries to match."""
+    n, t = 2047, 1000
+    c = Streams([(0, 8)], hq, 1, d, 1, n, kvk.SYMROW, seed=50)
+    c.v.copy_(c.v.float() * 2.0**-40)
+    c.v[..., t, :] = (c.v[..., t, :].float() * 2.0**80).bfloat16()
+    c.k[..., :] = 0.0
+    c.k[..., 0] = 1.0
+    c.k[..., t, 0] = 10.0  # ln of 2^13: 9 more than the others
+    c.append([0], [n])
+    q = (_randn(_gen(51), 1, 1, hq, 3, d) * abs(0.01 / scale)).bfloat16()
+    q[..., 0] = 1.0 / scale
+    _, out = _run_chunk(c, 0, 1, [n], [3], scale, q=q)
+    _check_rows(c, [n], [3], scale, q, out)
+
+
 @pytest.mark.parametrize("bits", [8, 4, 2])
 @pytest.mark.parametrize("d,hq", [(64, 64), (128, 5), (128, 20)])
 def test_chunk_symrow_infinite_token(d, hq, bits):
