@@ -639,6 +639,10 @@ kvk_status kvk_decode_setup(const kvk_table* table, int32_t layer_begin, int32_t
  *   scale    : softmax scale applied to the query-key dot product.
  *   workspace: device, >= kvk_workspace_bytes(...) bytes, 256-byte aligned; its
  *              contents on entry are ignored.
+ * Small values of quantised GQA layers: a probability times a value scale is held in fp16, whose
+ * steps end at 2^-24.  At 8 bits and values of standard deviation 2^-5 the outputs are off by
+ * 6e-4 (KIVI32, GROUP64; SYMROW 2e-4), of 2^-9 by 1e-2 (2e-3), of 2^-12 by more than a tenth
+ * (1e-2).  kvk_chunk_attention with one token scales such values first.
  * Calls that overlap on one workspace race.
  * Errors: KVK_ERR_INVALID, KVK_ERR_BUFFER (workspace too small), KVK_ERR_DEVICE. */
 kvk_status kvk_decode_attention(const kvk_table* table, int32_t layer_begin, int32_t layer_end,
@@ -707,7 +711,7 @@ kvk_status kvk_decode_attention_noalloc(const kvk_table* table, int32_t layer_be
  *              aligned; its contents on entry are ignored.  Calls that overlap on one
  *              workspace race.
  * Per-sequence tables need no set-up.  The full groups of quantised layers are dequantised to
- * fp16: KIVI32's and GROUP64's values must lie in its range, SYMROW's are scaled into it group by
+ * fp16: KIVI32's and GROUP64's dequantised values must lie in its range, SYMROW's are scaled into it group by
  * group (exact to fp16's 2^-11 from 2^-40 to 2^40, for tokens whose scale is at least 2^-24 of the
  * group's largest).  The queries and the window are any bf16.
  * Scores, sums and outputs are accumulated in fp32.  Tokens a row does not see (and stale slots) do not reach it,
