@@ -642,7 +642,7 @@ kvk_status kvk_decode_setup(const kvk_table* table, int32_t layer_begin, int32_t
  * Small values of quantised GQA layers: a probability times a value scale is held in fp16, whose
  * steps end at 2^-24.  At 8 bits and values of standard deviation 2^-5 the outputs are off by
  * 6e-4 (KIVI32, GROUP64; SYMROW 2e-4), of 2^-9 by 1e-2 (2e-3), of 2^-12 by more than a tenth
- * (1e-2).  kvk_chunk_attention with one token scales such values first.
+ * (1e-2).  kvk_chunk_attention, with one token too, holds them to its own 2^-11.
  * Calls that overlap on one workspace race.
  * Errors: KVK_ERR_INVALID, KVK_ERR_BUFFER (workspace too small), KVK_ERR_DEVICE. */
 kvk_status kvk_decode_attention(const kvk_table* table, int32_t layer_begin, int32_t layer_end,
