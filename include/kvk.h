@@ -22,8 +22,8 @@
  *     last failing call on the calling thread.
  *   - A kvk_table is immutable after creation; it may be shared between
  *     threads for concurrent calls.
- *   - Keys handed to the library are taken as they are (post-RoPE); the
- *     library never applies a rotary embedding.
+ *   - Keys and queries handed to the calls that write or read a cache are taken as
+ *     they are (post-RoPE); kvk_rotate makes them so.
  *   - GQA head map: query head h reads KV head h / (Hq / Hkv).
  */
 #ifndef KVK_H
@@ -481,6 +481,63 @@ typedef struct {
   int64_t seq, head, token;
 } kvk_strides;
 
+/* Rotary positions of queries and keys, in place or out of place: the step between the model's
+ * projections and the calls that write a cache or attend.  A pair (a, b) of a row at position p
+ * with frequency f becomes
+ *   (m (a cos pf - b sin pf), m (b cos pf + a sin pf)),
+ * m the magnitude; pair i of the `width` channels from `first` on is
+ *   KVK_ROTARY_HALVES : channels i and i + width / 2,
+ *   KVK_ROTARY_PAIRS  : channels 2 i and 2 i + 1.
+ * The other channels of a row are left as they are.
+ *
+ * kvk_rotary_frequencies: the usual frequencies, host only: out[i] (width / 2 of them, radians per
+ * position) = f = base^(-2 i / width), scaled for contexts longer than the model was trained on:
+ *   original_tokens 0 : f / factor (positions interpolated; factor 1: none);
+ *   original_tokens n : with r = n f / (2 pi) the turns over the original context and
+ *                       kept = clamp((r - slow_turns) / (fast_turns - slow_turns), 0, 1),
+ *                       f kept + (f / factor) (1 - kept).
+ * Errors: KVK_ERR_INVALID (width odd or below 2; base, factor not positive and finite; turns not
+ *         0 <= slow < fast; NULL).
+ * kvk_rotary_create: a handle that holds a layout, width / 2 frequencies (any finite ones, of any sign)
+ * and a magnitude; immutable, may be shared between threads.  width: a multiple of 8 up to 512.
+ * Errors: KVK_ERR_INVALID.  kvk_rotary_destroy frees it (NULL is accepted; calls made before are
+ * not affected). */
+typedef enum { KVK_ROTARY_HALVES = 0, KVK_ROTARY_PAIRS = 1 } kvk_rotary_layout;
+typedef struct kvk_rotary kvk_rotary;
+kvk_status kvk_rotary_frequencies(int32_t width, double base, double factor, int32_t original_tokens,
+                                  double slow_turns, double fast_turns, double* out);
+kvk_status kvk_rotary_create(int32_t layout, int32_t width, const double* frequencies, double magnitude,
+                             kvk_rotary** out);
+void kvk_rotary_destroy(kvk_rotary* rotary);
+
+/* Rows [n_seqs][n_heads][n_tokens] of head_dim elements, as kvk_strides lays them (a sequence
+ * stride of 0 here means that sequences share their rows, which only `in` may).  head_dim and first:
+ * multiples of 8, first + width <= head_dim. */
+typedef struct {
+  const void* in;
+  void* out;         /* in itself (the same strides), or rows that overlap none of the call's inputs */
+  int32_t n_heads, head_dim, first;
+  kvk_strides in_strides, out_strides;
+} kvk_rotary_rows;
+
+/* Turns the rows of 1..4 tensors (queries and keys) in one launch.
+ *   positions : device int32 [pos_seqs][n_tokens], any values; sequence s takes row s % pos_seqs
+ *               (1: shared by all; the layers of a [layers][B] batch share its B rows).  A packed
+ *               batch of ragged sequences is one sequence of all its tokens.
+ *   rows      : host [n_rows].
+ *   dtype     : of every in and out.  Products and sums are fp32, rounded once; sines and
+ *               cosines are those of the exact angle to 2^-23.
+ *   inverse   : != 0: the transposed map, sin -> -sin with the same m: the gradient of the forward
+ *               call, and with m = 1 its inverse (a key moved by d positions: the forward
+ *               call with d).
+ * Each pair is read before it is written; an infinite or NaN value makes its pair so.
+ * Errors: KVK_ERR_INVALID (sizes, strides, rows of out that overlap, NULL, misalignment: rows 16 B, positions
+ *         4 B; host memory), KVK_ERR_UNSUPPORTED (more than 2^31 pieces of a row in one call),
+ *         KVK_ERR_DEVICE. */
+kvk_status kvk_rotate(const kvk_rotary* rotary, int32_t n_seqs, int32_t n_tokens, const int32_t* positions,
+                      int32_t pos_seqs, const kvk_rotary_rows* rows, int32_t n_rows, int32_t dtype, int32_t inverse,
+                      hipStream_t stream);
+
 /* Attention of whole prompts at prefill: every token attends to the tokens of its own
  * sequence up to itself, softmax(scale q.k) v, with grouped heads (query head h reads KV head
  * h / (Hq / Hkv)).  Sequences of different lengths run in one launch.
@@ -726,6 +783,108 @@ kvk_status kvk_chunk_attention(const kvk_table* table, int32_t layer_begin, int3
                                int32_t n_chunk, const int32_t* n_stored, const int32_t* n_new, float scale,
                                const void* arena, void* out, void* workspace, size_t workspace_bytes,
                                hipStream_t stream);
+
+/* Decoding over chosen blocks of a long context, GQA tables: an index of the stored blocks' keys, a
+ * choice of blocks for each query by it, and attention that reads those blocks and the bf16 window
+ * alone.  A block is one of the cache's 32-token blocks; block i holds stored tokens 32 i .. 32 i + 31.
+ *
+ * The index holds for every anchor, stream and full block, with [lo_c, hi_c] the range of its stored (dequantised)
+ * keys in channel c, mid = (hi + lo) / 2 and half = (hi - lo) / 2, each vector in 8 bits: from values
+ * x (exact) scale = fp32( max|x| / 127 ), code = clamp( rint( x / scale ), -127, 127 ), 0 where the scale
+ * is.  A block with an infinite or NaN key has codes 0 and scales 0 (mid) and infinity (half).
+ * An anchor's part, [B][Hkv][nb] blocks with nb = stored_tokens_cap / 32: int8 codes [..][2][d_h]
+ * (mid, half), then fp32 scales [..][2]; kvk_index_part gives the byte offsets of both in the index,
+ * per-sequence tables: of one sequence's part ([1][Hkv][nb]); else sequence is 0.  kvk_index_bytes: of
+ * the whole index, which is caller-owned device memory, 256-byte aligned.
+ * Errors of both: KVK_ERR_INVALID, KVK_ERR_UNSUPPORTED (MLA table). */
+kvk_status kvk_index_bytes(const kvk_table* table, size_t* out_bytes);
+kvk_status kvk_index_part(const kvk_table* table, int32_t sequence, int32_t layer, int64_t* codes, int64_t* scales);
+
+/* Writes the summaries of the full blocks n_indexed[b] / 32 .. n_stored[b] / 32 - 1 of every sequence
+ * and every anchor in [layer_begin, layer_end): all blocks after a prefill, the new ones after an
+ * append (where no group was completed: nothing).  Blocks written again by an append after tokens
+ * were taken back have to be indexed again.
+ *   n_indexed: host [B], tokens that the index covers already, at most n_stored[b]; NULL: none.
+ *   n_stored : host [B], tokens stored per stream of each sequence.
+ * The host arrays are read before the call returns.
+ * Errors: KVK_ERR_INVALID (range, lengths, NULL, misalignment: arena 16 B, index 256 B; host memory),
+ *         KVK_ERR_UNSUPPORTED (MLA table; too many blocks for a launch), KVK_ERR_DEVICE. */
+kvk_status kvk_index_blocks(const kvk_table* table, int32_t layer_begin, int32_t layer_end, const int32_t* n_indexed,
+                            const int32_t* n_stored, const void* arena, void* index, hipStream_t stream);
+
+/* Chooses blocks for one new token's queries: per layer, sequence and KV head the blocks of largest
+ *   score = max over the G query heads of s_q (s_mid (q8 . mid8) + s_half (|q8| . half8)),
+ * q8 and s_q the head's query in 8 bits as above (s_q = fp32( max|q| / 127 ), codes rint( q / s_q ) in fp32; zeros
+ * where a query is not finite), an upper bound, up to the 8-bit rounding, of the largest product of the
+ * query with a key of the block (for a positive softmax scale).  The dot products are exact; fp32 rounds
+ * s_half (|q8| . half8), then the sum in one fused multiply and add, then the product with s_q; a score that
+ * is NaN counts as infinite (blocks with infinite or NaN keys come first), equal scores go to the lower block.
+ *   q        : device bf16 [layer_end-layer_begin][B][Hq][d_h].
+ *   n_stored : host [B]; the nb = n_stored[b] / 32 full blocks compete.
+ *   n_select : blocks chosen, >= 1; the n_first first and the n_recent last blocks are among them in any
+ *              case (n_first + n_recent <= n_select).
+ *   blocks   : device int32 [layer_end-layer_begin][B][Hkv][n_select], written in increasing order; where
+ *              a sequence has fewer blocks, all of them and then -1.
+ *   workspace: device, >= kvk_select_workspace_bytes of the range, 256-byte aligned; NULL where that is
+ *              0.  Its contents on entry are ignored; calls that overlap on one workspace race.
+ * Errors: KVK_ERR_INVALID (range, lengths, counts, NULL, misalignment: q 16 B, index and workspace 256 B,
+ *         blocks 4 B; host memory), KVK_ERR_BUFFER (workspace), KVK_ERR_UNSUPPORTED (MLA table; too many rows
+ *         for a launch), KVK_ERR_DEVICE. */
+kvk_status kvk_select_workspace_bytes(const kvk_table* table, int32_t layer_begin, int32_t layer_end, size_t* out_bytes);
+kvk_status kvk_select_blocks(const kvk_table* table, int32_t layer_begin, int32_t layer_end, const void* q,
+                             const int32_t* n_stored, int32_t n_select, int32_t n_first, int32_t n_recent,
+                             const void* index, int32_t* blocks, void* workspace, size_t workspace_bytes,
+                             hipStream_t stream);
+
+/* Attention of one new token per sequence over the blocks of its lists and the bf16 window, softmax(scale
+ * q.k) v over those tokens alone: kvk_chunk_attention's step for n_new = 1 with the other blocks left
+ * out (with every block listed, the same attention).
+ *   q        : device bf16 [layer_end-layer_begin][B][Hq][d_h].
+ *   n_stored : host [B], tokens stored per stream (the new token among them); the window is its last
+ *              n_stored[b] % 32 tokens.
+ *   blocks   : device int32 [layer_end-layer_begin][B][Hkv][n_select], any order; entries outside
+ *              0 .. n_stored[b] / 32 - 1 are passed over, a block listed twice counts twice.
+ *   n_select : >= 1.
+ *   out      : device bf16, as q; zeros where no token is seen.
+ *   workspace: device, >= kvk_block_workspace_bytes of the range and n_select, 256-byte aligned; its contents on
+ *              entry are ignored.  Calls that overlap on one workspace race.
+ * Layers that share an anchor read their own blocks of it.  Per-sequence tables need no set-up.  Values are
+ * held as by kvk_chunk_attention (fp16 for quantised layers, KIVI32's and GROUP64's dequantised values within
+ * its range; SYMROW's of any size, its value scales as there), sums in fp32.  A row whose seen scores are
+ * all -inf, or NaN in one, yields NaN; infinite values count as in kvk_prompt_attention.
+ * Errors: KVK_ERR_INVALID (range, lengths, scale not finite, NULL, misalignment: q, arena and out 16 B, blocks
+ *         4 B, workspace 256 B; host memory), KVK_ERR_BUFFER (workspace), KVK_ERR_UNSUPPORTED (MLA table; too
+ *         many rows for a launch), KVK_ERR_DEVICE. */
+kvk_status kvk_block_workspace_bytes(const kvk_table* table, int32_t layer_begin, int32_t layer_end, int32_t n_select,
+                                     size_t* out_bytes);
+kvk_status kvk_block_attention(const kvk_table* table, int32_t layer_begin, int32_t layer_end, const void* q,
+                               const int32_t* n_stored, const int32_t* blocks, int32_t n_select, float scale,
+                               const void* arena, void* out, void* workspace, size_t workspace_bytes,
+                               hipStream_t stream);
+
+/* Copies stored sequences, all layers, between slots of arenas: a prompt enters a running batch, a prefix is
+ * forked for several samples, sequences move to an arena of another batch or capacity; with a list of blocks,
+ * only those move (eviction by block, compaction).  Copy i reads sequence src[i] of src_arena and writes slot
+ * dst[i] of dst_arena: full blocks 0 .. n_stored[i] / 32 - 1 and, where n_stored[i] % 32 != 0, the bf16 window
+ * (whole, its undefined slots too).  Nothing else of dst_arena is written.
+ *   src_table, dst_table: their caches agree in kind, layers, KV heads and widths and quantiser, and copy i's
+ *               sequences in plan (inherit, bits, rank); batch, capacity and eviction may differ.  Tables
+ *               of one plan and per-sequence tables mix.
+ *   src, dst, n_stored: host [n_copies].  A sequence may be copied several times; no slot is written twice.
+ *               Within one arena (the same table and pointer twice) no slot that is read is written; arenas that
+ *               overlap otherwise are refused.
+ *   blocks    : NULL, or device int32 [n_layers][src batch][Hkv][n_blocks] (MLA: [n_layers][src batch][n_blocks]; anchors'
+ *               rows are read), as kvk_select_blocks writes them for all layers: entry j is the block that
+ *               becomes block j, for j < min(n_blocks, n_stored[i] / 32).  The copy then stores
+ *               32 min(n_blocks, n_stored[i] / 32) + n_stored[i] % 32 tokens.  Entries are trusted to name
+ *               blocks of the sequence; others are clamped.
+ * An index is not copied: kvk_index_blocks writes the new slots' part.  The host arrays are read before the
+ * call returns.
+ * Errors: KVK_ERR_INVALID (tables, slots, lengths, plans, overlap, NULL, misalignment: arenas 16 B, blocks 4 B;
+ *         host memory), KVK_ERR_UNSUPPORTED (batches beyond 65535; too much for a launch), KVK_ERR_DEVICE. */
+kvk_status kvk_copy_sequences(const kvk_table* src_table, const void* src_arena, const kvk_table* dst_table,
+                              void* dst_arena, int32_t n_copies, const int32_t* src, const int32_t* dst,
+                              const int32_t* n_stored, const int32_t* blocks, int32_t n_blocks, hipStream_t stream);
 
 /* Algorithmic bytes one decode call over [layer_begin, layer_end) reads from the
  * arena with n_stored tokens per stream: each distinct anchor's full blocks and

@@ -17,7 +17,7 @@ INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(HERE, "libkvk.so")
 OBJDIR = os.path.join(ROOT, "_build")
 SOURCES = ["table.cpp", "compress.hip", "decode.hip", "mla.hip", "snapkv.hip", "selector.hip",
-           "prompt.hip", "keep.hip", "chunk.hip"]
+           "prompt.hip", "keep.hip", "chunk.hip", "rotary.hip", "index.hip", "blocks.hip", "copy.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [
@@ -30,8 +30,8 @@ FLAGS = [
 # Per-source flags.  The selector's attention kernel rescales its product
 # accumulators on the VALU now and then; with the accumulators in AGPRs the compiler
 # copies them to VGPRs and back on every loop iteration, so its MFMAs write VGPRs; the
-# prompt and chunk kernels do the same.
-EXTRA = {src: ["-mllvm", "-amdgpu-mfma-vgpr-form"] for src in ("selector.hip", "prompt.hip", "chunk.hip")}
+# prompt, chunk and block kernels do the same.
+EXTRA = {src: ["-mllvm", "-amdgpu-mfma-vgpr-form"] for src in ("selector.hip", "prompt.hip", "chunk.hip", "blocks.hip")}
 
 
 def _compile(src: str) -> str:

@@ -1,0 +1,118 @@
+// What the kernels over stored 32-token blocks share: the layers and sequences of a launch.
+#pragma once
+
+#include <algorithm>
+#include <type_traits>
+
+#include "kvk_internal.h"
+
+namespace kvk {
+
+constexpr int kGroupSeqs = 64;  // sequences of a launch
+
+// Layers of one launch, which read anchors of one bit-width.
+struct GroupLayer {
+  int64_t region, index;  // byte offsets in the arena and in the index of the anchor's part
+  int32_t stream_bytes;
+  int32_t layer;          // of the call's
+};
+// Sequences of one launch: where the region of a sequence starts is the layer's plus its own, plus
+// `mult` sequences' streams (one plan: a layer's sequences follow each other; per-sequence plans:
+// the sequence's own table lies at `region`, its index at `index`, and a launch has one layer).
+struct GroupSeq {
+  int64_t region, index;
+  int32_t mult;
+  int32_t seq;           // of the batch
+  int32_t first, stored; // blocks to leave out at the front, tokens stored
+};
+struct Group {
+  int32_t n_layers, n_seqs, Hkv;
+  GroupLayer layers[KVK_MAX_LAYERS];
+  GroupSeq seqs[kGroupSeqs];
+#ifdef __HIPCC__
+  __host__ __device__
+#endif
+  int64_t stream_at(const GroupLayer& l, const GroupSeq& s, int kvh) const {
+    return l.region + s.region + ((int64_t)s.mult * Hkv + kvh) * l.stream_bytes;
+  }
+};
+static_assert(sizeof(Group) <= 3600, "leaves room for a kernel's own arguments");
+
+// The index of a one-plan table's anchor, `blocks` = streams * nb_cap summaries: [blocks][2 D] 8-bit
+// codes, then [blocks][2] fp32 scales, each part 256-byte aligned; the anchors in layer order.
+inline int64_t index_codes_bytes(const kvk_table* t) {
+  return round256((int64_t)t->d.batch * t->d.n_kv_heads * t->nb_cap * 2 * t->d.head_dim);
+}
+inline int64_t index_anchor_bytes(const kvk_table* t) {
+  return index_codes_bytes(t) + round256((int64_t)t->d.batch * t->d.n_kv_heads * t->nb_cap * 8);
+}
+inline int64_t index_offset(const kvk_table* t, int anchor) {
+  int64_t n = 0;
+  for (int l = 0; l < anchor; ++l) n += !t->plan[l].inherit;
+  return n * index_anchor_bytes(t);
+}
+inline int64_t index_total(const kvk_table* t) { return index_offset(t, t->d.n_layers); }
+
+// Calls f(bits, group) for the layers of [l0, l1) of a GQA table: only anchors of the range
+// (anchors_only), or every layer with its anchor's part; layers of all bit-widths in one group
+// (f's bits is 0) unless by_bits.  of(b, seq) fills first and stored of sequence
+// b and says whether it takes part.
+template <class Of, class F>
+kvk_status for_groups(const kvk_table* t, int l0, int l1, bool anchors_only, bool by_bits, Group& g, Of of, F f) {
+  g.Hkv = t->d.n_kv_heads;
+  constexpr int kBits[4] = {16, 8, 4, 2};
+  const int n_kinds = by_bits ? 4 : 1;
+  if (t->seq.empty()) {
+    for (int k = 0; k < n_kinds; ++k) {
+      const int bits = by_bits ? kBits[k] : 0;
+      g.n_layers = 0;
+      for (int l = l0; l < l1; ++l) {
+        const int anc = t->info.anchor_of[l];
+        if ((by_bits && t->bits[anc] != bits) || (anchors_only && anc != l)) continue;
+        g.layers[g.n_layers++] = GroupLayer{t->info.layer_offset[anc], index_offset(t, anc), (int32_t)t->info.stream_bytes[anc], l - l0};
+      }
+      if (g.n_layers == 0) continue;
+      g.n_seqs = 0;
+      for (int b = 0; b < t->d.batch; ++b) {
+        GroupSeq& s = g.seqs[g.n_seqs];
+        s = GroupSeq{0, 0, b, b, 0, 0};
+        if (of(b, s)) ++g.n_seqs;
+        if (g.n_seqs == kGroupSeqs || (b == t->d.batch - 1 && g.n_seqs)) {
+          if (kvk_status st = f(bits, g)) return st;
+          g.n_seqs = 0;
+        }
+      }
+    }
+    return KVK_OK;
+  }
+  for (int l = l0; l < l1; ++l)
+    for (int k = 0; k < n_kinds; ++k) {
+      const int bits = by_bits ? kBits[k] : 0;
+      g.n_layers = 1;
+      g.n_seqs = 0;
+      int64_t index = 0;
+      for (int b = 0; b < t->d.batch; ++b) {
+        const kvk_table* x = t->seq[b];
+        const int anc = x->info.anchor_of[l];
+        const int64_t at = index;
+        index += round256(index_total(x));
+        const bool last = b == t->d.batch - 1;
+        if ((!by_bits || x->bits[anc] == bits) && (!anchors_only || anc == l)) {
+          GroupSeq& s = g.seqs[g.n_seqs];
+          s = GroupSeq{t->seq_base[b] + x->info.layer_offset[anc], at + index_offset(x, anc), 0, b, 0, 0};
+          if (of(b, s)) {
+            // (a launch's streams have one size: that of the bit-width)
+            g.layers[0] = GroupLayer{0, 0, (int32_t)x->info.stream_bytes[anc], l - l0};
+            ++g.n_seqs;
+          }
+        }
+        if (g.n_seqs == kGroupSeqs || (last && g.n_seqs)) {
+          if (kvk_status st = f(bits, g)) return st;
+          g.n_seqs = 0;
+        }
+      }
+    }
+  return KVK_OK;
+}
+
+}  // namespace kvk

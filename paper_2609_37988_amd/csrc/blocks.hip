@@ -1,0 +1,631 @@
+// Attention of single tokens over chosen 32-token blocks of the compressed GQA caches.
+//
+// A workgroup of four waves takes the G query heads of a (layer, sequence, KV head), sixteen at a time,
+// and a part of its list; the waves take its blocks in turn and keep states of their own, which meet
+// in LDS at the end.  Where the rows alone leave the GPU idle the list is split over workgroups and
+// block_merge_kernel joins the parts.  The bf16 window counts as one block more.
+//
+// A block goes from the arena to registers in the order of the matrix operands (that is how it is
+// stored), 16 x 16 x 32 products:
+//   S^T[token, head] = K[token, :] . q[head, :]     O^T[channel, head] += V^T[channel, token] P^T[token, head]
+// so that a head's maximum and sum live in its column and the probabilities feed the second product
+// from where the first left them.  The next block's bytes are in flight meanwhile.
+//
+// Precision, in quantised layers: codes are exact in fp16.  KIVI32's keys and values, and GROUP64's
+// values, are dequantised to fp16 (2^-11 of a value's ulp range, one rounding); the scales of GROUP64's keys and of SYMROW's
+// keys multiply the products, in fp32; SYMROW's value scales (bf16, beyond fp16's range) multiply the probabilities, each block
+// scaled by the power of two that brings its largest to [1, 2).  Queries are bf16, in fp16 exactly (each row scaled by
+// a power of two); probabilities fp16, kept below 2^15.  16-bit layers: keys, values and queries exact, the probabilities bf16.
+// The window's probabilities enter as two bf16 parts in quantised layers.  Sums are fp32, outputs rounded once, to bf16.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+
+#include "block_groups.h"
+#include "tile_device.h"
+
+using namespace kvkd;
+
+namespace {
+
+using kvk::Group;
+using kvk::GroupLayer;
+using kvk::GroupSeq;
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kWaves = 4;
+// Largest power of two that scales a SYMROW block's values, either way (as in the chunk attention).
+constexpr int kBlockLift = 40;
+
+struct BlockArgs {
+  const uint8_t* arena;
+  const uint16_t* q;      // [nl][B][Hq][D]
+  const int32_t* blocks;  // [nl][B][Hkv][n_select]
+  uint16_t* out;
+  float* ws;              // records [nl][B][Hq][n_split][D + 4]
+  int32_t B, Hq, G, tiles;  // tiles of sixteen heads
+  int32_t n_select, n_split, per_split;  // list entries of a split
+  int32_t nb_cap, block_bytes;
+  int32_t qsign, most_lift;
+  float c;
+  Group g;
+};
+static_assert(sizeof(BlockArgs) <= 4096, "kernel arguments");
+
+template <bool HALF>
+__device__ __forceinline__ f4 mfma16(u4v a, u4v b, f4 c) {
+  if constexpr (HALF) return __builtin_amdgcn_mfma_f32_16x16x32_f16(bitcast<half8>(a), bitcast<half8>(b), c, 0, 0, 0);
+  else return __builtin_amdgcn_mfma_f32_16x16x32_bf16(bitcast<bf16x8>(a), bitcast<bf16x8>(b), c, 0, 0, 0);
+}
+__device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((uint32_t)(127 + e) << 23); }  // |e| < 127
+
+// A lane's bytes of one block.
+template <int D, int BITS, int QS>
+struct Raw {
+  static constexpr int KW = BITS == 16 ? D / 8 : D * BITS / 128;  // words of a key tile
+  static constexpr int VW = BITS == 16 ? D / 4 : D * BITS / 64;   // ... of the values
+  static constexpr int MW = BITS == 16 ? 0 : (QS == kQsKivi ? D / 32 : (QS == kQsG64 ? D / 64 : 8));  // metadata
+  uint32_t k[2][KW], v[VW], m[MW > 0 ? MW : 1];
+
+  template <int N>
+  __device__ __forceinline__ static void share(const uint8_t* p, int lane, uint32_t (&w)[N]) {
+    if constexpr (N >= 4) {
+#pragma unroll
+      for (int i = 0; i < N / 4; ++i) {
+        const u4v x = __builtin_nontemporal_load(reinterpret_cast<const u4v*>(p + 1024 * i + 16 * lane));
+        w[4 * i] = x[0]; w[4 * i + 1] = x[1]; w[4 * i + 2] = x[2]; w[4 * i + 3] = x[3];
+      }
+    } else if constexpr (N == 2) {
+      const u2v x = __builtin_nontemporal_load(reinterpret_cast<const u2v*>(p + 8 * lane));
+      w[0] = x[0]; w[1] = x[1];
+    } else {
+      w[0] = __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(p + 4 * lane));
+    }
+  }
+  __device__ __forceinline__ void load(const uint8_t* p, int lane) {
+#pragma unroll
+    for (int tau = 0; tau < 2; ++tau) share(p + tau * (BITS == 16 ? 32 * D : 2 * D * BITS), lane, k[tau]);
+    share(p + (BITS == 16 ? 64 * D : 4 * D * BITS), lane, v);
+    if constexpr (BITS != 16) {
+      const uint8_t* meta = p + 8 * D * BITS;
+      if constexpr (QS != kQsSym) {
+        share(meta, lane, m);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {  // keys then values, tokens 16 tau + 4 kg ..
+          const u2v x = *reinterpret_cast<const u2v*>(meta + 32 * i + 8 * (lane >> 4));
+          m[2 * i] = x[0]; m[2 * i + 1] = x[1];
+        }
+      }
+    }
+  }
+  // Codes of unit u of words w as fp16 integers, less `off`.
+  __device__ __forceinline__ static half8 codes(const uint32_t* w, int u, float off) {
+    if constexpr (BITS == 8) return unpack8(w[2 * u], w[2 * u + 1], off);
+    else if constexpr (BITS == 4) return unpack4(w[u], off);
+    else return unpack2_half(w[u >> 1] >> (8 * (u & 1)), off);
+  }
+};
+
+template <int D>
+struct State {
+  f4 o[D / 16];
+  float m, l;  // reference maximum (base 2); the lane's share of the sum
+};
+
+// Probabilities are kept multiplied by 2^kBias: 2^(kBias + kSlack) is the largest, and with SYMROW's scales below
+// 2 on top of it still in fp16's range.
+template <int BITS, int QS>
+constexpr float kBias = BITS == 16 ? 0.0f : (QS == kQsSym ? 6.0f : 7.0f);
+
+// Probabilities of the lane's eight scores in place (base-2 logits x c - drop, 2^bias times), the state's
+// reference and sums moved on; grow = 2^drop (see RowState in tile_device.h).
+template <int D>
+__device__ __forceinline__ void softmax_step(State<D>& st, float (&x)[8], float c, float bias, float drop, float grow) {
+  float mx = x[0];
+#pragma unroll
+  for (int e = 1; e < 8; ++e) mx = fmaxf(mx, x[e]);
+  mx = rows_max(mx) * c - drop;
+  if (__any(mx > st.m + kSlack)) {
+    const float mnew = fmaxf(st.m, mx), alpha = rescale(st.m, mnew);
+    st.m = mnew;
+    st.l *= alpha;
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) st.o[i] *= alpha;
+  }
+  const float ref = (st.m == -INFINITY ? 0.0f : st.m) - (bias - drop);
+  float sum = 0.0f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    x[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[e], c, -ref));
+    sum += x[e];
+  }
+  st.l += grow * sum;
+}
+
+template <bool HALF>
+__device__ __forceinline__ u4v pack8(const float (&x)[8]) {
+  return u4v{pack2<HALF>(x[0], x[1]), pack2<HALF>(x[2], x[3]), pack2<HALF>(x[4], x[5]), pack2<HALF>(x[6], x[7])};
+}
+
+// The lane's quarter of a row of bf16 queries as fp16, scaled by a power of two; c takes it back.
+template <int NJ>
+__device__ __forceinline__ float queries_to_half(u4v (&q)[NJ], float c, int most) {
+  uint32_t top = 0;
+#pragma unroll
+  for (int j = 0; j < NJ; ++j)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) top = max(top, max(q[j][i] & 0x7fffu, (q[j][i] >> 16) & 0x7fffu));
+  // (positive bf16 values order as their bits do, NaN above infinity)
+  const uint32_t ex0 = top >> 7;
+  const float row = rows_max((float)ex0);
+  const int ex = (int)row;
+  const int up = ex == 0 || ex == 255 ? 0 : min(127 + 15 - ex, most);
+  const float f = power_of_two(up);
+#pragma unroll
+  for (int j = 0; j < NJ; ++j)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      q[j][i] = pack2<true>(__uint_as_float(q[j][i] << 16) * f, __uint_as_float(q[j][i] & 0xffff0000u) * f);
+  return __builtin_ldexpf(c, -up);
+}
+
+// One full block.  q: the queries (fp16, bf16 in 16-bit layers); qsum: GROUP64, their sums by 64 channels.
+template <int D, int BITS, int QS>
+__device__ __forceinline__ void attend(State<D>& st, const Raw<D, BITS, QS>& r, const u4v (&q)[D / 32], const float* qsum,
+                                       float c, uint32_t* slot, int lane) {
+  constexpr bool HALF = BITS != 16;
+  constexpr int NJ = D / 32, NM = D / 16;
+  constexpr float bias = kBias<BITS, QS>;
+  using R = Raw<D, BITS, QS>;
+  const int kg = lane >> 4;
+  if constexpr (R::MW > 0 && QS != kQsSym) {
+    if constexpr (R::MW == 4) {
+      reinterpret_cast<u4v*>(slot)[lane] = u4v{r.m[0], r.m[1], r.m[2], r.m[3]};
+    } else {
+#pragma unroll
+      for (int i = 0; i < R::MW; ++i) slot[lane * R::MW + i] = r.m[i];
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+  }
+  const half8* h8 = reinterpret_cast<const half8*>(slot);
+  float x[8];
+  if constexpr (HALF && QS == kQsG64) {
+    constexpr int NG = D / 64;
+    f4 acc[2][NG];
+#pragma unroll
+    for (int tau = 0; tau < 2; ++tau)
+#pragma unroll
+      for (int g = 0; g < NG; ++g) acc[tau][g] = f4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int j = 0; j < NJ; ++j)
+#pragma unroll
+      for (int tau = 0; tau < 2; ++tau)
+        acc[tau][j / 2] = mfma16<true>(bitcast<u4v>(R::codes(r.k[tau], j, 0.0f)), q[j], acc[tau][j / 2]);
+#pragma unroll
+    for (int tau = 0; tau < 2; ++tau) {
+      f4 s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int g = 0; g < NG; ++g) {
+        const half8 sz = h8[(tau * 4 + kg) * NG + g];  // scales then zeros of tokens 16 tau + 4 kg ..
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          s[e] = __builtin_fmaf((float)sz[e], acc[tau][g][e], __builtin_fmaf((float)sz[4 + e], qsum[g], s[e]));
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[4 * tau + e] = s[e];
+    }
+  } else {
+    f4 acc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) {
+      half8 s, z;
+      if constexpr (HALF && QS == kQsKivi) {
+        s = h8[4 * j + kg];
+        z = h8[D / 8 + 4 * j + kg];
+      }
+#pragma unroll
+      for (int tau = 0; tau < 2; ++tau) {
+        u4v k;
+        if constexpr (!HALF) k = u4v{r.k[tau][4 * j], r.k[tau][4 * j + 1], r.k[tau][4 * j + 2], r.k[tau][4 * j + 3]};
+        else if constexpr (QS == kQsKivi) k = bitcast<u4v>(__builtin_elementwise_fma(R::codes(r.k[tau], j, 0.0f), s, z));
+        else k = bitcast<u4v>(R::codes(r.k[tau], j, (float)(1 << (BITS - 1))));
+        acc[tau] = mfma16<HALF>(k, q[j], acc[tau]);
+      }
+    }
+#pragma unroll
+    for (int tau = 0; tau < 2; ++tau)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        float y = acc[tau][e];
+        if constexpr (HALF && QS == kQsSym) {
+          const uint32_t w = r.m[2 * tau + (e >> 1)];
+          y *= __uint_as_float(e & 1 ? w & 0xffff0000u : w << 16);
+        }
+        x[4 * tau + e] = y;
+      }
+  }
+  if constexpr (HALF && QS == kQsSym) {
+    // the power of two that brings the block's largest (finite) value scale to [1, 2)
+    float vs[8];
+    uint32_t top = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const uint32_t w = r.m[4 + (e >> 1)], b = e & 1 ? w & 0xffff0000u : w << 16;
+      vs[e] = __uint_as_float(b);
+      top = max(top, b < 0x7f800000u ? b : 0u);  // (positive fp32 values order as their bits do)
+    }
+    const uint32_t t = __float_as_uint(rows_max(__uint_as_float(top)));
+    const int ex = __builtin_amdgcn_readfirstlane((int)(t >> 23));
+    const int up = ex == 0 ? 0 : max(min(127 - ex, kBlockLift), -kBlockLift);
+    const float f = power_of_two(up);
+    softmax_step<D>(st, x, c, bias, (float)up, f);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] *= vs[e] * f;
+    const u4v p = pack8<true>(x);
+#pragma unroll
+    for (int m = 0; m < NM; ++m)
+      st.o[m] = mfma16<true>(bitcast<u4v>(R::codes(r.v, m, (float)(1 << (BITS - 1)))), p, st.o[m]);
+  } else {
+    softmax_step<D>(st, x, c, bias, 0.0f, 1.0f);
+    const u4v p = pack8<HALF>(x);
+#pragma unroll
+    for (int m = 0; m < NM; ++m) {
+      u4v v;
+      if constexpr (!HALF) {
+        v = u4v{r.v[4 * m], r.v[4 * m + 1], r.v[4 * m + 2], r.v[4 * m + 3]};
+      } else {
+        constexpr int first = QS == kQsKivi ? D / 4 : D / 8;  // of the values' metadata
+        const int g = m / (QS == kQsKivi ? 2 : 4);
+        const half8 s = h8[first + (2 * g + 0) * 4 + kg], z = h8[first + (2 * g + 1) * 4 + kg];
+        v = bitcast<u4v>(__builtin_elementwise_fma(R::codes(r.v, m, 0.0f), s, z));
+      }
+      st.o[m] = mfma16<HALF>(v, p, st.o[m]);
+    }
+  }
+  if constexpr (R::MW > 0 && QS != kQsSym) {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+  }
+}
+
+// The window: `n` bf16 tokens at p.  HALF: a quantised layer's.
+template <int D, bool HALF>
+__device__ __forceinline__ void attend_window(State<D>& st, const uint8_t* p, int n, const u4v (&q)[D / 32], float c,
+                                              float bias, int lane) {
+  constexpr int NJ = D / 32, NM = D / 16;
+  const int kg = lane >> 4;
+  float x[8];
+#pragma unroll
+  for (int tau = 0; tau < 2; ++tau) {
+    f4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int j = 0; j < NJ; ++j)
+      acc = mfma16<false>(*reinterpret_cast<const u4v*>(p + tau * 32 * D + 1024 * j + 16 * lane), q[j], acc);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[4 * tau + e] = 16 * tau + 4 * kg + e < n ? acc[e] : -INFINITY;
+  }
+  softmax_step<D>(st, x, c, bias, 0.0f, 1.0f);
+  const u4v hi = pack8<false>(x);
+  u4v lo;
+  if constexpr (HALF) {
+    float y[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) y[e] = x[e] - __uint_as_float(e & 1 ? hi[e >> 1] & 0xffff0000u : hi[e >> 1] << 16);
+    lo = pack8<false>(y);
+  }
+#pragma unroll
+  for (int m = 0; m < NM; ++m) {
+    u4v v = *reinterpret_cast<const u4v*>(p + 64 * D + 1024 * m + 16 * lane);
+#pragma unroll
+    for (int e = 0; e < 8; ++e)  // slots past the tokens hold anything
+      if (16 * (e >> 2) + 4 * kg + (e & 3) >= n) v[e >> 1] &= e & 1 ? 0x0000ffffu : 0xffff0000u;
+    st.o[m] = mfma16<false>(v, hi, st.o[m]);
+    // (what the rounding left may be 0, which times an infinity were NaN)
+    if constexpr (HALF) st.o[m] = mfma16<false>(only_finite<false>(v), lo, st.o[m]);
+  }
+}
+
+template <int D, int BITS, int QS>
+__global__ __launch_bounds__(64 * kWaves, 2) void block_kernel(BlockArgs a) {
+  using R = Raw<D, BITS, QS>;
+  constexpr bool HALF = BITS != 16;
+  constexpr int NJ = D / 32, NM = D / 16, kRow = D + 4;  // (rows apart in the banks)
+  constexpr int kSlot = R::MW > 0 && QS != kQsSym ? R::MW * 64 : 4;
+  __shared__ __align__(16) float join[kWaves][16][kRow];
+  __shared__ float2 stats[kWaves][16];
+  __shared__ uint32_t saw[kWaves];
+  __shared__ __align__(16) uint32_t slots[kWaves][kSlot];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int col = lane & 15, kg = lane >> 4;
+
+  uint32_t id = blockIdx.x;
+  const int split = id % (uint32_t)a.n_split;
+  id /= (uint32_t)a.n_split;
+  const int tile = id % (uint32_t)a.tiles;
+  id /= (uint32_t)a.tiles;
+  const int kvh = id % (uint32_t)a.g.Hkv;
+  id /= (uint32_t)a.g.Hkv;
+  const GroupLayer& L = a.g.layers[id / (uint32_t)a.g.n_seqs];
+  const GroupSeq& S = a.g.seqs[id % (uint32_t)a.g.n_seqs];
+  const uint8_t* stream = a.arena + a.g.stream_at(L, S, kvh);
+  const int64_t call_row = (int64_t)L.layer * a.B + S.seq;
+  const int nbf = S.stored >> 5, rest = S.stored & 31;
+  const int32_t* list = a.blocks + (call_row * a.g.Hkv + kvh) * a.n_select;
+
+  const int head = 16 * tile + col;  // the lane's, of the group's
+  const int64_t qrow = (call_row * a.Hq + kvh * a.G + min(head, a.G - 1)) * D;
+  u4v q[NJ];
+  const auto load_queries = [&]() {
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) {
+      q[j] = *reinterpret_cast<const u4v*>(a.q + qrow + 32 * j + 8 * kg);
+      if (a.qsign <= 0) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) q[j][i] = a.qsign < 0 ? q[j][i] ^ 0x80008000u : 0u;
+      }
+    }
+  };
+
+  State<D> st;
+#pragma unroll
+  for (int i = 0; i < NM; ++i) st.o[i] = f4{0.f, 0.f, 0.f, 0.f};
+  st.m = -INFINITY;
+  st.l = 0.0f;
+  bool seen = false;
+
+  // The wave's list entries, 64 at a time; `mask` those left of them that name blocks.
+  const int e0 = split * a.per_split, e1 = min(a.n_select, e0 + a.per_split);
+  int chunk = e0 + wave, entry = -1;
+  uint64_t mask = 0;
+  const auto next = [&]() -> int {  // the next block, or -1
+    while (mask == 0) {
+      if (chunk >= e1) return -1;
+      const int e = chunk + kWaves * lane;
+      entry = e < e1 ? list[e] : -1;
+      mask = __ballot(entry >= 0 && entry < nbf);
+      chunk += 64 * kWaves;
+    }
+    const int i = __ffsll((unsigned long long)mask) - 1;
+    mask &= mask - 1;
+    return __builtin_amdgcn_readlane(entry, i);
+  };
+  int cur = next();
+  R raw[2];
+  if (cur >= 0) raw[0].load(stream + (int64_t)cur * a.block_bytes, lane);
+  load_queries();
+  float c = a.c;
+  float qsum[D / 64];
+  if (cur >= 0) {
+    seen = true;
+    if constexpr (HALF) c = queries_to_half(q, a.c, a.most_lift);
+    if constexpr (HALF && QS == kQsG64) {
+      constexpr uint32_t one = 0x3c003c00u;
+#pragma unroll
+      for (int g = 0; g < D / 64; ++g) {
+        f4 s = {0.f, 0.f, 0.f, 0.f};
+        s = mfma16<true>(u4v{one, one, one, one}, q[2 * g], s);
+        qsum[g] = mfma16<true>(u4v{one, one, one, one}, q[2 * g + 1], s)[0];
+      }
+    }
+    // (the last block is loaded again, by all lanes, in the place of a next one: loads without a branch)
+    while (true) {
+      int nxt = next();
+      raw[1].load(stream + (int64_t)(nxt < 0 ? cur : nxt) * a.block_bytes, lane);
+      attend<D, BITS, QS>(st, raw[0], q, qsum, c, slots[wave], lane);
+      if (nxt < 0) break;
+      cur = nxt;
+      nxt = next();
+      raw[0].load(stream + (int64_t)(nxt < 0 ? cur : nxt) * a.block_bytes, lane);
+      attend<D, BITS, QS>(st, raw[1], q, qsum, c, slots[wave], lane);
+      if (nxt < 0) break;
+      cur = nxt;
+    }
+  }
+  if (rest && split == a.n_split - 1 && wave == kWaves - 1) {  // (the wave with the fewest blocks)
+    if constexpr (HALF) {
+      if (seen) load_queries();
+    }
+    seen = true;
+    attend_window<D, HALF>(st, stream + (int64_t)a.nb_cap * a.block_bytes, rest, q, a.c, kBias<BITS, QS>, lane);
+  }
+
+  // The waves' states meet in LDS.
+  const float l = rows_sum(st.l);
+#pragma unroll
+  for (int m = 0; m < NM; ++m) *reinterpret_cast<f4*>(&join[wave][col][16 * m + 4 * kg]) = st.o[m];
+  if (kg == 0) stats[wave][col] = make_float2(st.m, l);
+  if (lane == 0) saw[wave] = seen;
+  __syncthreads();
+  const int row = tid >> 4, ch = (tid & 15) * (D / 16), h = 16 * tile + row;
+  if (h >= a.G) return;
+  float M = -INFINITY, sum = 0.0f;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) M = fmaxf(M, stats[w][row].x);
+  float o[D / 16];
+#pragma unroll
+  for (int k = 0; k < D / 16; ++k) o[k] = 0.0f;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    const float2 s = stats[w][row];
+    const float f = s.x == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(s.x - M);  // (no mass, or NaN)
+    sum += s.y * f;
+#pragma unroll
+    for (int k = 0; k < D / 16; k += 4) {
+      const f4 x = *reinterpret_cast<const f4*>(&join[w][row][ch + k]);
+#pragma unroll
+      for (int y = 0; y < 4; ++y) o[k + y] += x[y] * f;
+    }
+  }
+  const bool any = saw[0] | saw[1] | saw[2] | saw[3];
+  const int64_t at = call_row * a.Hq + kvh * a.G + h;
+  if (a.n_split == 1) {
+    const float inv = any ? 1.0f / sum : 0.0f;
+#pragma unroll
+    for (int k = 0; k < D / 16; k += 4)
+      *reinterpret_cast<u2v*>(a.out + at * D + ch + k) =
+          u2v{pack2<false>(o[k] * inv, o[k + 1] * inv), pack2<false>(o[k + 2] * inv, o[k + 3] * inv)};
+    return;
+  }
+  float* rec = a.ws + (at * a.n_split + split) * kRow;
+#pragma unroll
+  for (int k = 0; k < D / 16; k += 4) *reinterpret_cast<f4*>(rec + ch + k) = f4{o[k], o[k + 1], o[k + 2], o[k + 3]};
+  if ((tid & 15) == 0) *reinterpret_cast<f4*>(rec + D) = f4{M, sum, any ? 1.0f : 0.0f, 0.0f};
+}
+
+// The splits of every row joined, a quarter of a wave per row.
+template <int D>
+__global__ __launch_bounds__(256) void block_merge_kernel(BlockArgs a, int64_t rows) {
+  constexpr int V = D / 16, kRow = D + 4;
+  const int l16 = threadIdx.x & 15;
+  const int64_t row = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
+  if (row >= rows) return;
+  const float* rec = a.ws + row * a.n_split * kRow;
+  float M = -INFINITY, sum = 0.0f, any = 0.0f, o[V];
+  for (int i = 0; i < a.n_split; ++i) M = fmaxf(M, rec[i * kRow + D]);
+#pragma unroll
+  for (int k = 0; k < V; ++k) o[k] = 0.0f;
+  for (int i = 0; i < a.n_split; ++i) {
+    const float* p = rec + i * kRow;
+    const f4 s = *reinterpret_cast<const f4*>(p + D);
+    const float f = s[0] == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(s[0] - M);  // (no mass, or NaN)
+    sum += s[1] * f;
+    any += s[2];
+#pragma unroll
+    for (int k = 0; k < V; k += 4) {
+      const f4 x = *reinterpret_cast<const f4*>(p + V * l16 + k);
+#pragma unroll
+      for (int y = 0; y < 4; ++y) o[k + y] += x[y] * f;
+    }
+  }
+  const float inv = any > 0.0f ? 1.0f / sum : 0.0f;
+#pragma unroll
+  for (int k = 0; k < V; k += 4)
+    *reinterpret_cast<u2v*>(a.out + row * D + V * l16 + k) =
+        u2v{pack2<false>(o[k] * inv, o[k + 1] * inv), pack2<false>(o[k + 2] * inv, o[k + 3] * inv)};
+}
+
+}  // namespace
+
+using namespace kvk;
+
+namespace {
+
+// Workgroups that a call's splits aim at, and list entries that a split has at least.
+constexpr int64_t kAimWgs = 1024;
+constexpr int64_t kMinEntries = 8;
+
+// Parts of each list.
+int32_t splits_of(const kvk_table* t, int32_t l0, int32_t l1, int32_t n_select) {
+  const int64_t G = t->d.n_q_heads / t->d.n_kv_heads;
+  const int64_t wgs = (int64_t)(l1 - l0) * t->d.batch * t->d.n_kv_heads * ((G + 15) / 16);
+  return (int32_t)std::max<int64_t>(1, std::min((kAimWgs + wgs - 1) / wgs, (n_select + kMinEntries - 1) / kMinEntries));
+}
+
+kvk_status check_call(const kvk_table* t, const char* what, int32_t l0, int32_t l1, int32_t n_select) {
+  if (!t) return fail(KVK_ERR_INVALID, "%s: NULL table", what);
+  if (t->d.kind != KVK_GQA) return fail(KVK_ERR_UNSUPPORTED, "%s: GQA tables only", what);
+  if (l0 < 0 || l1 > t->d.n_layers || l0 >= l1)
+    return fail(KVK_ERR_INVALID, "layer range [%d, %d) invalid for %d layers", l0, l1, t->d.n_layers);
+  if (n_select < 1) return fail(KVK_ERR_INVALID, "%s: n_select %d", what, n_select);
+  return KVK_OK;
+}
+
+template <int D, int QS>
+void launch(int bits, dim3 g, const BlockArgs& a, hipStream_t st) {
+  const dim3 b(64 * kWaves);
+  if (bits == 16) hipLaunchKernelGGL((block_kernel<D, 16, kQsKivi>), g, b, 0, st, a);
+  else if (bits == 8) hipLaunchKernelGGL((block_kernel<D, 8, QS>), g, b, 0, st, a);
+  else if (bits == 4) hipLaunchKernelGGL((block_kernel<D, 4, QS>), g, b, 0, st, a);
+  else hipLaunchKernelGGL((block_kernel<D, 2, QS>), g, b, 0, st, a);
+}
+template <int D>
+void launch(int qs, int bits, dim3 g, const BlockArgs& a, hipStream_t st) {
+  if (qs == KVK_Q_KIVI32) launch<D, kQsKivi>(bits, g, a, st);
+  else if (qs == KVK_Q_GROUP64) launch<D, kQsG64>(bits, g, a, st);
+  else launch<D, kQsSym>(bits, g, a, st);
+}
+
+}  // namespace
+
+extern "C" kvk_status kvk_block_workspace_bytes(const kvk_table* t, int32_t l0, int32_t l1, int32_t n_select, size_t* out) {
+  if (kvk_status st = check_call(t, "kvk_block_workspace_bytes", l0, l1, n_select)) return st;
+  if (!out) return fail(KVK_ERR_INVALID, "kvk_block_workspace_bytes: NULL output");
+  const int64_t ns = splits_of(t, l0, l1, n_select);
+  const int64_t rows = (int64_t)(l1 - l0) * t->d.batch * t->d.n_q_heads;
+  *out = (size_t)(ns > 1 ? round256(rows * ns * (t->d.head_dim + 4) * 4) : 256);
+  return KVK_OK;
+}
+
+extern "C" kvk_status kvk_block_attention(const kvk_table* t, int32_t l0, int32_t l1, const void* q, const int32_t* n_stored,
+                                          const int32_t* blocks, int32_t n_select, float scale, const void* arena, void* out,
+                                          void* workspace, size_t ws_bytes, hipStream_t stream) {
+  const char* what = "kvk_block_attention";
+  if (kvk_status st = check_call(t, what, l0, l1, n_select)) return st;
+  const kvk_dims& d = t->d;
+  if (!q || !n_stored || !blocks || !arena || !out || !workspace) return fail(KVK_ERR_INVALID, "%s: NULL buffer", what);
+  if (!std::isfinite(scale)) return fail(KVK_ERR_INVALID, "%s: scale must be finite", what);
+  for (int b = 0; b < d.batch; ++b)
+    if (n_stored[b] < 0 || n_stored[b] > t->cap)
+      return fail(KVK_ERR_INVALID, "%s: n_stored[%d] = %d outside 0..%d", what, b, n_stored[b], t->cap);
+  if ((reinterpret_cast<uintptr_t>(q) & 15) || (reinterpret_cast<uintptr_t>(arena) & 15) ||
+      (reinterpret_cast<uintptr_t>(out) & 15) || (reinterpret_cast<uintptr_t>(blocks) & 3) ||
+      (reinterpret_cast<uintptr_t>(workspace) & 255))
+    return fail(KVK_ERR_INVALID, "%s: misaligned buffer (q, arena, out 16 B, blocks 4 B, workspace 256 B)", what);
+  size_t need = 0;
+  if (kvk_status st = kvk_block_workspace_bytes(t, l0, l1, n_select, &need)) return st;
+  BlockArgs a;
+  a.n_split = splits_of(t, l0, l1, n_select);
+  if (a.n_split > 1 && ws_bytes < need) return fail(KVK_ERR_BUFFER, "%s: workspace %zu bytes < %zu needed", what, ws_bytes, need);
+  if (kvk_status st = check_gpu_buffers({q, blocks, arena, out, workspace}, what)) return st;
+  a.arena = static_cast<const uint8_t*>(arena);
+  a.q = static_cast<const uint16_t*>(q);
+  a.blocks = blocks;
+  a.out = static_cast<uint16_t*>(out);
+  a.ws = static_cast<float*>(workspace);
+  a.B = d.batch;
+  a.Hq = d.n_q_heads;
+  a.G = d.n_q_heads / d.n_kv_heads;
+  a.tiles = (a.G + 15) / 16;
+  a.n_select = n_select;
+  a.per_split = (n_select + a.n_split - 1) / a.n_split;
+  a.nb_cap = t->nb_cap;
+  a.qsign = scale > 0.0f ? 1 : (scale < 0.0f ? -1 : 0);
+  a.c = a.qsign ? std::fabs(scale) * kLog2e : 1.0f;
+  // c / 2^(most_lift + kBlockLift) stays a normal number; queries so small that this binds give
+  // logits that do not count.  (c itself may have overflowed)
+  a.most_lift = std::isinf(a.c) ? 120 : std::min(120, std::ilogb(a.c) + 60);
+  const int64_t rows = (int64_t)(l1 - l0) * d.batch * d.n_q_heads;
+  if (rows > 0x7fffffffLL) return fail(KVK_ERR_UNSUPPORTED, "%s: too many query rows in one call", what);
+  for (const bool go : {false, true}) {
+    const kvk_status st = for_groups(
+        t, l0, l1, false, true, a.g,
+        [&](int b, GroupSeq& s) {
+          s.stored = n_stored[b];
+          return true;
+        },
+        [&](int bits, Group& g) -> kvk_status {
+          const int64_t wgs = (int64_t)g.n_layers * g.n_seqs * d.n_kv_heads * a.tiles * a.n_split;
+          if (wgs > 0xffffffLL) return fail(KVK_ERR_UNSUPPORTED, "%s: grid too large", what);  // (less than 2^32 threads)
+          if (!go) return KVK_OK;
+          a.block_bytes = (int32_t)gqa_block_bytes(d.head_dim, bits, d.qscheme);
+          const dim3 grid((unsigned)wgs);
+          if (d.head_dim == 128) launch<128>(d.qscheme, bits, grid, a, stream);
+          else launch<64>(d.qscheme, bits, grid, a, stream);
+          const hipError_t e = hipGetLastError();
+          if (e != hipSuccess) return fail(KVK_ERR_DEVICE, "%s launch: %s", what, hipGetErrorString(e));
+          return KVK_OK;
+        });
+    if (st != KVK_OK) return st;
+  }
+  if (a.n_split > 1) {
+    const dim3 g((unsigned)((rows + 15) / 16)), b(256);
+    if (d.head_dim == 128) hipLaunchKernelGGL(block_merge_kernel<128>, g, b, 0, stream, a, rows);
+    else hipLaunchKernelGGL(block_merge_kernel<64>, g, b, 0, stream, a, rows);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return fail(KVK_ERR_DEVICE, "%s launch: %s", what, hipGetErrorString(e));
+  }
+  return KVK_OK;
+}

@@ -1,0 +1,226 @@
+// Copies of stored sequences between slots and arenas: admission into a batch, forks, moves to an
+// arena of another capacity, and compaction to chosen blocks.
+//
+// A stream's full blocks lie one after another and its bf16 window sits past the capacity, so a
+// copy moves 32-token blocks (those of a list, or all) and then the window, whole.  Bytes are
+// not looked at: a quantised block's codes and scales go together.
+//
+// A wave moves one block at a time; the copies of one source (a fork) are neighbours in the grid, so that its
+// bytes come from HBM once and from the caches for the others.
+//
+// Bound.  HBM.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "kvk_device.h"
+#include "kvk_internal.h"
+
+using namespace kvkd;
+
+namespace {
+
+constexpr int kCopies = 96;   // of a launch
+constexpr int kPiece = 16384; // bytes that a wave moves, about
+
+struct CopyLayer {
+  int64_t from, to;  // byte offsets of the layer's regions (of the sequence's, per-sequence plans)
+  int32_t from_stream, to_stream, block_bytes;
+  int32_t row;       // of the lists
+  int32_t per_wave;  // blocks a wave moves
+  int32_t wave0;     // waves of a (copy, stream) before this layer's
+};
+
+struct CopyArgs {
+  const uint8_t* src;
+  uint8_t* dst;
+  const int32_t* blocks;  // NULL, or [layers][slots][streams][n_blocks]
+  int32_t n_blocks, list_slots;
+  int32_t n_copies, n_layers, streams;  // streams of a sequence
+  int32_t from_cap, to_cap, window;     // capacities in blocks, bytes of a window
+  int32_t waves;                        // of a (copy, stream)
+  CopyLayer layer[KVK_MAX_LAYERS];
+  int32_t stored[kCopies];
+  uint16_t from[kCopies], to[kCopies], list[kCopies];  // slots within the regions and the lists
+};
+static_assert(sizeof(CopyArgs) <= 4096, "kernel arguments");
+
+__device__ __forceinline__ void move(const uint8_t* from, uint8_t* to, int bytes, int lane) {
+  int at = 16 * lane;
+  for (; at + 3072 < bytes; at += 4096) {  // (every lane's four pieces are inside but perhaps the last lanes')
+    u4v x[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = *reinterpret_cast<const u4v*>(from + at + 1024 * i);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) *reinterpret_cast<u4v*>(to + at + 1024 * i) = x[i];
+  }
+  for (; at < bytes; at += 1024) *reinterpret_cast<u4v*>(to + at) = *reinterpret_cast<const u4v*>(from + at);
+}
+
+__global__ __launch_bounds__(256) void copy_kernel(CopyArgs a) {
+  const int lane = threadIdx.x & 63;
+  const int copy = blockIdx.x % (uint32_t)a.n_copies;
+  const int w = __builtin_amdgcn_readfirstlane((int)(blockIdx.x / (uint32_t)a.n_copies * 4 + (threadIdx.x >> 6)));
+  if (w >= a.waves) return;
+  int l = 0;
+  while (l + 1 < a.n_layers && w >= a.layer[l + 1].wave0) ++l;
+  const CopyLayer& y = a.layer[l];
+  const int stream = blockIdx.y, part = w - y.wave0;
+  const int stored = a.stored[copy], full = stored >> 5;
+  const int n = a.blocks ? min(a.n_blocks, full) : full;
+  const uint8_t* from = a.src + y.from + ((int64_t)a.from[copy] * a.streams + stream) * y.from_stream;
+  uint8_t* to = a.dst + y.to + ((int64_t)a.to[copy] * a.streams + stream) * y.to_stream;
+  if (part == 0) {  // the first wave also moves the window
+    if (stored & 31)
+      move(from + (int64_t)a.from_cap * y.block_bytes, to + (int64_t)a.to_cap * y.block_bytes, a.window, lane);
+  }
+  const int i0 = part * y.per_wave, i1 = min(n, i0 + y.per_wave);
+  if (a.blocks) {
+    const int32_t* list = a.blocks + (((int64_t)y.row * a.list_slots + a.list[copy]) * a.streams + stream) * a.n_blocks;
+    for (int i = i0; i < i1; ++i) {
+      const int b = min(max(__builtin_amdgcn_readfirstlane(list[i]), 0), full - 1);
+      move(from + (int64_t)b * y.block_bytes, to + (int64_t)i * y.block_bytes, y.block_bytes, lane);
+    }
+  } else if (i0 < i1) {
+    move(from + (int64_t)i0 * y.block_bytes, to + (int64_t)i0 * y.block_bytes, (i1 - i0) * y.block_bytes, lane);
+  }
+}
+
+}  // namespace
+
+using namespace kvk;
+
+namespace {
+
+int64_t window_bytes(const kvk_table* s, int l) {
+  return s->d.kind == KVK_MLA ? 64LL * (s->rank[l] + s->d.rope_dim) : 128LL * s->d.head_dim;
+}
+
+bool same_plan(const kvk_table* a, const kvk_table* b) {
+  for (int l = 0; l < a->d.n_layers; ++l) {
+    if (!a->plan[l].inherit != !b->plan[l].inherit) return false;
+    if (!a->plan[l].inherit && (a->bits[l] != b->bits[l] || a->rank[l] != b->rank[l])) return false;
+  }
+  return true;
+}
+
+bool same_shape(const kvk_dims& a, const kvk_dims& b) {
+  if (a.kind != b.kind || a.n_layers != b.n_layers || a.qscheme != b.qscheme) return false;
+  if (a.kind == KVK_MLA) return a.latent_dim == b.latent_dim && a.rope_dim == b.rope_dim;
+  return a.n_kv_heads == b.n_kv_heads && a.head_dim == b.head_dim;
+}
+
+}  // namespace
+
+extern "C" kvk_status kvk_copy_sequences(const kvk_table* st, const void* src_arena, const kvk_table* dt, void* dst_arena,
+                                         int32_t n_copies, const int32_t* src, const int32_t* dst, const int32_t* n_stored,
+                                         const int32_t* blocks, int32_t n_blocks, hipStream_t stream) {
+  const char* what = "kvk_copy_sequences";
+  if (!st || !dt) return fail(KVK_ERR_INVALID, "%s: NULL table", what);
+  if (!same_shape(st->d, dt->d)) return fail(KVK_ERR_INVALID, "%s: the tables' caches differ in shape or quantiser", what);
+  if (n_copies < 0) return fail(KVK_ERR_INVALID, "%s: %d copies", what, n_copies);
+  if (n_copies == 0) return KVK_OK;
+  if (!src_arena || !dst_arena || !src || !dst || !n_stored) return fail(KVK_ERR_INVALID, "%s: NULL argument", what);
+  if (n_copies > dt->d.batch) return fail(KVK_ERR_INVALID, "%s: %d copies into %d slots", what, n_copies, dt->d.batch);
+  if (blocks && n_blocks < 0) return fail(KVK_ERR_INVALID, "%s: lists of %d blocks", what, n_blocks);
+  if (st->d.batch > 65535 || dt->d.batch > 65535)
+    return fail(KVK_ERR_UNSUPPORTED, "%s: batches of %d and %d (at most 65535)", what, st->d.batch, dt->d.batch);
+  if ((reinterpret_cast<uintptr_t>(src_arena) & 15) || (reinterpret_cast<uintptr_t>(dst_arena) & 15) ||
+      (reinterpret_cast<uintptr_t>(blocks) & 3))
+    return fail(KVK_ERR_INVALID, "%s: misaligned buffer (arenas 16 B, blocks 4 B)", what);
+  const uintptr_t s0 = reinterpret_cast<uintptr_t>(src_arena), s1 = s0 + st->info.arena_bytes;
+  const uintptr_t d0 = reinterpret_cast<uintptr_t>(dst_arena), d1 = d0 + dt->info.arena_bytes;
+  const bool within = src_arena == dst_arena && st == dt;
+  if (!within && s0 < d1 && d0 < s1)
+    return fail(KVK_ERR_INVALID, "%s: the arenas overlap (one arena: the same pointer and table twice)", what);
+  const auto plan_of = [](const kvk_table* t, int b) { return t->seq.empty() ? t : t->seq[b]; };
+  for (int i = 0; i < n_copies; ++i) {
+    if (src[i] < 0 || src[i] >= st->d.batch) return fail(KVK_ERR_INVALID, "%s: src[%d] = %d outside 0..%d", what, i, src[i], st->d.batch - 1);
+    if (dst[i] < 0 || dst[i] >= dt->d.batch) return fail(KVK_ERR_INVALID, "%s: dst[%d] = %d outside 0..%d", what, i, dst[i], dt->d.batch - 1);
+    if (n_stored[i] < 0 || n_stored[i] > st->cap)
+      return fail(KVK_ERR_INVALID, "%s: n_stored[%d] = %d outside 0..%d", what, i, n_stored[i], st->cap);
+    const int32_t kept = blocks ? std::min(n_blocks, n_stored[i] / 32) * 32 + n_stored[i] % 32 : n_stored[i];
+    if (kept > dt->cap) return fail(KVK_ERR_INVALID, "%s: %d tokens of copy %d beyond the capacity %d", what, kept, i, dt->cap);
+  }
+  {  // every slot written once, and none read that is written
+    uint64_t use[1024] = {};
+    const auto used = [&](int b) { return use[b >> 6] >> (b & 63) & 1; };
+    for (int i = 0; i < n_copies; ++i) {
+      if (used(dst[i])) return fail(KVK_ERR_INVALID, "%s: slot %d is written twice", what, dst[i]);
+      use[dst[i] >> 6] |= 1ull << (dst[i] & 63);
+    }
+    for (int i = 0; within && i < n_copies; ++i)
+      if (used(src[i])) return fail(KVK_ERR_INVALID, "%s: slot %d is read and written in one arena", what, src[i]);
+  }
+  const bool per_seq = !st->seq.empty() || !dt->seq.empty();
+  for (int i = 0; i < (per_seq ? n_copies : 1); ++i)
+    if (!same_plan(plan_of(st, src[i]), plan_of(dt, dst[i])))
+      return fail(KVK_ERR_INVALID, "%s: the plans of copy %d's source and destination differ", what, i);
+  if (kvk_status e = check_gpu_buffers({src_arena, dst_arena, blocks}, what)) return e;
+
+  CopyArgs a;
+  a.src = static_cast<const uint8_t*>(src_arena);
+  a.dst = static_cast<uint8_t*>(dst_arena);
+  a.blocks = blocks;
+  a.n_blocks = blocks ? n_blocks : 0;
+  a.list_slots = st->d.batch;
+  a.streams = st->d.kind == KVK_MLA ? 1 : st->d.n_kv_heads;
+  a.from_cap = st->nb_cap;
+  a.to_cap = dt->nb_cap;
+  if (a.streams > 65535) return fail(KVK_ERR_UNSUPPORTED, "%s: %d KV heads", what, a.streams);
+  // One plan: launches of up to kCopies copies.  Per-sequence plans: one copy each.
+  // Two passes: the grids are checked before the first launch.
+  for (const bool go : {false, true}) {
+    for (int c0 = 0; c0 < n_copies;) {
+      const int c1 = per_seq ? c0 + 1 : std::min(n_copies, c0 + kCopies);
+      const kvk_table *s = plan_of(st, src[c0]), *t = plan_of(dt, dst[c0]);
+      int32_t most = 0;
+      a.n_copies = c1 - c0;
+      for (int i = c0; i < c1; ++i) {
+        a.stored[i - c0] = n_stored[i];
+        a.from[i - c0] = st->seq.empty() ? (uint16_t)src[i] : 0;
+        a.to[i - c0] = dt->seq.empty() ? (uint16_t)dst[i] : 0;
+        a.list[i - c0] = (uint16_t)src[i];
+        most = std::max(most, blocks ? std::min(n_blocks, n_stored[i] / 32) : n_stored[i] / 32);
+      }
+      a.n_layers = 0;
+      int64_t waves = 0, window = -1;
+      const auto flush = [&]() -> kvk_status {
+        if (a.n_layers == 0) return KVK_OK;
+        a.waves = (int32_t)waves;
+        a.window = (int32_t)window;
+        const int64_t gx = (waves + 3) / 4 * a.n_copies;
+        if (gx * a.streams * 256 > 0xffffffffLL) return fail(KVK_ERR_UNSUPPORTED, "%s: grid too large", what);
+        if (go) {
+          hipLaunchKernelGGL(copy_kernel, dim3((unsigned)gx, (unsigned)a.streams), dim3(256), 0, stream, a);
+          const hipError_t e = hipGetLastError();
+          if (e != hipSuccess) return fail(KVK_ERR_DEVICE, "%s launch: %s", what, hipGetErrorString(e));
+        }
+        a.n_layers = 0;
+        waves = 0;
+        return KVK_OK;
+      };
+      for (int l = 0; l < s->d.n_layers; ++l) {
+        if (s->plan[l].inherit) continue;
+        const int64_t w = window_bytes(s, l);
+        if (a.n_layers && w != window)  // (latent layers of other widths)
+          if (kvk_status e = flush()) return e;
+        window = w;
+        CopyLayer& y = a.layer[a.n_layers];
+        y.from = (st->seq.empty() ? 0 : st->seq_base[src[c0]]) + s->info.layer_offset[l];
+        y.to = (dt->seq.empty() ? 0 : dt->seq_base[dst[c0]]) + t->info.layer_offset[l];
+        y.from_stream = (int32_t)s->info.stream_bytes[l];
+        y.to_stream = (int32_t)t->info.stream_bytes[l];
+        y.block_bytes = (int32_t)s->block_bytes[l];
+        y.row = l;
+        y.per_wave = std::max<int32_t>(1, kPiece / y.block_bytes);
+        y.wave0 = (int32_t)waves;
+        waves += std::max<int64_t>(1, (most + y.per_wave - 1) / y.per_wave);
+        ++a.n_layers;
+      }
+      if (kvk_status e = flush()) return e;
+      c0 = c1;
+    }
+  }
+  return KVK_OK;
+}

@@ -1,0 +1,786 @@
+// Summaries of the stored blocks' keys, and the blocks that they choose for a query.
+//
+// For a 32-token block and a channel c let [lo_c, hi_c] hold the block's stored keys; then no key k of
+// the block has a larger product with a query q than
+//   sum_c max(q_c lo_c, q_c hi_c) = q . mid + |q| . half,   mid = (hi + lo) / 2, half = (hi - lo) / 2.
+// Both products are of one row [mid | half] with one row [q | |q|].  The rows are held in 8 bits with
+// one fp32 scale for each part (the query's, one for both), so that the products are sums of integers:
+// exact, the same in any order, and the choice is the same on every run.
+//
+//   index_kernel   one wave per block.  Its keys pass through the matrix cores (a product with a
+//                  selection of 16 channels is exact and turns tokens x channels into one channel per
+//                  lane), so that minima and maxima run over registers; codes are enough for KIVI32,
+//                  whose scale and zero belong to the channel.  Sums, scales and codes are in 64 bits:
+//                  they cost a wave 4 values per lane.
+//   select_kernel  one workgroup per (layer, sequence, KV head): scores into LDS, then the choice.
+//   score_kernel, choose_kernel  the same in two launches, the scores through the workspace: for
+//                  launches of few rows or of more blocks than LDS holds.
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+
+#include "block_groups.h"
+#include "kvk_device.h"
+
+using namespace kvkd;
+
+namespace {
+
+using kvk::Group;
+using kvk::GroupLayer;
+using kvk::GroupSeq;
+
+// ---------------------------------------------------------------------------
+// Index
+// ---------------------------------------------------------------------------
+
+struct IndexArgs {
+  const uint8_t* arena;
+  uint8_t* index;
+  int64_t scales;  // bytes from an anchor's codes to its scales
+  int32_t nb_cap, block_bytes;
+  Group g;
+};
+static_assert(sizeof(IndexArgs) <= 4096, "kernel arguments");
+
+template <bool HALF>
+__device__ __forceinline__ f4 mfma16(u4v a, u4v b, f4 c) {
+  if constexpr (HALF) return __builtin_amdgcn_mfma_f32_16x16x32_f16(bitcast<half8>(a), bitcast<half8>(b), c, 0, 0, 0);
+  else return __builtin_amdgcn_mfma_f32_16x16x32_bf16(bitcast<bf16x8>(a), bitcast<bf16x8>(b), c, 0, 0, 0);
+}
+
+// Minimum and maximum over the four 16-lane rows of N values per lane: afterwards the lane of row r
+// holds, in place v < N / 4, value v + (r % 2) N / 4 + (r / 2) N / 2.  (Each swap leaves a lane the two halves
+// of one value, so that every step halves the values.)
+template <int N, class Op>
+__device__ __forceinline__ void rows_scatter(float (&x)[N], Op op) {
+#pragma unroll
+  for (int v = 0; v < N / 2; ++v) {
+    const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(x[v]), __float_as_uint(x[v + N / 2]), false, false);
+    x[v] = op(__uint_as_float(p[0]), __uint_as_float(p[1]));
+  }
+#pragma unroll
+  for (int v = 0; v < N / 4; ++v) {
+    const auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(x[v]), __float_as_uint(x[v + N / 4]), false, false);
+    x[v] = op(__uint_as_float(p[0]), __uint_as_float(p[1]));
+  }
+}
+
+// a / b, b > 0, with r near 1 / b: rounded to nearest as the quotient is.
+__device__ __forceinline__ double quotient(double a, double b, double r) {
+  const double q = a * r;
+  return __builtin_fma(__builtin_fma(-q, b, a), r, q);
+}
+
+// A part of a block summary, N values per lane: the scale (largest magnitude / 127, in fp32) and
+// the codes.
+template <int N>
+__device__ __forceinline__ float eight_bits(const double (&x)[N], int (&code)[N]) {
+  float top = 0.0f;
+#pragma unroll
+  for (int i = 0; i < N; ++i) top = fmaxf(top, (float)quotient(__builtin_fabs(x[i]), 127.0, 1.0 / 127.0));
+  top = rows_max(max16(top));  // (rounding keeps the order)
+  const double s = (double)top, r = top > 0.0f ? 1.0 / s : 0.0;
+#pragma unroll
+  for (int i = 0; i < N; ++i) code[i] = (int)fmin(fmax(__builtin_rint(quotient(x[i], s, r)), -127.0), 127.0);
+  return top;
+}
+
+template <int D, int BITS, int QS>
+__global__ __launch_bounds__(256) void index_kernel(IndexArgs a) {
+  constexpr bool HALF = BITS != 16;
+  constexpr int NJ = D / 32, NC = D / 16, NV = NC / 4;  // k-steps, 16-channel tiles, channels of a lane
+  constexpr int KB = BITS == 16 ? D / 2 : D * BITS / 32, KW = KB / 4;  // bytes and words of a lane's tile
+  const int lane = threadIdx.x & 63, n = lane & 15, kg = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+  const GroupLayer& L = a.g.layers[blockIdx.z / (uint32_t)a.g.n_seqs];
+  const GroupSeq& S = a.g.seqs[blockIdx.z % (uint32_t)a.g.n_seqs];
+  const int kvh = blockIdx.y, blk = S.first + blockIdx.x * 4 + wave;
+  if (blk >= S.stored >> 5) return;
+  const uint8_t* p = a.arena + a.g.stream_at(L, S, kvh) + (int64_t)blk * a.block_bytes;
+  const uint8_t* meta = p + 8 * D * BITS;
+
+  uint32_t w[2][KW];
+#pragma unroll
+  for (int tau = 0; tau < 2; ++tau) {
+    const uint8_t* q = p + tau * (BITS == 16 ? 32 * D : 2 * D * BITS);
+    if constexpr (KW >= 4) {
+#pragma unroll
+      for (int i = 0; i < KW / 4; ++i) {
+        const u4v x = *reinterpret_cast<const u4v*>(q + 1024 * i + 16 * lane);
+        w[tau][4 * i] = x[0]; w[tau][4 * i + 1] = x[1]; w[tau][4 * i + 2] = x[2]; w[tau][4 * i + 3] = x[3];
+      }
+    } else if constexpr (KW == 2) {
+      const u2v x = *reinterpret_cast<const u2v*>(q + 8 * lane);
+      w[tau][0] = x[0]; w[tau][1] = x[1];
+    } else {
+      w[tau][0] = *reinterpret_cast<const uint32_t*>(q + 4 * lane);
+    }
+  }
+  bool bad = false;  // an infinite or NaN key
+  float rs[8];       // SYMROW: the scales of the lane's tokens 16 tau + 4 kg + r
+  half8 sz[QS == kQsG64 ? 2 : 1][QS == kQsG64 ? D / 64 : 1];  // GROUP64: their scales and zeros
+  float ks[NV], kz[NV];  // KIVI32: of the lane's channels
+  const auto channel = [&](int v) { return 16 * (v + (kg & 1) * (NC / 4) + (kg >> 1) * (NC / 2)) + n; };
+  if constexpr (BITS != 16 && QS == kQsSym) {
+#pragma unroll
+    for (int tau = 0; tau < 2; ++tau) {
+      const u2v x = *reinterpret_cast<const u2v*>(meta + 32 * tau + 8 * kg);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        rs[4 * tau + r] = __uint_as_float(r & 1 ? x[r >> 1] & 0xffff0000u : x[r >> 1] << 16);
+        bad |= (__float_as_uint(rs[4 * tau + r]) & 0x7f800000u) == 0x7f800000u;
+      }
+    }
+  } else if constexpr (BITS != 16 && QS == kQsG64) {
+#pragma unroll
+    for (int tau = 0; tau < 2; ++tau)
+#pragma unroll
+      for (int g = 0; g < D / 64; ++g) {
+        sz[tau][g] = *reinterpret_cast<const half8*>(meta + 2 * ((tau * 4 + kg) * (D / 64) * 2 + g * 2) * 4);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) bad |= (bitcast<uint16_t>(sz[tau][g][i]) & 0x7c00u) == 0x7c00u;
+      }
+  } else if constexpr (BITS != 16) {
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      ks[v] = (float)reinterpret_cast<const _Float16*>(meta)[channel(v)];
+      kz[v] = (float)reinterpret_cast<const _Float16*>(meta)[D + channel(v)];
+    }
+  }
+
+  // the lane's part of the selections of channels 16 h .. 16 h + 15 of a k-step
+  constexpr uint32_t kOne = HALF ? 0x3c00u : 0x3f80u;
+  u4v sel[2];
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      sel[h][i] = kg == 2 * h + (n >> 3) && ((n & 7) >> 1) == i ? (n & 1 ? kOne << 16 : kOne) : 0u;
+
+  float lo[NC], hi[NC];
+  float nan = 0.0f;
+#pragma unroll
+  for (int j = 0; j < NJ; ++j) {
+    u4v k[2];
+#pragma unroll
+    for (int tau = 0; tau < 2; ++tau) {
+      if constexpr (BITS == 16) k[tau] = u4v{w[tau][4 * j], w[tau][4 * j + 1], w[tau][4 * j + 2], w[tau][4 * j + 3]};
+      else {
+        const float off = QS == kQsSym ? (float)(1 << (BITS - 1)) : 0.0f;
+        if constexpr (BITS == 8) k[tau] = bitcast<u4v>(unpack8(w[tau][2 * j], w[tau][2 * j + 1], off));
+        else if constexpr (BITS == 4) k[tau] = bitcast<u4v>(unpack4(w[tau][j], off));
+        else k[tau] = bitcast<u4v>(unpack2_half(w[tau][j >> 1] >> (8 * (j & 1)), off));
+      }
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int c = 2 * j + h;
+      float x[8];
+#pragma unroll
+      for (int tau = 0; tau < 2; ++tau) {
+        const f4 t = mfma16<HALF>(k[tau], sel[h], f4{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          float y = t[r];
+          if constexpr (BITS == 16) {
+            // (an infinite or NaN key makes the products of all 16 columns infinite or NaN)
+            if (h == 0) nan = __builtin_fmaf(y, 0.0f, nan);
+          } else if constexpr (QS == kQsSym) {
+            y *= rs[4 * tau + r];
+          } else if constexpr (QS == kQsG64) {
+            y = __builtin_fmaf(y, (float)sz[tau][c / 4][r], (float)sz[tau][c / 4][4 + r]);
+          }
+          x[4 * tau + r] = y;
+        }
+      }
+      lo[c] = hi[c] = x[0];
+#pragma unroll
+      for (int e = 1; e < 8; ++e) {
+        lo[c] = fminf(lo[c], x[e]);
+        hi[c] = fmaxf(hi[c], x[e]);
+      }
+    }
+  }
+  rows_scatter(lo, [](float x, float y) { return fminf(x, y); });
+  rows_scatter(hi, [](float x, float y) { return fmaxf(x, y); });
+  double mid[NV], half[NV];
+#pragma unroll
+  for (int v = 0; v < NV; ++v) {
+    float x = lo[v], y = hi[v];
+    if constexpr (BITS != 16 && QS == kQsKivi) {
+      x = __builtin_fmaf(x, ks[v], kz[v]);
+      y = __builtin_fmaf(y, ks[v], kz[v]);
+      nan = __builtin_fmaf(x, 0.0f, __builtin_fmaf(y, 0.0f, nan));
+    }
+    mid[v] = 0.5 * ((double)x + (double)y);
+    half[v] = 0.5 * ((double)y - (double)x);
+  }
+  if (__any(bad || nan != 0.0f)) {  // (NaN)
+#pragma unroll
+    for (int v = 0; v < NV; ++v) mid[v] = half[v] = 0.0;
+    bad = true;
+  } else {
+    bad = false;
+  }
+  int cm[NV], ch[NV];
+  const float sm = eight_bits(mid, cm);
+  float sh = eight_bits(half, ch);
+  if (bad) sh = INFINITY;
+
+  // Four lanes' bytes to a word each; of a quad's 2 NV words each lane stores some.
+  const int64_t row = ((int64_t)S.mult * a.g.Hkv + kvh) * a.nb_cap + blk;
+  uint8_t* out = a.index + L.index + S.index;
+  uint32_t words[2 * NV];
+#pragma unroll
+  for (int i = 0; i < 2 * NV; ++i) {
+    uint32_t x = (uint32_t)(uint8_t)(i < NV ? cm[i % NV] : ch[i % NV]) << (8 * (n & 3));
+    x |= (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, kQuadXor1, 0xF, 0xF, false);
+    x |= (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, kQuadXor2, 0xF, 0xF, false);
+    words[i] = x;
+  }
+  const int i = n & 3;
+  if (i < 2 * NV) {
+    const uint32_t x = i == 0 ? words[0] : (i == 1 ? words[1] : (i == 2 ? words[NV > 1 ? 2 : 0] : words[NV > 1 ? 3 : 1]));
+    const int v = i % NV, part = i / NV;
+    *reinterpret_cast<uint32_t*>(out + row * 2 * D + part * D + (channel(v) & ~3)) = x;
+  }
+  if (lane == 0) *reinterpret_cast<float2*>(out + a.scales + row * 8) = make_float2(sm, sh);
+}
+
+// ---------------------------------------------------------------------------
+// Choice
+// ---------------------------------------------------------------------------
+
+struct SelectArgs {
+  const uint8_t* index;
+  const uint16_t* q;   // [nl][B][Hq][D]
+  int32_t* blocks;     // [nl][B][Hkv][n_select]
+  uint32_t* keys;      // [rows of the launch][nb_cap], in the workspace
+  int64_t scales;
+  int32_t nb_cap, B, Hq, G, n_select, n_first, n_recent;
+  int32_t chunk;       // blocks that a workgroup of score_kernel scores
+  Group g;
+};
+static_assert(sizeof(SelectArgs) <= 4096, "kernel arguments");
+
+constexpr int kThreads = 256, kWaves = 4;
+constexpr int kBins = 256;
+
+typedef int i4v __attribute__((ext_vector_type(4)));
+
+// A score as an unsigned key of the same order (-0 equal to 0); never 0.
+__device__ __forceinline__ uint32_t key_of(float x) {
+  const uint32_t b = __float_as_uint(x + 0.0f);
+  return b & 0x80000000u ? ~b : b | 0x80000000u;
+}
+
+// The heads of a (layer, sequence, KV head) in 8 bits, [q | |q|] per row, and their scales.
+template <int D, int T>
+struct Queries {
+  static constexpr int kStride = 2 * D + 16;  // (bytes; rows apart in the banks)
+  uint8_t rows[16 * T * kStride];
+  float scale[16 * T];
+
+  __device__ __forceinline__ void fill(const uint16_t* q, int G, int lane, int wave) {
+    for (int h = wave; h < 16 * T; h += kWaves) {
+      float x[D / 64];
+      bool odd = false;
+#pragma unroll
+      for (int i = 0; i < D / 64; ++i) {
+        const uint16_t b = h < G ? q[h * D + lane * (D / 64) + i] : 0;
+        odd |= (b & 0x7f80u) == 0x7f80u;
+        x[i] = bf16_to_f32(b);
+      }
+      float top = 0.0f;
+#pragma unroll
+      for (int i = 0; i < D / 64; ++i) top = fmaxf(top, __builtin_fabsf(x[i]));
+      top = rows_max(max16(top));
+      const float s = __any(odd) ? 0.0f : top / 127.0f;
+      if (lane == 0) scale[h] = s;
+#pragma unroll
+      for (int i = 0; i < D / 64; ++i) {
+        const int c = s > 0.0f ? (int)rintf(x[i] / s) : 0;
+        rows[h * kStride + lane * (D / 64) + i] = (uint8_t)c;
+        rows[h * kStride + D + lane * (D / 64) + i] = (uint8_t)(c < 0 ? -c : c);
+      }
+    }
+  }
+};
+
+// Scores of blocks [b0, b1) as keys into out[b]; the waves of a workgroup share them, sixteen blocks at
+// a time: block b0 + lane % 16 is the lane's column of the products, head 4 (lane / 16) + r of a tile its row r.
+template <int D, int T>
+__device__ __forceinline__ void score(const Queries<D, T>& qs, const uint8_t* codes, const float2* scales, int G, int b0,
+                                      int b1, uint32_t* out, int lane, int wave) {
+  constexpr int NK = D / 64;  // products of a part
+  const int col = lane & 15, kg = lane >> 4;
+  const auto load_rows = [&](i4v (&x)[2 * NK], int t) {
+#pragma unroll
+    for (int k = 0; k < 2 * NK; ++k)
+      x[k] = *reinterpret_cast<const i4v*>(qs.rows + (16 * t + col) * Queries<D, T>::kStride + 64 * k + 16 * kg);
+  };
+  i4v q0[2 * NK];
+  load_rows(q0, 0);
+  f4 sq0;
+#pragma unroll
+  for (int r = 0; r < 4; ++r) sq0[r] = qs.scale[4 * kg + r];
+  constexpr int N = 2;  // groups of sixteen in flight
+  for (int base = b0 + 16 * N * wave; base < b1; base += 16 * N * kWaves) {
+    i4v m[N][2 * NK];
+    float2 s[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int64_t b = min(base + 16 * i + col, b1 - 1);
+#pragma unroll
+      for (int k = 0; k < 2 * NK; ++k) m[i][k] = *reinterpret_cast<const i4v*>(codes + b * 2 * D + 64 * k + 16 * kg);
+      s[i] = scales[b];
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      float best = -INFINITY;
+#pragma unroll
+      for (int t = 0; t < T; ++t) {
+        i4v q[2 * NK];
+        f4 sq = sq0;
+        if (T == 1 || t == 0) {
+#pragma unroll
+          for (int k = 0; k < 2 * NK; ++k) q[k] = q0[k];
+        } else {
+          load_rows(q, t);
+#pragma unroll
+          for (int r = 0; r < 4; ++r) sq[r] = qs.scale[16 * t + 4 * kg + r];
+        }
+        i4v dm = {0, 0, 0, 0}, dh = {0, 0, 0, 0};
+#pragma unroll
+        for (int k = 0; k < NK; ++k) {
+          dm = __builtin_amdgcn_mfma_i32_16x16x64_i8(q[k], m[i][k], dm, 0, 0, 0);
+          dh = __builtin_amdgcn_mfma_i32_16x16x64_i8(q[NK + k], m[i][NK + k], dh, 0, 0, 0);
+        }
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          // one rounding each, in this order (whole numbers below 2^24 are exact)
+          float x = __builtin_fmaf((float)dm[r], s[i].x, (float)dh[r] * s[i].y) * sq[r];
+          x = x != x ? INFINITY : x;  // a block with infinite or NaN keys comes first
+          if (16 * t + 4 * kg + r < G) best = fmaxf(best, x);
+        }
+      }
+      best = rows_max(best);
+      const int b = base + 16 * i + col;
+      if (kg == 0 && b < b1) out[b] = key_of(best);
+    }
+  }
+}
+
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t dpp_add(uint32_t x) {
+  return x + (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, ROWS, 0xF, false);
+}
+// Inclusive prefix sum over the wave.
+__device__ __forceinline__ uint32_t wave_scan(uint32_t x) {
+  x = dpp_add<0x111, 0xF>(x);  // row_shr 1, 2, 4, 8: within 16 lanes
+  x = dpp_add<0x112, 0xF>(x);
+  x = dpp_add<0x114, 0xF>(x);
+  x = dpp_add<0x118, 0xF>(x);
+  x = dpp_add<0x142, 0xA>(x);  // the last lane of a row to the next row
+  return dpp_add<0x143, 0xC>(x);  // ... of the first half to the second
+}
+__device__ __forceinline__ uint32_t wave_umax(uint32_t x) {
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) x = max(x, (uint32_t)__shfl_xor((int)x, d));
+  return x;
+}
+
+struct Choice {
+  uint32_t hist[kBins];
+  uint32_t wave[2][kWaves];
+  uint32_t found[3];
+};
+
+// Writes a row's list: blocks before n_first, the `want` blocks of [n_first, end) with the largest
+// keys (equal ones: the lower block), blocks end .. nb - 1, and -1 up to n_select.  key(b): of a block.
+template <class Key>
+__device__ __forceinline__ void choose(Choice& sh, Key key, int nb, int n_select, int n_first, int n_recent, int32_t* out,
+                                       int tid) {
+  const int lane = tid & 63, wave = tid >> 6;
+  if (nb <= n_select) {
+    for (int i = tid; i < n_select; i += kThreads) out[i] = i < nb ? i : -1;
+    return;
+  }
+  const int end = nb - n_recent, want = n_select - n_first - n_recent;
+  for (int i = tid; i < n_first; i += kThreads) out[i] = i;
+  for (int i = tid; i < n_recent; i += kThreads) out[n_first + want + i] = end + i;
+  if (want == 0) return;
+  // The largest and the smallest key: digits start where they differ.
+  uint32_t top = 0, low = 0;  // low: of the complements
+  for (int b = n_first + tid; b < end; b += kThreads) {
+    const uint32_t k = key(b);
+    top = max(top, k);
+    low = max(low, ~k);
+  }
+  top = wave_umax(top);
+  low = wave_umax(low);
+  if (lane == 0) {
+    sh.wave[0][wave] = top;
+    sh.wave[1][wave] = low;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    top = max(top, sh.wave[0][w]);
+    low = max(low, sh.wave[1][w]);
+  }
+  uint32_t base = ~low, need = want;  // keys of [base, base + 2^bits) hold the want-th largest
+  int bits = 32 - __clz((int)(top - base) | 1);
+  uint32_t cut, ties;  // keys above cut are chosen, and the first `ties` equal ones
+  while (true) {
+    const int shift = bits > 8 ? bits - 8 : 0;
+    __syncthreads();
+    sh.hist[tid] = 0;
+    __syncthreads();
+    for (int b = n_first + tid; b < end; b += kThreads) {
+      const uint32_t k = key(b), d = (k - base) >> shift;
+      if (k >= base && d < 1u << (bits < 8 ? bits : 8)) atomicAdd(&sh.hist[d], 1u);
+    }
+    __syncthreads();
+    // bins from the top: thread tid looks at bin 255 - tid
+    const uint32_t h = sh.hist[kBins - 1 - tid], incl = wave_scan(h);
+    if (lane == 63) sh.wave[0][wave] = incl;
+    __syncthreads();
+    uint32_t before = incl - h;
+    for (int w = 0; w < wave; ++w) before += sh.wave[0][w];
+    if (before < need && before + h >= need) {
+      sh.found[0] = kBins - 1 - tid;
+      sh.found[1] = need - before;
+      sh.found[2] = h;
+    }
+    __syncthreads();
+    base += sh.found[0] << shift;
+    need = sh.found[1];
+    if (need == sh.found[2]) {  // the whole bin
+      cut = base - 1;           // (a key is never 0)
+      ties = 0;
+      break;
+    }
+    if (shift == 0) {
+      cut = base;
+      ties = need;
+      break;
+    }
+    bits = shift;
+  }
+  // In order: each wave takes a run of blocks.
+  const int count = end - n_first, run = (count + 64 * kWaves - 1) / (64 * kWaves) * 64;
+  const int r0 = n_first + wave * run, r1 = min(end, r0 + run);
+  uint32_t na = 0, ne = 0;
+  for (int b0 = r0; b0 < r1; b0 += 64) {
+    const uint32_t k = b0 + lane < r1 ? key(b0 + lane) : 0u;
+    na += __popcll(__ballot(k > cut));
+    ne += __popcll(__ballot(b0 + lane < r1 && k == cut));
+  }
+  __syncthreads();
+  if (lane == 0) {
+    sh.wave[0][wave] = na;
+    sh.wave[1][wave] = ne;
+  }
+  __syncthreads();
+  uint32_t above = 0, equal = 0;
+  for (int w = 0; w < wave; ++w) {
+    above += sh.wave[0][w];
+    equal += sh.wave[1][w];
+  }
+  uint32_t left = ties - min(equal, ties), at = n_first + above + min(equal, ties);
+  const auto below = [](uint64_t m, uint32_t x) {  // bits of m below the lane's own, added to x
+    return __builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, x));
+  };
+  for (int b0 = r0; b0 < r1; b0 += 64) {
+    const bool has = b0 + lane < r1;
+    const uint32_t k = has ? key(b0 + lane) : 0u;
+    bool kept = has && k > cut;
+    const uint64_t e = __ballot(has && k == cut);
+    if (e && left) {
+      kept |= has && k == cut && below(e, 0) < left;
+      left -= min(left, (uint32_t)__popcll(e));
+    }
+    const uint64_t m = __ballot(kept);
+    if (kept) out[below(m, at)] = b0 + lane;
+    at += __popcll(m);
+  }
+}
+
+// The launch's row: layer, sequence and KV head.
+struct Row {
+  int layer, seq, kvh;
+};
+__device__ __forceinline__ Row row_of(const Group& g, uint32_t x) {
+  const uint32_t kvh = x % (uint32_t)g.Hkv, y = x / (uint32_t)g.Hkv;
+  return Row{(int)(y / (uint32_t)g.n_seqs), (int)(y % (uint32_t)g.n_seqs), (int)kvh};
+}
+
+template <int D, int T>
+__global__ __launch_bounds__(kThreads) void select_kernel(SelectArgs a) {
+  __shared__ __align__(16) Queries<D, T> qs;
+  __shared__ Choice sh;
+  extern __shared__ uint32_t keys[];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const Row r = row_of(a.g, blockIdx.x);
+  const GroupLayer& L = a.g.layers[r.layer];
+  const GroupSeq& S = a.g.seqs[r.seq];
+  const int nb = S.stored >> 5;
+  const int64_t call_row = (int64_t)L.layer * a.B + S.seq;
+  if (nb > a.n_select) {
+    qs.fill(a.q + (call_row * a.Hq + r.kvh * a.G) * D, a.G, lane, wave);
+    __syncthreads();
+    const uint8_t* index = a.index + L.index + S.index;
+    const int64_t row = ((int64_t)S.mult * a.g.Hkv + r.kvh) * a.nb_cap;
+    score<D, T>(qs, index + row * 2 * D, reinterpret_cast<const float2*>(index + a.scales) + row, a.G, a.n_first,
+                nb - a.n_recent, keys, lane, wave);
+    __syncthreads();
+  }
+  choose(sh, [&](int b) { return keys[b]; }, nb, a.n_select, a.n_first, a.n_recent,
+         a.blocks + (call_row * a.g.Hkv + r.kvh) * a.n_select, tid);
+}
+
+template <int D, int T>
+__global__ __launch_bounds__(kThreads) void score_kernel(SelectArgs a) {
+  __shared__ __align__(16) Queries<D, T> qs;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const Row r = row_of(a.g, blockIdx.y);
+  const GroupLayer& L = a.g.layers[r.layer];
+  const GroupSeq& S = a.g.seqs[r.seq];
+  const int nb = S.stored >> 5;
+  const int b0 = a.n_first + blockIdx.x * a.chunk, b1 = min(nb - a.n_recent, b0 + a.chunk);
+  if (nb <= a.n_select || b0 >= b1) return;
+  qs.fill(a.q + (((int64_t)L.layer * a.B + S.seq) * a.Hq + r.kvh * a.G) * D, a.G, lane, wave);
+  __syncthreads();
+  const uint8_t* index = a.index + L.index + S.index;
+  const int64_t row = ((int64_t)S.mult * a.g.Hkv + r.kvh) * a.nb_cap;
+  score<D, T>(qs, index + row * 2 * D, reinterpret_cast<const float2*>(index + a.scales) + row, a.G, b0, b1,
+              a.keys + (int64_t)blockIdx.y * a.nb_cap, lane, wave);
+}
+
+__global__ __launch_bounds__(kThreads) void choose_kernel(SelectArgs a) {
+  __shared__ Choice sh;
+  const Row r = row_of(a.g, blockIdx.x);
+  const GroupLayer& L = a.g.layers[r.layer];
+  const GroupSeq& S = a.g.seqs[r.seq];
+  const uint32_t* keys = a.keys + (int64_t)blockIdx.x * a.nb_cap;
+  choose(sh, [&](int b) { return keys[b]; }, S.stored >> 5, a.n_select, a.n_first, a.n_recent,
+         a.blocks + (((int64_t)L.layer * a.B + S.seq) * a.g.Hkv + r.kvh) * a.n_select, threadIdx.x);
+}
+
+}  // namespace
+
+using namespace kvk;
+
+namespace {
+
+constexpr int kResident = 8192;  // keys of a row in LDS
+constexpr int64_t kFewRows = 512;
+constexpr int kLongRow = 1024;
+
+// Whether rows of up to nb blocks go through the workspace.
+bool in_two(int64_t rows, int64_t nb) { return nb > kResident || (rows < kFewRows && nb >= kLongRow); }
+
+kvk_status check_call(const kvk_table* t, const char* what, int32_t l0, int32_t l1) {
+  if (!t) return fail(KVK_ERR_INVALID, "%s: NULL table", what);
+  if (t->d.kind != KVK_GQA) return fail(KVK_ERR_UNSUPPORTED, "%s: GQA tables only", what);
+  if (l0 < 0 || l1 > t->d.n_layers || l0 >= l1)
+    return fail(KVK_ERR_INVALID, "layer range [%d, %d) invalid for %d layers", l0, l1, t->d.n_layers);
+  return KVK_OK;
+}
+
+kvk_status check_lengths(const kvk_table* t, const char* what, const char* name, const int32_t* n, const int32_t* most) {
+  for (int b = 0; b < t->d.batch; ++b) {
+    const int32_t top = most ? most[b] : t->cap;
+    if (n[b] < 0 || n[b] > top) return fail(KVK_ERR_INVALID, "%s: %s[%d] = %d outside 0..%d", what, name, b, n[b], top);
+  }
+  return KVK_OK;
+}
+
+const kvk_table* first_of(const kvk_table* t) { return t->seq.empty() ? t : t->seq[0]; }
+
+template <int D, int QS>
+void launch_index(int bits, dim3 g, const IndexArgs& a, hipStream_t st) {
+  const dim3 b(256);
+  if (bits == 16) hipLaunchKernelGGL((index_kernel<D, 16, kQsKivi>), g, b, 0, st, a);
+  else if (bits == 8) hipLaunchKernelGGL((index_kernel<D, 8, QS>), g, b, 0, st, a);
+  else if (bits == 4) hipLaunchKernelGGL((index_kernel<D, 4, QS>), g, b, 0, st, a);
+  else hipLaunchKernelGGL((index_kernel<D, 2, QS>), g, b, 0, st, a);
+}
+template <int D>
+void launch_index(int qs, int bits, dim3 g, const IndexArgs& a, hipStream_t st) {
+  if (qs == KVK_Q_KIVI32) launch_index<D, kQsKivi>(bits, g, a, st);
+  else if (qs == KVK_Q_GROUP64) launch_index<D, kQsG64>(bits, g, a, st);
+  else launch_index<D, kQsSym>(bits, g, a, st);
+}
+
+template <int D, int T>
+void launch_select(const SelectArgs& a, uint32_t rows, int32_t nb, bool two, hipStream_t st) {
+  const dim3 b(kThreads);
+  if (!two) {
+    hipLaunchKernelGGL((select_kernel<D, T>), dim3(rows), b, nb > a.n_select ? 4 * (size_t)nb : 0, st, a);
+  } else {
+    const int32_t n = nb - a.n_first - a.n_recent;
+    hipLaunchKernelGGL((score_kernel<D, T>), dim3((n + a.chunk - 1) / a.chunk, rows), b, 0, st, a);
+    hipLaunchKernelGGL(choose_kernel, dim3(rows), b, 0, st, a);
+  }
+}
+template <int D>
+void launch_select(const SelectArgs& a, uint32_t rows, int32_t nb, bool two, hipStream_t st) {
+  if (a.G <= 16) launch_select<D, 1>(a, rows, nb, two, st);
+  else if (a.G <= 32) launch_select<D, 2>(a, rows, nb, two, st);
+  else launch_select<D, 4>(a, rows, nb, two, st);
+}
+
+}  // namespace
+
+extern "C" kvk_status kvk_index_bytes(const kvk_table* t, size_t* out) {
+  const char* what = "kvk_index_bytes";
+  if (kvk_status st = check_call(t, what, 0, t ? t->d.n_layers : 0)) return st;
+  if (!out) return fail(KVK_ERR_INVALID, "%s: NULL output", what);
+  int64_t n = t->seq.empty() ? index_total(t) : 0;
+  for (const kvk_table* s : t->seq) n += round256(index_total(s));
+  *out = (size_t)std::max<int64_t>(n, 256);
+  return KVK_OK;
+}
+
+extern "C" kvk_status kvk_index_part(const kvk_table* t, int32_t sequence, int32_t layer, int64_t* codes, int64_t* scales) {
+  const char* what = "kvk_index_part";
+  if (kvk_status st = check_call(t, what, layer, layer < 0x7fffffff ? layer + 1 : layer)) return st;
+  if (!codes || !scales) return fail(KVK_ERR_INVALID, "%s: NULL output", what);
+  if (sequence < 0 || sequence >= (t->seq.empty() ? 1 : t->d.batch))
+    return fail(KVK_ERR_INVALID, "%s: sequence %d (0 for a table of one plan)", what, sequence);
+  int64_t at = 0;
+  const kvk_table* s = t;
+  if (!t->seq.empty()) {
+    for (int b = 0; b < sequence; ++b) at += round256(index_total(t->seq[b]));
+    s = t->seq[sequence];
+  }
+  *codes = at + index_offset(s, s->info.anchor_of[layer]);
+  *scales = *codes + index_codes_bytes(s);
+  return KVK_OK;
+}
+
+extern "C" kvk_status kvk_index_blocks(const kvk_table* t, int32_t l0, int32_t l1, const int32_t* n_indexed,
+                                       const int32_t* n_stored, const void* arena, void* index, hipStream_t stream) {
+  const char* what = "kvk_index_blocks";
+  if (kvk_status st = check_call(t, what, l0, l1)) return st;
+  const kvk_dims& d = t->d;
+  if (!n_stored || !arena || !index) return fail(KVK_ERR_INVALID, "%s: NULL buffer", what);
+  if (kvk_status st = check_lengths(t, what, "n_stored", n_stored, nullptr)) return st;
+  if (n_indexed)
+    if (kvk_status st = check_lengths(t, what, "n_indexed", n_indexed, n_stored)) return st;
+  if ((reinterpret_cast<uintptr_t>(arena) & 15) || (reinterpret_cast<uintptr_t>(index) & 255))
+    return fail(KVK_ERR_INVALID, "%s: misaligned buffer (arena 16 B, index 256 B)", what);
+  bool any = false;
+  for (int b = 0; b < d.batch; ++b) any |= n_stored[b] / 32 > (n_indexed ? n_indexed[b] / 32 : 0);
+  if (!any) return KVK_OK;
+  if (d.n_kv_heads > 65535) return fail(KVK_ERR_UNSUPPORTED, "%s: %d KV heads", what, d.n_kv_heads);
+  if (kvk_status st = check_gpu_buffers({arena, index}, what)) return st;
+  IndexArgs a;
+  a.arena = static_cast<const uint8_t*>(arena);
+  a.index = static_cast<uint8_t*>(index);
+  a.scales = index_codes_bytes(first_of(t));
+  a.nb_cap = t->nb_cap;
+  for (const bool go : {false, true}) {
+    const kvk_status st = for_groups(
+        t, l0, l1, true, true, a.g,
+        [&](int b, GroupSeq& s) {
+          s.stored = n_stored[b];
+          s.first = n_indexed ? n_indexed[b] / 32 : 0;
+          return s.stored / 32 > s.first;
+        },
+        [&](int bits, Group& g) -> kvk_status {
+          int64_t most = 0;
+          for (int i = 0; i < g.n_seqs; ++i) most = std::max<int64_t>(most, g.seqs[i].stored / 32 - g.seqs[i].first);
+          a.block_bytes = (int32_t)gqa_block_bytes(d.head_dim, bits, d.qscheme);
+          const dim3 grid((unsigned)((most + 3) / 4), (unsigned)d.n_kv_heads, (unsigned)(g.n_layers * g.n_seqs));
+          if ((int64_t)grid.x * grid.y * grid.z > 0xffffffLL) return fail(KVK_ERR_UNSUPPORTED, "%s: grid too large", what);
+          if (!go) return KVK_OK;
+          if (d.head_dim == 128) launch_index<128>(d.qscheme, bits, grid, a, stream);
+          else launch_index<64>(d.qscheme, bits, grid, a, stream);
+          const hipError_t e = hipGetLastError();
+          if (e != hipSuccess) return fail(KVK_ERR_DEVICE, "%s launch: %s", what, hipGetErrorString(e));
+          return KVK_OK;
+        });
+    if (st != KVK_OK) return st;
+  }
+  return KVK_OK;
+}
+
+extern "C" kvk_status kvk_select_workspace_bytes(const kvk_table* t, int32_t l0, int32_t l1, size_t* out) {
+  const char* what = "kvk_select_workspace_bytes";
+  if (kvk_status st = check_call(t, what, l0, l1)) return st;
+  if (!out) return fail(KVK_ERR_INVALID, "%s: NULL output", what);
+  const int64_t all = (int64_t)(l1 - l0) * t->d.batch * t->d.n_kv_heads;
+  // launches run one after another and share the workspace
+  const int64_t rows = (int64_t)(l1 - l0) * std::min<int64_t>(t->d.batch, kGroupSeqs) * t->d.n_kv_heads;
+  *out = in_two(all, t->nb_cap) ? (size_t)round256(rows * t->nb_cap * 4) : 0;
+  return KVK_OK;
+}
+
+extern "C" kvk_status kvk_select_blocks(const kvk_table* t, int32_t l0, int32_t l1, const void* q, const int32_t* n_stored,
+                                        int32_t n_select, int32_t n_first, int32_t n_recent, const void* index,
+                                        int32_t* blocks, void* workspace, size_t ws_bytes, hipStream_t stream) {
+  const char* what = "kvk_select_blocks";
+  if (kvk_status st = check_call(t, what, l0, l1)) return st;
+  const kvk_dims& d = t->d;
+  if (!q || !n_stored || !index || !blocks) return fail(KVK_ERR_INVALID, "%s: NULL buffer", what);
+  if (n_select < 1) return fail(KVK_ERR_INVALID, "%s: n_select %d", what, n_select);
+  if (n_first < 0 || n_recent < 0 || n_first > n_select || n_recent > n_select - n_first)
+    return fail(KVK_ERR_INVALID, "%s: %d first and %d recent blocks of %d", what, n_first, n_recent, n_select);
+  if (kvk_status st = check_lengths(t, what, "n_stored", n_stored, nullptr)) return st;
+  if ((reinterpret_cast<uintptr_t>(q) & 15) || (reinterpret_cast<uintptr_t>(index) & 255) ||
+      (reinterpret_cast<uintptr_t>(blocks) & 3) || (reinterpret_cast<uintptr_t>(workspace) & 255))
+    return fail(KVK_ERR_INVALID, "%s: misaligned buffer (q 16 B, index and workspace 256 B, blocks 4 B)", what);
+  int32_t nb = 0;
+  for (int b = 0; b < d.batch; ++b) nb = std::max(nb, n_stored[b] / 32);
+  const int64_t all = (int64_t)(l1 - l0) * d.batch * d.n_kv_heads;
+  const bool two = nb > n_select && in_two(all, nb);
+  if (two) {
+    size_t need = 0;
+    if (kvk_status st = kvk_select_workspace_bytes(t, l0, l1, &need)) return st;
+    if (!workspace) return fail(KVK_ERR_INVALID, "%s: NULL workspace", what);
+    if (ws_bytes < need) return fail(KVK_ERR_BUFFER, "%s: workspace %zu bytes < %zu needed", what, ws_bytes, need);
+  }
+  if (kvk_status st = check_gpu_buffers({q, index, blocks, two ? workspace : nullptr}, what)) return st;
+  SelectArgs a;
+  a.index = static_cast<const uint8_t*>(index);
+  a.q = static_cast<const uint16_t*>(q);
+  a.blocks = blocks;
+  a.keys = static_cast<uint32_t*>(workspace);
+  a.scales = index_codes_bytes(first_of(t));
+  a.nb_cap = t->nb_cap;
+  a.B = d.batch;
+  a.Hq = d.n_q_heads;
+  a.G = d.n_q_heads / d.n_kv_heads;
+  a.n_select = n_select;
+  a.n_first = n_first;
+  a.n_recent = n_recent;
+  a.chunk = 512;
+  for (const bool go : {false, true}) {
+    const kvk_status st = for_groups(
+        t, l0, l1, false, false, a.g,
+        [&](int b, GroupSeq& s) {
+          s.stored = n_stored[b];
+          return true;
+        },
+        [&](int, Group& g) -> kvk_status {
+          const int64_t rows = (int64_t)g.n_layers * g.n_seqs * d.n_kv_heads;
+          int32_t most = 0;
+          for (int i = 0; i < g.n_seqs; ++i) most = std::max(most, g.seqs[i].stored / 32);
+          const bool split = two && most > n_select;
+          if (rows > (split ? 65535 : 0xffffff) || (split && (int64_t)most / a.chunk * rows > 0xfffff0))
+            return fail(KVK_ERR_UNSUPPORTED, "%s: grid too large", what);
+          if (!go) return KVK_OK;
+          if (d.head_dim == 128) launch_select<128>(a, (uint32_t)rows, most, split, stream);
+          else launch_select<64>(a, (uint32_t)rows, most, split, stream);
+          const hipError_t e = hipGetLastError();
+          if (e != hipSuccess) return fail(KVK_ERR_DEVICE, "%s launch: %s", what, hipGetErrorString(e));
+          return KVK_OK;
+        });
+    if (st != KVK_OK) return st;
+  }
+  return KVK_OK;
+}

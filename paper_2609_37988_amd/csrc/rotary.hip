@@ -1,0 +1,360 @@
+// Rotary positions of queries and keys, before they are written to or attend to the caches.
+//
+//   pair (a, b) of a row at position p, frequency f:  (a cos pf - b sin pf, b cos pf + a sin pf) m
+//
+// Angles.  p f grows with the position and only its part past the last whole turn counts, of which
+// fp32 would keep nothing at far positions.  A frequency is held as a 64-bit fraction of a turn,
+// so that p f modulo one turn is the low 64 bits of an integer product (exact to p 2^-65 turns, any
+// 32-bit position, negative ones too).  Its two top bits name the quadrant; the rest, an angle
+// within an eighth of a turn, goes through the Taylor polynomials of sine (to x^9) and cosine (to
+// x^10), whose first terms left out are below 2^-29 and 2^-33.
+//
+// A thread turns U pairs of one token in every head of a run of heads, so that its sines and
+// cosines are formed once.
+//
+// Bound.  HBM: each value read once and written once.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <new>
+#include <utility>
+
+#include "kvk_device.h"
+#include "kvk_internal.h"
+
+using namespace kvkd;
+
+namespace {
+
+constexpr int kMaxPairs = 256;  // of a rotated part of 512 channels
+constexpr int kMaxRows = 4;     // tensors of a call
+constexpr int kThreads = 256;
+
+struct RowsArg {
+  const uint8_t* in;
+  uint8_t* out;
+  int64_t in_seq, in_head, in_token, out_seq, out_head, out_token;  // bytes
+  int32_t heads, first;  // first: the first channel that turns
+  int32_t below, above;  // channels copied before it and after the last one, in pieces of eight
+  int32_t units;         // of a row: pieces of U pairs, then the copied ones
+  int32_t y0, run;       // grid rows before this tensor, heads of a thread
+};
+
+struct RotateArgs {
+  RowsArg rows[kMaxRows];
+  const int32_t* positions;
+  uint32_t n_rows, n_tokens, total;  // tensors, tokens of a sequence, tokens of all
+  uint32_t pos_seqs;
+  int32_t turning;   // pieces of U pairs of a row
+  int32_t half;      // pairs of a row
+  float cos_factor, sin_factor;
+  uint64_t phase[kMaxPairs];
+};
+static_assert(sizeof(RotateArgs) <= 4096, "kernel arguments");
+
+// cos and sin of a fraction of a turn.
+__device__ __forceinline__ void turn(uint64_t fraction, float& c, float& s) {
+  const uint64_t p = fraction + (1ull << 61);  // quadrants centred on the axes
+  const uint32_t quadrant = (uint32_t)(p >> 62);
+  const float x = (float)(int32_t)((uint32_t)(p >> 30) ^ 0x80000000u) * 3.6572952e-10f;  // pi / 2 / 2^32
+  const float y = x * x;
+  float sn = __builtin_fmaf(y, 1.0f / 362880.0f, -1.0f / 5040.0f);
+  sn = __builtin_fmaf(y, sn, 1.0f / 120.0f);
+  sn = __builtin_fmaf(y, sn, -1.0f / 6.0f);
+  sn = __builtin_fmaf(x * y, sn, x);
+  float cs = __builtin_fmaf(y, -1.0f / 3628800.0f, 1.0f / 40320.0f);
+  cs = __builtin_fmaf(y, cs, -1.0f / 720.0f);
+  cs = __builtin_fmaf(y, cs, 1.0f / 24.0f);
+  cs = __builtin_fmaf(y, cs, -0.5f);
+  cs = __builtin_fmaf(y, cs, 1.0f);
+  const float a = quadrant & 1 ? sn : cs, b = quadrant & 1 ? cs : sn;
+  c = quadrant == 1 || quadrant == 2 ? -a : a;
+  s = quadrant >= 2 ? -b : b;
+}
+
+// N consecutive values as fp32, and back (rounded to nearest even).
+template <bool F32, int N>
+struct Piece {
+  static constexpr int W = F32 ? N : N / 2;  // words
+  uint32_t w[W];
+  __device__ __forceinline__ void load(const uint8_t* p) {
+    if constexpr (W == 2) {
+      const u2v x = *reinterpret_cast<const u2v*>(p);
+      w[0] = x[0]; w[1] = x[1];
+    } else {
+#pragma unroll
+      for (int i = 0; i < W / 4; ++i) {
+        const u4v x = reinterpret_cast<const u4v*>(p)[i];
+        w[4 * i] = x[0]; w[4 * i + 1] = x[1]; w[4 * i + 2] = x[2]; w[4 * i + 3] = x[3];
+      }
+    }
+  }
+  __device__ __forceinline__ void store(uint8_t* p) const {
+    if constexpr (W == 2) {
+      *reinterpret_cast<u2v*>(p) = u2v{w[0], w[1]};
+    } else {
+#pragma unroll
+      for (int i = 0; i < W / 4; ++i)
+        reinterpret_cast<u4v*>(p)[i] = u4v{w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]};
+    }
+  }
+  __device__ __forceinline__ float get(int i) const {
+    if constexpr (F32) return __uint_as_float(w[i]);
+    else return __uint_as_float(i & 1 ? w[i >> 1] & 0xffff0000u : w[i >> 1] << 16);
+  }
+  __device__ __forceinline__ void set2(int i, float a, float b) {  // i even
+    if constexpr (F32) {
+      w[i] = __float_as_uint(a);
+      w[i + 1] = __float_as_uint(b);
+    } else {
+      w[i >> 1] = (uint32_t)f32_to_bf16_bits(a) | (uint32_t)f32_to_bf16_bits(b) << 16;
+    }
+  }
+};
+
+template <bool F32, bool PAIRS, int U>
+__global__ __launch_bounds__(kThreads) void rotate_kernel(RotateArgs a) {
+  constexpr int ES = F32 ? 4 : 2;
+  int t = 0;
+#pragma unroll
+  for (int i = 1; i < kMaxRows; ++i)
+    if (i < (int)a.n_rows && (int)blockIdx.y >= a.rows[i].y0) t = i;
+  const RowsArg& r = a.rows[t];
+  const uint32_t id = blockIdx.x * kThreads + threadIdx.x;
+  const uint32_t token = id / (uint32_t)r.units, unit = id - token * r.units;
+  if (token >= a.total) return;
+  const uint32_t seq = token / a.n_tokens, n = token - seq * a.n_tokens;
+  const int h0 = ((int)blockIdx.y - r.y0) * r.run, h1 = min(h0 + r.run, r.heads);
+  const uint8_t* in = r.in + seq * r.in_seq + n * r.in_token + h0 * r.in_head;
+  uint8_t* out = r.out + seq * r.out_seq + n * r.out_token + h0 * r.out_head;
+
+  if ((int)unit >= a.turning) {  // channels that do not turn, eight at a time
+    const int k = unit - a.turning, ch = k < r.below ? 8 * k : r.first + 2 * a.half + 8 * (k - r.below);
+    for (int h = h0; h < h1; ++h, in += r.in_head, out += r.out_head) {
+      Piece<F32, 8> x;
+      x.load(in + ch * ES);
+      x.store(out + ch * ES);
+    }
+    return;
+  }
+  const int pair = unit * U;
+  const int at0 = (r.first + (PAIRS ? 2 * pair : pair)) * ES, at1 = at0 + (PAIRS ? U : a.half) * ES;
+  const int32_t pos = a.positions[(seq % a.pos_seqs) * a.n_tokens + n];
+  float c[U], s[U];
+#pragma unroll
+  for (int i = 0; i < U; ++i) {
+    turn(a.phase[pair + i] * (uint64_t)(int64_t)pos, c[i], s[i]);
+    c[i] *= a.cos_factor;
+    s[i] *= a.sin_factor;
+  }
+  // four heads' loads in flight
+  for (int h = h0; h < h1; h += 4, in += 4 * r.in_head, out += 4 * r.out_head) {
+    Piece<F32, U> x[4], y[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (h + k < h1) {
+        x[k].load(in + k * r.in_head + at0);
+        y[k].load(in + k * r.in_head + at1);
+      }
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (h + k < h1) {
+        if constexpr (PAIRS) {  // x: the first U / 2 pairs, y: the others
+#pragma unroll
+          for (int i = 0; i < U; i += 2) {
+            const float p = x[k].get(i), q = x[k].get(i + 1), u = y[k].get(i), v = y[k].get(i + 1);
+            const int e = i / 2, f = (U + i) / 2;
+            x[k].set2(i, __builtin_fmaf(p, c[e], -q * s[e]), __builtin_fmaf(q, c[e], p * s[e]));
+            y[k].set2(i, __builtin_fmaf(u, c[f], -v * s[f]), __builtin_fmaf(v, c[f], u * s[f]));
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < U; i += 2) {
+            const float p = x[k].get(i), q = x[k].get(i + 1), u = y[k].get(i), v = y[k].get(i + 1);
+            x[k].set2(i, __builtin_fmaf(p, c[i], -u * s[i]), __builtin_fmaf(q, c[i + 1], -v * s[i + 1]));
+            y[k].set2(i, __builtin_fmaf(u, c[i], p * s[i]), __builtin_fmaf(v, c[i + 1], q * s[i + 1]));
+          }
+        }
+        x[k].store(out + k * r.out_head + at0);
+        y[k].store(out + k * r.out_head + at1);
+      }
+  }
+}
+
+}  // namespace
+
+struct kvk_rotary {
+  int32_t layout, width;
+  float magnitude;
+  uint64_t phase[kMaxPairs];
+};
+
+using namespace kvk;
+
+extern "C" kvk_status kvk_rotary_frequencies(int32_t width, double base, double factor, int32_t original_tokens,
+                                             double slow_turns, double fast_turns, double* out) {
+  const char* what = "kvk_rotary_frequencies";
+  if (width < 2 || width % 2) return fail(KVK_ERR_INVALID, "%s: width %d must be even and positive", what, width);
+  if (!(std::isfinite(base) && base > 0) || !(std::isfinite(factor) && factor > 0))
+    return fail(KVK_ERR_INVALID, "%s: base and factor must be positive and finite", what);
+  if (original_tokens < 0) return fail(KVK_ERR_INVALID, "%s: original_tokens %d", what, original_tokens);
+  if (original_tokens > 0 &&
+      !(std::isfinite(slow_turns) && std::isfinite(fast_turns) && slow_turns >= 0 && fast_turns > slow_turns))
+    return fail(KVK_ERR_INVALID, "%s: turns must satisfy 0 <= slow (%g) < fast (%g)", what, slow_turns, fast_turns);
+  if (!out) return fail(KVK_ERR_INVALID, "%s: NULL output", what);
+  for (int i = 0; i < width / 2; ++i) {
+    const double f = std::pow(base, -2.0 * i / width);
+    double kept = 0.0;
+    if (original_tokens > 0) {
+      const double turns = original_tokens * f / 6.283185307179586476925287;
+      kept = std::min(1.0, std::max(0.0, (turns - slow_turns) / (fast_turns - slow_turns)));
+    }
+    out[i] = f * kept + f / factor * (1.0 - kept);
+  }
+  return KVK_OK;
+}
+
+extern "C" kvk_status kvk_rotary_create(int32_t layout, int32_t width, const double* frequencies, double magnitude,
+                                        kvk_rotary** out) {
+  const char* what = "kvk_rotary_create";
+  if (layout != KVK_ROTARY_HALVES && layout != KVK_ROTARY_PAIRS)
+    return fail(KVK_ERR_INVALID, "%s: layout %d", what, layout);
+  if (width < 8 || width % 8 || width > 2 * kMaxPairs)
+    return fail(KVK_ERR_INVALID, "%s: width %d must be a multiple of 8 up to %d", what, width, 2 * kMaxPairs);
+  if (!frequencies || !out) return fail(KVK_ERR_INVALID, "%s: NULL argument", what);
+  if (!std::isfinite(magnitude) || std::fabs(magnitude) > 3.4e38)
+    return fail(KVK_ERR_INVALID, "%s: magnitude must be finite in fp32", what);
+  for (int i = 0; i < width / 2; ++i)
+    if (!std::isfinite(frequencies[i])) return fail(KVK_ERR_INVALID, "%s: frequency %d is not finite", what, i);
+  kvk_rotary* r = new (std::nothrow) kvk_rotary;
+  if (!r) return fail(KVK_ERR_INVALID, "%s: out of host memory", what);
+  r->layout = layout;
+  r->width = width;
+  r->magnitude = (float)magnitude;
+  for (int i = 0; i < width / 2; ++i) {
+    const long double turns = (long double)frequencies[i] / 6.283185307179586476925286766559L;
+    const long double part = turns - floorl(turns);
+    r->phase[i] = part < 1.0L ? (uint64_t)ldexpl(part, 64) : 0;
+  }
+  *out = r;
+  return KVK_OK;
+}
+
+extern "C" void kvk_rotary_destroy(kvk_rotary* r) { delete r; }
+
+namespace {
+
+// A tensor's places [n_seqs][heads][tokens] of rows of `width` elements; written ones may not overlap: of the
+// dimensions with more than one place, in the order of their strides, each steps over all before it.
+kvk_status check_rows(const char* what, int i, const char* side, const kvk_strides& s, int32_t width, int64_t n_seqs,
+                      int32_t heads, int32_t tokens, bool written) {
+  if (s.seq < 0 || s.head < 0 || s.token < 0 || s.seq % 8 || s.head % 8 || s.token % 8)
+    return fail(KVK_ERR_INVALID, "%s: %s strides (%lld, %lld, %lld) of tensor %d must be multiples of 8 elements", what, side,
+                (long long)s.seq, (long long)s.head, (long long)s.token, i);
+  std::pair<int64_t, int64_t> dims[3] = {{s.token, tokens}, {s.head, heads}, {s.seq, n_seqs}};
+  std::sort(dims, dims + 3);
+  __int128 extent = width;
+  bool apart = true;
+  for (const auto& [stride, count] : dims) {
+    if (count < 2) continue;
+    apart &= stride >= extent;
+    extent += (__int128)stride * (count - 1);
+  }
+  if (extent > ((__int128)1 << 60))
+    return fail(KVK_ERR_INVALID, "%s: %s strides of tensor %d reach beyond any memory", what, side, i);
+  if (written && !apart) return fail(KVK_ERR_INVALID, "%s: %s rows of tensor %d overlap", what, side, i);
+  return KVK_OK;
+}
+
+// Heads of a thread: long runs share the sines, short ones fill the GPU.  (Threads with one
+// head each; eight waves per SIMD are 2048 workgroups.)
+int run_of(int64_t threads, int32_t heads) {
+  const int64_t wgs = threads / kThreads;
+  return (int)std::min<int64_t>(heads, std::max<int64_t>(1, std::min<int64_t>(8, wgs / 2048)));
+}
+
+}  // namespace
+
+extern "C" kvk_status kvk_rotate(const kvk_rotary* rotary, int32_t n_seqs, int32_t n_tokens, const int32_t* positions,
+                                 int32_t pos_seqs, const kvk_rotary_rows* rows, int32_t n_rows, int32_t dtype,
+                                 int32_t inverse, hipStream_t stream) {
+  const char* what = "kvk_rotate";
+  if (!rotary || !rows) return fail(KVK_ERR_INVALID, "%s: NULL argument", what);
+  if (n_rows < 1 || n_rows > kMaxRows) return fail(KVK_ERR_INVALID, "%s: %d tensors (1..%d)", what, n_rows, kMaxRows);
+  if (dtype != KVK_BF16 && dtype != KVK_F32) return fail(KVK_ERR_INVALID, "%s: dtype %d", what, dtype);
+  if (n_seqs < 0 || n_tokens < 0) return fail(KVK_ERR_INVALID, "%s: %d sequences of %d tokens", what, n_seqs, n_tokens);
+  if (n_seqs == 0 || n_tokens == 0) return KVK_OK;
+  if (pos_seqs < 1 || n_seqs % pos_seqs)
+    return fail(KVK_ERR_INVALID, "%s: positions of %d sequences for %d", what, pos_seqs, n_seqs);
+  const int64_t total = (int64_t)n_seqs * n_tokens;
+  const bool f32 = dtype == KVK_F32;
+  const int es = f32 ? 4 : 2, width = rotary->width;
+  const int U = !f32 && width % 16 == 0 ? 8 : 4;
+  RotateArgs a;
+  a.positions = positions;
+  a.n_rows = n_rows;
+  a.n_tokens = n_tokens;
+  a.total = (uint32_t)total;
+  a.pos_seqs = pos_seqs;
+  a.half = width / 2;
+  a.turning = a.half / U;
+  a.cos_factor = rotary->magnitude;
+  a.sin_factor = inverse ? -rotary->magnitude : rotary->magnitude;
+  std::copy(rotary->phase, rotary->phase + a.half, a.phase);
+  int64_t gx = 0, gy = 0;
+  for (int i = 0; i < n_rows; ++i) {
+    const kvk_rotary_rows& x = rows[i];
+    if (!x.in || !x.out) return fail(KVK_ERR_INVALID, "%s: NULL buffer", what);
+    if (x.n_heads < 1 || x.head_dim < 8 || x.head_dim % 8 || x.head_dim > (1 << 20))
+      return fail(KVK_ERR_INVALID, "%s: %d heads of width %d (a positive multiple of 8)", what, x.n_heads, x.head_dim);
+    if (x.first < 0 || x.first % 8 || x.first > x.head_dim - width)
+      return fail(KVK_ERR_INVALID, "%s: channels %d .. of %d do not hold %d that turn (a multiple of 8 first)", what, x.first,
+                  x.head_dim, width);
+    if ((reinterpret_cast<uintptr_t>(x.in) & 15) || (reinterpret_cast<uintptr_t>(x.out) & 15))
+      return fail(KVK_ERR_INVALID, "%s: misaligned buffer (16 B)", what);
+    if (kvk_status st = check_rows(what, i, "in", x.in_strides, x.head_dim, n_seqs, x.n_heads, n_tokens, false)) return st;
+    if (kvk_status st = check_rows(what, i, "out", x.out_strides, x.head_dim, n_seqs, x.n_heads, n_tokens, true)) return st;
+    const bool in_place = x.in == x.out;
+    const kvk_strides &p = x.in_strides, &q = x.out_strides;
+    if (in_place && ((n_seqs > 1 && p.seq != q.seq) || (x.n_heads > 1 && p.head != q.head) || (n_tokens > 1 && p.token != q.token)))
+      return fail(KVK_ERR_INVALID, "%s: tensor %d in place with two layouts", what, i);
+    RowsArg& r = a.rows[i];
+    r.in = static_cast<const uint8_t*>(x.in);
+    r.out = static_cast<uint8_t*>(x.out);
+    r.in_seq = p.seq * es; r.in_head = p.head * es; r.in_token = p.token * es;
+    r.out_seq = q.seq * es; r.out_head = q.head * es; r.out_token = q.token * es;
+    r.heads = x.n_heads;
+    r.first = x.first;
+    r.below = in_place ? 0 : x.first / 8;
+    r.above = in_place ? 0 : (x.head_dim - x.first - width) / 8;
+    r.units = a.turning + r.below + r.above;
+    if (total * r.units > 0x7fffffffLL) return fail(KVK_ERR_UNSUPPORTED, "%s: %lld tokens in one call", what, (long long)total);
+    r.run = run_of(total * r.units * x.n_heads, x.n_heads);
+    r.y0 = (int32_t)gy;
+    gy += (x.n_heads + r.run - 1) / r.run;
+    gx = std::max(gx, (total * r.units + kThreads - 1) / kThreads);
+  }
+  if (!positions) return fail(KVK_ERR_INVALID, "%s: NULL buffer", what);
+  if (reinterpret_cast<uintptr_t>(positions) & 3) return fail(KVK_ERR_INVALID, "%s: misaligned positions (4 B)", what);
+  if (gy > 65535 || gx * gy * kThreads > 0xffffffffLL)  // (a grid has less than 2^32 threads)
+    return fail(KVK_ERR_UNSUPPORTED, "%s: too many rows in one call", what);
+  if (kvk_status st = check_gpu_buffers({positions}, what)) return st;
+  for (int i = 0; i < n_rows; ++i)
+    if (kvk_status st = check_gpu_buffers({rows[i].in, rows[i].out}, what)) return st;
+  const dim3 g((unsigned)gx, (unsigned)gy), b(kThreads);
+  const bool pairs = rotary->layout == KVK_ROTARY_PAIRS;
+  if (f32) {
+    if (pairs) hipLaunchKernelGGL((rotate_kernel<true, true, 4>), g, b, 0, stream, a);
+    else hipLaunchKernelGGL((rotate_kernel<true, false, 4>), g, b, 0, stream, a);
+  } else if (U == 8) {
+    if (pairs) hipLaunchKernelGGL((rotate_kernel<false, true, 8>), g, b, 0, stream, a);
+    else hipLaunchKernelGGL((rotate_kernel<false, false, 8>), g, b, 0, stream, a);
+  } else {
+    if (pairs) hipLaunchKernelGGL((rotate_kernel<false, true, 4>), g, b, 0, stream, a);
+    else hipLaunchKernelGGL((rotate_kernel<false, false, 4>), g, b, 0, stream, a);
+  }
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return fail(KVK_ERR_DEVICE, "%s launch: %s", what, hipGetErrorString(e));
+  return KVK_OK;
+}

@@ -22,6 +22,7 @@ OK, ERR_INVALID, ERR_UNSUPPORTED, ERR_DEVICE, ERR_BUFFER = 0, -1, -2, -3, -4
 GQA, MLA = 0, 1
 KIVI32, SYMROW, GROUP64 = 0, 1, 2
 BF16, F32 = 0, 1
+HALVES, PAIRS = 0, 1
 
 
 class Dims(ctypes.Structure):
@@ -63,7 +64,7 @@ def load() -> ctypes.CDLL:
         if not os.path.exists(LIB_PATH):
             raise ImportError(f"{LIB_PATH} is missing: run `python -m paper_2609_37988_amd.build`")
         lib = ctypes.CDLL(LIB_PATH)
-        P, I32, I64, F = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float
+        P, I32, I64, F, D = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float, ctypes.c_double
         sig = {
             "kvk_layer_table": (I32, [ctypes.POINTER(Dims), ctypes.POINTER(Action), ctypes.POINTER(P)]),
             "kvk_table_query": (I32, [P, ctypes.POINTER(TableInfo)]),
@@ -90,6 +91,18 @@ def load() -> ctypes.CDLL:
             "kvk_append_chunk": (I32, [P, I32, I32, P, P, I32, I32, P, P, P, P]),
             "kvk_chunk_workspace_bytes": (I32, [P, I32, I32, I32, ctypes.POINTER(ctypes.c_size_t)]),
             "kvk_chunk_attention": (I32, [P, I32, I32, P, I32, P, P, F, P, P, P, ctypes.c_size_t, P]),
+            "kvk_rotary_frequencies": (I32, [I32, D, D, I32, D, D, P]),
+            "kvk_rotary_create": (I32, [I32, I32, P, D, ctypes.POINTER(P)]),
+            "kvk_rotary_destroy": (None, [P]),
+            "kvk_rotate": (I32, [P, I32, I32, P, I32, P, I32, I32, I32, P]),
+            "kvk_index_bytes": (I32, [P, ctypes.POINTER(ctypes.c_size_t)]),
+            "kvk_index_part": (I32, [P, I32, I32, ctypes.POINTER(I64), ctypes.POINTER(I64)]),
+            "kvk_index_blocks": (I32, [P, I32, I32, P, P, P, P, P]),
+            "kvk_select_workspace_bytes": (I32, [P, I32, I32, ctypes.POINTER(ctypes.c_size_t)]),
+            "kvk_select_blocks": (I32, [P, I32, I32, P, P, I32, I32, I32, P, P, P, ctypes.c_size_t, P]),
+            "kvk_block_workspace_bytes": (I32, [P, I32, I32, I32, ctypes.POINTER(ctypes.c_size_t)]),
+            "kvk_block_attention": (I32, [P, I32, I32, P, P, P, I32, F, P, P, P, ctypes.c_size_t, P]),
+            "kvk_copy_sequences": (I32, [P, P, P, P, I32, P, P, P, P, I32, P]),
             "kvk_decode_attention": (I32, [P, I32, I32, P, I32, I32, F, P, P, P, P, P, ctypes.c_size_t, P]),
             "kvk_decode_splits": (I32, [P, I32, I32, P, I32, I32, F, P, P, P, P, ctypes.c_size_t, P]),
             "kvk_decode_attention_noalloc": (I32, [P, I32, I32, P, I32, I32, F, P, P, P, P, P]),
@@ -121,6 +134,9 @@ def exported_symbols() -> List[str]:
             "kvk_prompt_attention", "kvk_attention_weight_workspace_bytes", "kvk_attention_weight", "kvk_keep_workspace_bytes",
             "kvk_keep_heaviest",
             "kvk_append_chunk", "kvk_chunk_workspace_bytes", "kvk_chunk_attention",
+            "kvk_rotary_frequencies", "kvk_rotary_create", "kvk_rotary_destroy", "kvk_rotate",
+            "kvk_index_bytes", "kvk_index_part", "kvk_index_blocks", "kvk_select_workspace_bytes", "kvk_select_blocks",
+            "kvk_block_workspace_bytes", "kvk_block_attention", "kvk_copy_sequences",
             "kvk_decode_attention", "kvk_decode_splits", "kvk_decode_merge", "kvk_decode_attention_noalloc", "kvk_decode_setup",
             "kvk_read_bytes", "kvk_debug_dequantize",
             "kvk_realized_bits", "kvk_rho_range", "kvk_last_error", "kvk_version"]
@@ -185,6 +201,7 @@ class Table:
         self.mla_weights = None  # (w_uk, w_uv) attached by set_mla_weights
         self.plans = None        # per-sequence plans (layer_table_batched)
         self._arena_bytes = None
+        self._index_bytes = None
 
     @property
     def handle(self):
@@ -695,6 +712,211 @@ def chunk_attention(t: Table, layer_begin: int, layer_end: int, q: torch.Tensor,
     _check(load().kvk_chunk_attention(t.handle, layer_begin, layer_end, q.data_ptr(), shape[3], _address(stored),
                                       _address(new), scale, arena.data_ptr(), out.data_ptr(), workspace.data_ptr(),
                                       _nbytes(workspace), _stream(stream)))
+
+
+class _Strides(ctypes.Structure):
+    _fields_ = [("seq", ctypes.c_int64), ("head", ctypes.c_int64), ("token", ctypes.c_int64)]
+
+
+class _RotaryRows(ctypes.Structure):
+    _fields_ = [("in_", ctypes.c_void_p), ("out", ctypes.c_void_p), ("n_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("first", ctypes.c_int32), ("in_strides", _Strides),
+                ("out_strides", _Strides)]
+
+
+def rotary_frequencies(width: int, base: float = 10000.0, factor: float = 1.0, original_tokens: int = 0,
+                       slow_turns: float = 1.0, fast_turns: float = 32.0) -> List[float]:
+    """Radians per position of the width / 2 pairs, scaled for long contexts where asked (see kvk.h)."""
+    out = (ctypes.c_double * max(1, width // 2))()
+    _check(load().kvk_rotary_frequencies(width, base, factor, original_tokens, slow_turns, fast_turns, out))
+    return list(out)
+
+
+class Rotary:
+    """Owning handle of a kvk_rotary."""
+
+    def __init__(self, handle: ctypes.c_void_p, layout: int, width: int):
+        self._h, self.layout, self.width = handle, layout, width
+
+    @property
+    def handle(self):
+        return self._h
+
+    def __del__(self):
+        if getattr(self, "_h", None) and _lib is not None:
+            _lib.kvk_rotary_destroy(self._h)
+            self._h = None
+
+
+def rotary(width: int, frequencies: Sequence[float], layout: int = HALVES, magnitude: float = 1.0) -> Rotary:
+    """What `rotate` turns by: width / 2 frequencies (radians per position), pairs as halves or as
+    neighbours, and the factor of every turned value."""
+    if len(frequencies) != width // 2:
+        raise ValueError(f"{width // 2} frequencies expected, got {len(frequencies)}")
+    arr = (ctypes.c_double * max(1, len(frequencies)))(*frequencies)
+    h = ctypes.c_void_p()
+    _check(load().kvk_rotary_create(layout, width, arr, magnitude, ctypes.byref(h)))
+    return Rotary(h, layout, width)
+
+
+def _rotary_strides(x: torch.Tensor):
+    """Element strides of sequence, head and token of a packed [tokens, heads, d] or padded
+    [B, heads, n, d] tensor.  (The stride of a dimension of one element is never taken.)"""
+    shape, st = x.shape, x.stride()
+    if len(shape) == 3:
+        n, h, d = shape
+        return 0, st[1] if h > 1 else 0, st[0] if n > 1 else 0
+    b, h, n, d = shape
+    return st[0] if b > 1 else 0, st[1] if h > 1 else 0, st[2] if n > 1 else 0
+
+
+def rotate(rot: Rotary, positions: torch.Tensor, tensors: Sequence[torch.Tensor],
+           outs: Optional[Sequence[torch.Tensor]] = None, first=0, inverse: bool = False, stream=None):
+    """Rotary positions of queries and keys, in one launch.  tensors: 1 to 4 bf16 or fp32 tensors of one
+    dtype, packed [tokens, heads, d] or padded [B, heads, n, d] (all alike), any strides with
+    contiguous rows; outs: where they go (None: in place).  first: the first channel that turns, one
+    number or one per tensor.  positions int32, contiguous: [tokens], or [B, n] ([P, n], P a divisor of B:
+    sequence b takes row b % P; [n]: shared).  inverse: the transposed map, the forward's gradient."""
+    outs = tensors if outs is None else outs
+    count = len(tensors)
+    firsts = [first] * count if hasattr(first, "__index__") else list(first)
+    if len(outs) != count or len(firsts) != count or not 1 <= count <= 4:
+        raise ValueError("1 to 4 tensors, with an output and a first channel each")
+    x0 = tensors[0]
+    rank = x0.dim()
+    if rank not in (3, 4):
+        raise ValueError("tensors must be [tokens, heads, d] or [B, heads, n, d]")
+    seqs, n = (1, x0.shape[0]) if rank == 3 else (x0.shape[0], x0.shape[2])
+    rows = (_RotaryRows * count)()
+    for r, x, y, f in zip(rows, tensors, outs, firsts):
+        if (x.dtype != x0.dtype or y.dtype != x0.dtype or x.dim() != rank or x.shape != y.shape or x.stride(-1) != 1
+                or y.stride(-1) != 1 or (x.shape[0] if rank == 3 else x.shape[2]) != n or (rank == 4 and x.shape[0] != seqs)):
+            raise ValueError("tensors and outputs must agree in dtype, tokens and sequences, with contiguous rows")
+        r.in_, r.out, r.n_heads, r.head_dim, r.first = x.data_ptr(), y.data_ptr(), x.shape[1], x.shape[-1], f
+        a, b = _rotary_strides(x), _rotary_strides(y)
+        r.in_strides, r.out_strides = _Strides(*a), _Strides(*b)
+    if positions.dtype != torch.int32 or not positions.is_contiguous() or positions.dim() > 2 or positions.shape[-1:] != (n,):
+        raise ValueError(f"positions must be contiguous int32 [{n}] or [rows, {n}]")
+    _here(positions, *tensors, *outs)
+    pos_seqs = positions.shape[0] if positions.dim() == 2 else 1
+    _check(load().kvk_rotate(rot.handle, seqs, n, positions.data_ptr(), pos_seqs, rows, count, _dtype_code(x0), int(inverse),
+                             _stream(stream)))
+
+
+def index_bytes(t: Table) -> int:
+    if t._index_bytes is None:
+        out = ctypes.c_size_t(0)
+        _check(load().kvk_index_bytes(t.handle, ctypes.byref(out)))
+        t._index_bytes = out.value
+    return t._index_bytes
+
+
+def index_views(t: Table, index: torch.Tensor, layer: int, sequence: int = 0):
+    """The summaries that `layer` reads (its anchor's), as views of the index: codes int8
+    [B, Hkv, blocks, 2, d_h] (middles, then halves) and scales fp32 [B, Hkv, blocks, 2]; per-sequence
+    tables: of one sequence, B = 1."""
+    codes, scales = ctypes.c_int64(), ctypes.c_int64()
+    _check(load().kvk_index_part(t.handle, sequence, layer, ctypes.byref(codes), ctypes.byref(scales)))
+    if index.dtype != torch.uint8 or not index.is_contiguous() or index.numel() < index_bytes(t):
+        raise ValueError("index must be contiguous uint8, index_bytes")
+    d = t.dims
+    shape = (1 if t.plans else d.batch, d.n_kv_heads, (d.keep_tokens or d.max_tokens) // 32, 2)
+    n = shape[0] * shape[1] * shape[2] * 2
+    flat = index.view(-1)
+    return (flat[codes.value:codes.value + n * d.head_dim].view(torch.int8).view(*shape, d.head_dim),
+            flat[scales.value:scales.value + 4 * n].view(torch.float32).view(shape))
+
+
+def index_blocks(t: Table, layer_begin: int, layer_end: int, n_stored, arena: torch.Tensor, index: torch.Tensor,
+                 n_indexed=None, stream=None):
+    """Summaries of the full blocks that n_stored tokens fill, past those that n_indexed tokens
+    (None: none) fill, of every anchor in [layer_begin, layer_end); n_stored, n_indexed: one length, or one
+    per sequence, on the host.  index: uint8, index_bytes, 256-byte aligned."""
+    B = t.dims.batch
+    _here(arena, index)
+    if _nbytes(arena) < t.arena_bytes or _nbytes(index) < index_bytes(t):
+        raise ValueError("arena smaller than arena_bytes, or index smaller than index_bytes")
+    stored = _lengths(n_stored, B, "n_stored")
+    done = None if n_indexed is None else _lengths(n_indexed, B, "n_indexed")
+    _check(load().kvk_index_blocks(t.handle, layer_begin, layer_end, _address(done), _address(stored), arena.data_ptr(),
+                                   index.data_ptr(), _stream(stream)))
+
+
+def select_workspace_bytes(t: Table, layer_begin: int, layer_end: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check(load().kvk_select_workspace_bytes(t.handle, layer_begin, layer_end, ctypes.byref(out)))
+    return out.value
+
+
+def _one_token(t: Table, layer_begin: int, layer_end: int, q: torch.Tensor, blocks: torch.Tensor):
+    d, nl = t.dims, layer_end - layer_begin
+    if q.dtype != torch.bfloat16 or not q.is_contiguous() or tuple(q.shape) != (nl, d.batch, d.n_q_heads, d.head_dim):
+        raise ValueError("q must be contiguous bf16 [layers, B, Hq, d_h]")
+    if blocks.dtype != torch.int32 or not blocks.is_contiguous() or blocks.dim() != 4 or \
+            tuple(blocks.shape[:3]) != (nl, d.batch, d.n_kv_heads):
+        raise ValueError("blocks must be contiguous int32 [layers, B, Hkv, n_select]")
+
+
+def select_blocks(t: Table, layer_begin: int, layer_end: int, q: torch.Tensor, n_stored, index: torch.Tensor,
+                  blocks: torch.Tensor, n_first: int = 0, n_recent: int = 0, workspace: Optional[torch.Tensor] = None,
+                  stream=None):
+    """The blocks of largest score for one new token's queries q bf16 [layers, B, Hq, d_h]; blocks int32
+    [layers, B, Hkv, n_select] receives them in increasing order, then -1.  n_stored: one length, or
+    one per sequence, on the host.  workspace: select_workspace_bytes bytes (None where that is 0)."""
+    _one_token(t, layer_begin, layer_end, q, blocks)
+    _here(q, index, blocks, workspace)
+    if _nbytes(index) < index_bytes(t):
+        raise ValueError("index smaller than index_bytes")
+    stored = _lengths(n_stored, t.dims.batch, "n_stored")
+    size = 0 if workspace is None else _nbytes(workspace)
+    _check(load().kvk_select_blocks(t.handle, layer_begin, layer_end, q.data_ptr(), _address(stored), blocks.shape[3], n_first,
+                                    n_recent, index.data_ptr(), blocks.data_ptr(), workspace.data_ptr() if size else None,
+                                    size, _stream(stream)))
+
+
+def block_workspace_bytes(t: Table, layer_begin: int, layer_end: int, n_select: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check(load().kvk_block_workspace_bytes(t.handle, layer_begin, layer_end, n_select, ctypes.byref(out)))
+    return out.value
+
+
+def block_attention(t: Table, layer_begin: int, layer_end: int, q: torch.Tensor, n_stored, blocks: torch.Tensor,
+                    scale: float, arena: torch.Tensor, out: torch.Tensor, workspace: torch.Tensor, stream=None):
+    """Attention of one new token per sequence over the listed blocks and the bf16 window.  q, out bf16
+    [layers, B, Hq, d_h]; blocks int32 [layers, B, Hkv, n_select] (entries that name no full block are
+    passed over); n_stored (the new token among them): one length, or one per sequence, on the host."""
+    _one_token(t, layer_begin, layer_end, q, blocks)
+    if out.dtype != torch.bfloat16 or not out.is_contiguous() or out.shape != q.shape:
+        raise ValueError("out must be as q")
+    _here(q, blocks, arena, out, workspace)
+    if _nbytes(arena) < t.arena_bytes:
+        raise ValueError("arena smaller than arena_bytes")
+    stored = _lengths(n_stored, t.dims.batch, "n_stored")
+    _check(load().kvk_block_attention(t.handle, layer_begin, layer_end, q.data_ptr(), _address(stored), blocks.data_ptr(),
+                                      blocks.shape[3], scale, arena.data_ptr(), out.data_ptr(), workspace.data_ptr(),
+                                      _nbytes(workspace), _stream(stream)))
+
+
+def copy_sequences(src_table: Table, src_arena: torch.Tensor, dst_table: Table, dst_arena: torch.Tensor, src, dst, n_stored,
+                   blocks: Optional[torch.Tensor] = None, stream=None):
+    """Copies stored sequences, all layers: sequence src[i] of src_arena into slot dst[i] of dst_arena, n_stored[i]
+    tokens (one number: of each).  blocks int32 [n_layers, src batch, Hkv, n] (MLA: [n_layers, src batch, n]):
+    only these blocks, in this order, and the bf16 window."""
+    _here(src_arena, dst_arena, blocks)
+    if _nbytes(src_arena) < src_table.arena_bytes or _nbytes(dst_arena) < dst_table.arena_bytes:
+        raise ValueError("arena smaller than arena_bytes")
+    a, count = array("i", src), len(src)
+    b, stored = _lengths(dst, count, "dst"), _lengths(n_stored, count, "n_stored")
+    if blocks is not None:
+        d = src_table.dims
+        lead = (d.n_layers, d.batch) + (() if d.kind == MLA else (d.n_kv_heads,))
+        if blocks.dtype != torch.int32 or not blocks.is_contiguous() or tuple(blocks.shape[:-1]) != lead:
+            raise ValueError(f"blocks must be contiguous int32 {list(lead)} + [n]")
+    _check(load().kvk_copy_sequences(src_table.handle, src_arena.data_ptr(), dst_table.handle, dst_arena.data_ptr(), count,
+                                     _address(a), _address(b), _address(stored),
+                                     # (lists of no blocks have no address, but are lists)
+                                     None if blocks is None else blocks.data_ptr() or src_arena.data_ptr(),
+                                     0 if blocks is None else blocks.shape[-1], _stream(stream)))
 
 
 def decode_attention(t: Table, layer_begin: int, layer_end: int, q: torch.Tensor, n_stored: int,

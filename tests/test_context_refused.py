@@ -1,0 +1,351 @@
+"""What the rotary, block and copy calls refuse, before anything is launched (no GPU), and the host-side
+formulas: rotary frequencies, workspace and index sizes."""
+import ctypes
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2609_37988_amd import kvk
+
+P0 = 1 << 20  # an aligned address that is no GPU memory
+I32 = ctypes.c_int32
+
+
+def _arr(vals):
+    return None if vals is None else (I32 * max(1, len(vals)))(*vals)
+
+
+def _refused(status, want, *words):
+    assert status == want, (status, kvk.last_error())
+    for w in words:
+        assert w in kvk.last_error(), kvk.last_error()
+
+
+def _table(kind=kvk.GQA, plan=None, **kw):
+    a = dict(n_layers=2, n_q_heads=4, n_kv_heads=2, head_dim=64, batch=3, max_tokens=100)
+    if kind == kvk.MLA:
+        a.update(n_q_heads=8, head_dim=128, latent_dim=256, rope_dim=64, nope_dim=128, v_dim=128)
+    a.update(kw)
+    plan = plan or [(0, 8, 256 if kind == kvk.MLA else 0), (1, 8)]
+    return kvk.layer_table(kvk.make_dims(kind, **a), kvk.make_plan(plan))
+
+
+# --------------------------------------------------------------------------------------
+# Rotary positions
+# --------------------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("width,base", [(2, 10000.0), (64, 10000.0), (128, 1e6), (96, 5e5)])
+def test_rotary_frequencies(width, base):
+    i = np.arange(width // 2)
+    f = base ** (-2.0 * i / width)
+    assert np.allclose(kvk.rotary_frequencies(width, base), f, rtol=1e-14)
+    assert np.allclose(kvk.rotary_frequencies(width, base, factor=4), f / 4, rtol=1e-14)
+    # by parts: fast pairs stay, slow ones are interpolated, between them a ramp in turns
+    got = np.array(kvk.rotary_frequencies(width, base, factor=8.0, original_tokens=4096, slow_turns=1.0, fast_turns=4.0))
+    turns = 4096 * f / (2 * math.pi)
+    assert np.allclose(got[turns >= 4], f[turns >= 4], rtol=1e-14)
+    assert np.allclose(got[turns <= 1], f[turns <= 1] / 8, rtol=1e-14)
+    ramp = (turns > 1) & (turns < 4)
+    kept = (turns[ramp] - 1) / 3
+    assert np.allclose(got[ramp], f[ramp] * kept + f[ramp] / 8 * (1 - kept), rtol=1e-13)
+
+
+def test_rotary_frequencies_refused():
+    call = kvk.load().kvk_rotary_frequencies
+    out = (ctypes.c_double * 64)()
+    for w in (0, -2, 7):
+        _refused(call(w, 1e4, 1.0, 0, 1.0, 32.0, out), kvk.ERR_INVALID, "width")
+    for base, factor in ((0.0, 1.0), (-1.0, 1.0), (float("nan"), 1.0), (float("inf"), 1.0), (1e4, 0.0), (1e4, -2.0), (1e4, float("nan"))):
+        _refused(call(64, base, factor, 0, 1.0, 32.0, out), kvk.ERR_INVALID, "base and factor")
+    _refused(call(64, 1e4, 2.0, -1, 1.0, 32.0, out), kvk.ERR_INVALID, "original_tokens")
+    for slow, fast in ((2.0, 2.0), (3.0, 2.0), (-1.0, 2.0), (1.0, float("inf")), (float("nan"), 2.0)):
+        _refused(call(64, 1e4, 2.0, 4096, slow, fast, out), kvk.ERR_INVALID, "turns")
+        assert call(64, 1e4, 2.0, 0, slow, fast, out) == kvk.OK  # not used
+    _refused(call(64, 1e4, 1.0, 0, 1.0, 32.0, None), kvk.ERR_INVALID, "NULL")
+
+
+def test_rotary_create_refused():
+    call = kvk.load().kvk_rotary_create
+    f, h = (ctypes.c_double * 512)(*([0.5] * 512)), ctypes.c_void_p()
+    _refused(call(2, 64, f, 1.0, ctypes.byref(h)), kvk.ERR_INVALID, "layout")
+    for w in (0, 4, 12, 520, -8):
+        _refused(call(0, w, f, 1.0, ctypes.byref(h)), kvk.ERR_INVALID, "width")
+    for m in (float("nan"), float("inf"), 1e39):
+        _refused(call(0, 64, f, m, ctypes.byref(h)), kvk.ERR_INVALID, "magnitude")
+    _refused(call(0, 64, None, 1.0, ctypes.byref(h)), kvk.ERR_INVALID, "NULL")
+    _refused(call(0, 64, f, 1.0, None), kvk.ERR_INVALID, "NULL")
+    f[31] = float("inf")
+    _refused(call(0, 64, f, 1.0, ctypes.byref(h)), kvk.ERR_INVALID, "frequency 31")
+    kvk.load().kvk_rotary_destroy(None)
+    with pytest.raises(ValueError):
+        kvk.rotary(64, [1.0] * 31)
+    with pytest.raises(kvk.KvkError):
+        kvk.rotary(12, [1.0] * 6)
+
+
+def _rows(**kw):
+    a = dict(in_=P0, out=P0 + (1 << 20), n_heads=4, head_dim=64, first=0, in_strides=(2048, 64, 256), out_strides=(2048, 64, 256))
+    a.update(kw)
+    a["in_strides"], a["out_strides"] = kvk._Strides(*a["in_strides"]), kvk._Strides(*a["out_strides"])
+    return kvk._RotaryRows(**a)
+
+
+def _rotate(rows=None, width=64, seqs=2, tokens=8, positions=P0, pos_seqs=1, n=None, dtype=kvk.BF16, rot=0):
+    rows = [_rows()] if rows is None else rows
+    rot = kvk.rotary(width, [0.5] * (width // 2)) if rot == 0 else rot
+    arr = (kvk._RotaryRows * max(1, len(rows)))(*rows)
+    return kvk.load().kvk_rotate(rot.handle if rot else None, seqs, tokens, positions, pos_seqs, arr,
+                                 len(rows) if n is None else n, dtype, 0, None)
+
+
+def test_rotate_refused():
+    _refused(_rotate(rot=None), kvk.ERR_INVALID, "NULL")
+    for n in (0, 5, -1):
+        _refused(_rotate(rows=[_rows()] * 5, n=n), kvk.ERR_INVALID, "tensors")
+    _refused(_rotate(dtype=2), kvk.ERR_INVALID, "dtype")
+    _refused(_rotate(seqs=-1), kvk.ERR_INVALID, "sequences")
+    _refused(_rotate(tokens=-1), kvk.ERR_INVALID, "sequences")
+    for p in (0, 3, -1):
+        _refused(_rotate(pos_seqs=p), kvk.ERR_INVALID, "positions")
+    _refused(_rotate(positions=None), kvk.ERR_INVALID, "NULL")
+    _refused(_rotate(positions=P0 + 2), kvk.ERR_INVALID, "misaligned positions")
+    for name in ("in_", "out"):
+        _refused(_rotate(rows=[_rows(**{name: None})]), kvk.ERR_INVALID, "NULL")
+        _refused(_rotate(rows=[_rows(**{name: P0 + 8})]), kvk.ERR_INVALID, "misaligned")
+    _refused(_rotate(rows=[_rows(n_heads=0)]), kvk.ERR_INVALID, "0 heads")
+    for d in (0, 60, 4):
+        _refused(_rotate(rows=[_rows(head_dim=d)]), kvk.ERR_INVALID, "width")
+    for first in (-8, 4, 8):
+        _refused(_rotate(rows=[_rows(first=first)]), kvk.ERR_INVALID, "channels")
+    _refused(_rotate(rows=[_rows(head_dim=56)]), kvk.ERR_INVALID, "channels")
+    for bad in ((2048, 60, 256), (-8, 64, 256), (2048, 64, 4)):
+        _refused(_rotate(rows=[_rows(in_strides=bad)]), kvk.ERR_INVALID, "in strides")
+        _refused(_rotate(rows=[_rows(out_strides=bad)]), kvk.ERR_INVALID, "out strides")
+    for bad in ((2048, 0, 256), (0, 64, 256), (2048, 64, 192), (2048, 64, 0), (1984, 64, 256)):
+        _refused(_rotate(rows=[_rows(out_strides=bad)]), kvk.ERR_INVALID, "overlap")
+    _refused(_rotate(rows=[_rows(out=P0, out_strides=(4096, 64, 256))]), kvk.ERR_INVALID, "in place")
+    _refused(_rotate(rows=[_rows(in_strides=(2**62, 64, 256))]), kvk.ERR_INVALID, "beyond")
+    # the stride of a dimension of one element is never taken; inputs may repeat
+    _refused(_rotate(rows=[_rows(out_strides=(0, 64, 256))], seqs=1), kvk.ERR_INVALID, "not GPU-accessible")
+    _refused(_rotate(rows=[_rows(in_strides=(0, 0, 0))]), kvk.ERR_INVALID, "not GPU-accessible")
+    _refused(_rotate(), kvk.ERR_INVALID, "not GPU-accessible")
+    assert _rotate(seqs=0) == kvk.OK
+    assert _rotate(tokens=0) == kvk.OK
+    big = _rows(in_strides=(0, 64, 256), out_strides=(2**34, 64, 256))
+    _refused(_rotate(rows=[big], seqs=1, tokens=2**30), kvk.ERR_UNSUPPORTED, "tokens in one call")
+
+
+def test_rotate_binding_refuses():
+    r = kvk.rotary(64, [0.5] * 32)
+    x, pos = torch.zeros(8, 4, 64, dtype=torch.bfloat16), torch.zeros(8, dtype=torch.int32)
+    y = torch.zeros(2, 4, 8, 64, dtype=torch.bfloat16)
+    for args, kw in (((pos, []), {}), ((pos, [x] * 5), {}), ((pos, [x], [x, x]), {}), ((pos, [x], None, [0, 0]), {}),
+                     ((pos, [x[0]]), {}), ((pos, [x, x.float()]), {}), ((pos, [x, y]), {}), ((pos, [x], [x[:, :2]]), {}),
+                     ((pos, [x.transpose(1, 2)]), {}), ((pos.long(), [x]), {}), ((pos[:7], [x]), {}), ((pos[::2], [x[:4]]), {}),
+                     ((pos, [x]), {})):  # (the last: on the host)
+        with pytest.raises(ValueError):
+            kvk.rotate(r, *args, **kw)
+
+
+# --------------------------------------------------------------------------------------
+# Index, choice, attention over chosen blocks
+# --------------------------------------------------------------------------------------
+
+
+def _index(t, l0=0, l1=2, done=None, stored=(10, 64, 100), arena=P0, index=P0):
+    return kvk.load().kvk_index_blocks(t.handle if t else None, l0, l1, _arr(done), _arr(stored), arena, index, None)
+
+
+def _select(t, l0=0, l1=2, q=P0, stored=(10, 64, 100), n=2, first=0, recent=0, index=P0, blocks=P0, ws=None, ws_bytes=0):
+    return kvk.load().kvk_select_blocks(t.handle if t else None, l0, l1, q, _arr(stored), n, first, recent, index, blocks, ws,
+                                        ws_bytes, None)
+
+
+def _attend(t, l0=0, l1=2, q=P0, stored=(10, 64, 100), blocks=P0, n=2, scale=0.1, arena=P0, out=P0, ws=P0, ws_bytes=1 << 30):
+    return kvk.load().kvk_block_attention(t.handle if t else None, l0, l1, q, _arr(stored), blocks, n, scale, arena, out, ws,
+                                          ws_bytes, None)
+
+
+@pytest.mark.parametrize("call", [_index, _select, _attend])
+def test_block_calls_refused(call):
+    t = _table()
+    _refused(call(None), kvk.ERR_INVALID, "NULL table")
+    _refused(call(_table(kvk.MLA)), kvk.ERR_UNSUPPORTED, "GQA")
+    for l0, l1 in ((-1, 1), (0, 3), (1, 1), (2, 1)):
+        _refused(call(t, l0, l1), kvk.ERR_INVALID, "layer range")
+    _refused(call(t, stored=None), kvk.ERR_INVALID, "NULL")
+    _refused(call(t, stored=(0, -1, 0)), kvk.ERR_INVALID, "n_stored[1]")
+    _refused(call(t, stored=(0, 0, 101)), kvk.ERR_INVALID, "n_stored[2] = 101")
+    _refused(call(t), kvk.ERR_INVALID, "not GPU-accessible")
+
+
+def test_index_refused():
+    t = _table()
+    for name, off in (("arena", 8), ("index", 128)):
+        _refused(_index(t, **{name: None}), kvk.ERR_INVALID, "NULL")
+        _refused(_index(t, **{name: P0 + off}), kvk.ERR_INVALID, "misaligned")
+    _refused(_index(t, done=(11, 0, 0)), kvk.ERR_INVALID, "n_indexed[0] = 11")
+    _refused(_index(t, done=(0, -1, 0)), kvk.ERR_INVALID, "n_indexed[1]")
+    assert _index(t, done=(0, 64, 96)) == kvk.OK       # no new block
+    assert _index(t, stored=(0, 31, 5)) == kvk.OK
+    _refused(_index(t, done=(0, 64, 95)), kvk.ERR_INVALID, "not GPU-accessible")
+
+
+def test_index_sizes():
+    t = _table(plan=[(0, 8), (1, 8), (0, 4)], n_layers=3)
+    # two anchors of 3 x 2 streams of 3 blocks
+    part = (18 * 128 + 255) // 256 * 256 + 256
+    assert kvk.index_bytes(t) == 2 * part
+    index = torch.zeros(kvk.index_bytes(t), dtype=torch.uint8)
+    views = [kvk.index_views(t, index, l) for l in range(3)]
+    assert [v[0].shape for v in views] == [(3, 2, 3, 2, 64)] * 3 and views[0][1].shape == (3, 2, 3, 2)
+    offs = [v[0].data_ptr() - index.data_ptr() for v in views]
+    assert offs == [0, 0, part]
+    assert [v[1].data_ptr() - index.data_ptr() for v in views] == [x + part - 256 for x in offs]
+    assert kvk.index_bytes(_table(max_tokens=31)) == 256
+    out = ctypes.c_size_t()
+    lo, hi = ctypes.c_int64(), ctypes.c_int64()
+    lib = kvk.load()
+    _refused(lib.kvk_index_bytes(_table(kvk.MLA).handle, ctypes.byref(out)), kvk.ERR_UNSUPPORTED, "GQA")
+    _refused(lib.kvk_index_bytes(None, ctypes.byref(out)), kvk.ERR_INVALID)
+    _refused(lib.kvk_index_bytes(t.handle, None), kvk.ERR_INVALID)
+    for seq, layer in ((1, 0), (-1, 0), (0, 3), (0, -1), (0, 2**31 - 1)):
+        _refused(lib.kvk_index_part(t.handle, seq, layer, ctypes.byref(lo), ctypes.byref(hi)), kvk.ERR_INVALID)
+    _refused(lib.kvk_index_part(t.handle, 0, 0, None, ctypes.byref(hi)), kvk.ERR_INVALID)
+    with pytest.raises(ValueError):
+        kvk.index_views(t, index[:-1], 0)
+    # per-sequence tables: one index after another
+    dims = kvk.make_dims(kvk.GQA, 2, 4, 2, 64, batch=2, max_tokens=100)
+    p = kvk.layer_table_batched(dims, [kvk.make_plan([(0, 8), (1, 8)]), kvk.make_plan([(0, 4), (0, 2)])])
+    one = (6 * 128 + 255) // 256 * 256 + 256
+    assert kvk.index_bytes(p) == 3 * one
+    index = torch.zeros(3 * one, dtype=torch.uint8)
+    offs = [kvk.index_views(p, index, l, b)[0].data_ptr() - index.data_ptr() for b in range(2) for l in range(2)]
+    assert offs == [0, 0, one, 2 * one]
+    assert kvk.index_views(p, index, 1, 1)[0].shape == (1, 2, 3, 2, 64)
+
+
+def test_select_refused():
+    t = _table()
+    for name, off in (("q", 8), ("index", 128), ("blocks", 2)):
+        _refused(_select(t, **{name: None}), kvk.ERR_INVALID, "NULL")
+        _refused(_select(t, **{name: P0 + off}), kvk.ERR_INVALID, "misaligned")
+    for n in (0, -1):
+        _refused(_select(t, n=n), kvk.ERR_INVALID, "n_select")
+    for first, recent in ((-1, 0), (0, -1), (3, 0), (0, 3), (1, 2), (2**31 - 1, 2**31 - 1)):
+        _refused(_select(t, first=first, recent=recent), kvk.ERR_INVALID, "first and")
+    _refused(_select(t, ws=P0 + 128), kvk.ERR_INVALID, "misaligned")
+    assert kvk.select_workspace_bytes(t, 0, 2) == 0
+    t = _table(max_tokens=100000)
+    need = kvk.select_workspace_bytes(t, 0, 2)
+    assert need >= 12 * 3125 * 4 and kvk.select_workspace_bytes(t, 0, 1) <= need
+    stored = (100000, 1, 0)
+    _refused(_select(t, stored=stored), kvk.ERR_INVALID, "NULL workspace")
+    _refused(_select(t, stored=stored, ws=P0, ws_bytes=need - 1), kvk.ERR_BUFFER, "workspace")
+    _refused(_select(t, stored=stored, ws=P0, ws_bytes=need), kvk.ERR_INVALID, "not GPU-accessible")
+    _refused(_select(t, stored=stored, n=3125), kvk.ERR_INVALID, "not GPU-accessible")  # every block: no scores
+    out = ctypes.c_size_t()
+    call = kvk.load().kvk_select_workspace_bytes
+    _refused(call(t.handle, 0, 2, None), kvk.ERR_INVALID)
+    _refused(call(t.handle, 1, 1, ctypes.byref(out)), kvk.ERR_INVALID)
+
+
+def test_attend_refused():
+    t = _table()
+    for name, off in (("q", 8), ("blocks", 2), ("arena", 8), ("out", 8), ("ws", 128)):
+        _refused(_attend(t, **{name: None}), kvk.ERR_INVALID, "NULL")
+        _refused(_attend(t, **{name: P0 + off}), kvk.ERR_INVALID, "misaligned")
+    for n in (0, -5):
+        _refused(_attend(t, n=n), kvk.ERR_INVALID, "n_select")
+    for scale in (float("nan"), float("inf")):
+        _refused(_attend(t, scale=scale), kvk.ERR_INVALID, "finite")
+    need = kvk.block_workspace_bytes(t, 0, 2, 1000)
+    _refused(_attend(t, n=1000, ws_bytes=need - 1), kvk.ERR_BUFFER, "workspace")
+    sizes = [kvk.block_workspace_bytes(t, 0, 2, n) for n in (1, 2, 8, 9, 64, 100, 1000, 100000)]
+    assert sizes == sorted(sizes) and sizes[0] > 0
+    out = ctypes.c_size_t()
+    call = kvk.load().kvk_block_workspace_bytes
+    _refused(call(t.handle, 0, 2, 0, ctypes.byref(out)), kvk.ERR_INVALID)
+    _refused(call(t.handle, 0, 2, 1, None), kvk.ERR_INVALID)
+
+
+def test_block_binding_refuses():
+    t = _table()
+    arena = torch.zeros(kvk.table_query(t).arena_bytes, dtype=torch.uint8)
+    index, ws = torch.zeros(kvk.index_bytes(t), dtype=torch.uint8), torch.zeros(1 << 16, dtype=torch.uint8)
+    q, blocks = torch.zeros(2, 3, 4, 64, dtype=torch.bfloat16), torch.zeros(2, 3, 2, 5, dtype=torch.int32)
+    for bad_q, bad_b in ((q.float(), blocks), (q[:1], blocks), (q[..., :32], blocks), (q, blocks.long()), (q, blocks[:, :, :1]),
+                         (q, blocks[..., ::2]), (q, blocks[0]), (q, blocks)):  # (the last: on the host)
+        with pytest.raises(ValueError):
+            kvk.select_blocks(t, 0, 2, bad_q, 4, index, bad_b)
+        with pytest.raises(ValueError):
+            kvk.block_attention(t, 0, 2, bad_q, 4, bad_b, 0.1, arena, q, ws)
+    with pytest.raises(ValueError):
+        kvk.block_attention(t, 0, 2, q, 4, blocks, 0.1, arena, q.float(), ws)
+    with pytest.raises(ValueError):
+        kvk.index_blocks(t, 0, 2, 4, arena, index)
+
+
+# --------------------------------------------------------------------------------------
+# Copies
+# --------------------------------------------------------------------------------------
+
+FAR = 1 << 40
+
+
+def _copy(a, b, src=(0,), dst=(1,), stored=(50,), pa=P0, pb=FAR, blocks=None, n=0, count=None):
+    return kvk.load().kvk_copy_sequences(a.handle if a else None, pa, b.handle if b else None, pb,
+                                         len(src) if count is None else count, _arr(src), _arr(dst), _arr(stored), blocks, n, None)
+
+
+def test_copy_refused():
+    t = _table()
+    _refused(_copy(None, t), kvk.ERR_INVALID, "NULL table")
+    _refused(_copy(t, None), kvk.ERR_INVALID, "NULL table")
+    for kw in (dict(head_dim=128), dict(n_kv_heads=4), dict(qscheme=kvk.SYMROW), dict(n_layers=3, plan=[(0, 8), (1, 8), (1, 8)])):
+        _refused(_copy(t, _table(**kw)), kvk.ERR_INVALID, "differ in shape")
+    _refused(_copy(t, _table(kvk.MLA)), kvk.ERR_INVALID, "differ in shape")
+    for plan in ([(0, 4), (1, 8)], [(0, 8), (0, 8)]):
+        _refused(_copy(t, _table(plan=plan)), kvk.ERR_INVALID, "plans")
+    m = _table(kvk.MLA)
+    _refused(_copy(m, _table(kvk.MLA, plan=[(0, 8, 128), (1, 8)])), kvk.ERR_INVALID, "plans")
+    _refused(_copy(t, t, count=-1), kvk.ERR_INVALID, "copies")
+    _refused(_copy(t, t, src=(0,) * 4, dst=(0, 1, 2, 0), stored=(1,) * 4), kvk.ERR_INVALID, "4 copies into 3 slots")
+    assert _copy(t, t, count=0) == kvk.OK
+    for kw in (dict(src=None, count=1), dict(dst=None), dict(stored=None), dict(pa=None), dict(pb=None)):
+        _refused(_copy(t, t, **kw), kvk.ERR_INVALID, "NULL")
+    for kw in (dict(pa=P0 + 8), dict(pb=FAR + 8), dict(blocks=P0 + 2, n=1)):
+        _refused(_copy(t, t, **kw), kvk.ERR_INVALID, "misaligned")
+    _refused(_copy(t, t, blocks=P0, n=-1), kvk.ERR_INVALID, "lists")
+    for x in (-1, 3):
+        _refused(_copy(t, t, src=(x,)), kvk.ERR_INVALID, "src[0]")
+        _refused(_copy(t, t, dst=(x,)), kvk.ERR_INVALID, "dst[0]")
+    for x in (-1, 101):
+        _refused(_copy(t, t, stored=(x,)), kvk.ERR_INVALID, "n_stored[0]")
+    small = _table(max_tokens=49)
+    _refused(_copy(t, small), kvk.ERR_INVALID, "beyond the capacity 49")
+    _refused(_copy(t, small, blocks=P0, n=1), kvk.ERR_INVALID, "beyond the capacity 49")     # 32 + 18
+    _refused(_copy(t, small, blocks=P0, n=0), kvk.ERR_INVALID, "not GPU-accessible")         # the window's 18
+    _refused(_copy(t, _table(keep_tokens=49)), kvk.ERR_INVALID, "beyond the capacity 49")
+    _refused(_copy(t, t, src=(0, 0), dst=(1, 1), stored=(1, 1)), kvk.ERR_INVALID, "written twice")
+    _refused(_copy(t, t, pb=P0, src=(1,), dst=(1,)), kvk.ERR_INVALID, "read and written")
+    _refused(_copy(t, t, pb=P0, src=(0, 1), dst=(1, 2), stored=(1, 1)), kvk.ERR_INVALID, "read and written")
+    _refused(_copy(t, t, pb=P0), kvk.ERR_INVALID, "not GPU-accessible")
+    _refused(_copy(t, t, pb=P0 + 256), kvk.ERR_INVALID, "overlap")
+    _refused(_copy(t, _table(), pb=P0), kvk.ERR_INVALID, "overlap")
+    _refused(_copy(t, t), kvk.ERR_INVALID, "not GPU-accessible")
+    # plans are compared copy by copy
+    dims = kvk.make_dims(kvk.GQA, 2, 4, 2, 64, batch=2, max_tokens=100)
+    p = kvk.layer_table_batched(dims, [kvk.make_plan([(0, 8), (1, 8)]), kvk.make_plan([(0, 4), (0, 2)])])
+    _refused(_copy(p, t, src=(0, 1), dst=(0, 1), stored=(5, 5)), kvk.ERR_INVALID, "copy 1")
+    _refused(_copy(p, t, src=(0, 0), dst=(0, 1), stored=(5, 5)), kvk.ERR_INVALID, "not GPU-accessible")
+
+
+def test_copy_binding_refuses():
+    t = _table()
+    arena = torch.zeros(kvk.table_query(t).arena_bytes, dtype=torch.uint8)
+    with pytest.raises(ValueError):
+        kvk.copy_sequences(t, arena, t, arena.clone(), [0], [1], 5)
