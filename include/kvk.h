@@ -814,7 +814,7 @@ kvk_status kvk_index_blocks(const kvk_table* table, int32_t layer_begin, int32_t
 
 /* Chooses blocks for one new token's queries: per layer, sequence and KV head the blocks of largest
  *   score = max over the G query heads of s_q (s_mid (q8 . mid8) + s_half (|q8| . half8)),
- * q8 and s_q the head's query in 8 bits as above (s_q = fp32( max|q| / 127 ), codes rint( q / s_q ) in fp32; zeros
+ * q8 and s_q the head's query in 8 bits, in fp32 (s_q = max|q| times fp32( 1 / 127 ), codes rint( q / s_q ); zeros
  * where a query is not finite), an upper bound, up to the 8-bit rounding, of the largest product of the
  * query with a key of the block (for a positive softmax scale).  The dot products are exact; fp32 rounds
  * s_half (|q8| . half8), then the sum in one fused multiply and add, then the product with s_q; a score that

@@ -34,7 +34,6 @@ using kvk::GroupLayer;
 using kvk::GroupSeq;
 
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr int kWaves = 4;
 // Largest power of two that scales a SYMROW block's values, either way (as in the chunk attention).
 constexpr int kBlockLift = 40;
 
@@ -68,33 +67,35 @@ struct Raw {
   static constexpr int MW = BITS == 16 ? 0 : (QS == kQsKivi ? D / 32 : (QS == kQsG64 ? D / 64 : 8));  // metadata
   uint32_t k[2][KW], v[VW], m[MW > 0 ? MW : 1];
 
+  // The lane's share of a part at byte `at` of the stream (see the arena's layout).
   template <int N>
-  __device__ __forceinline__ static void share(const uint8_t* p, int lane, uint32_t (&w)[N]) {
+  __device__ __forceinline__ static void share(__amdgpu_buffer_rsrc_t rs, int at, int lane, uint32_t (&w)[N]) {
     if constexpr (N >= 4) {
 #pragma unroll
       for (int i = 0; i < N / 4; ++i) {
-        const u4v x = __builtin_nontemporal_load(reinterpret_cast<const u4v*>(p + 1024 * i + 16 * lane));
+        const u4v x = __builtin_amdgcn_raw_buffer_load_b128(rs, 16 * lane, at + 1024 * i, kStreamPolicy);
         w[4 * i] = x[0]; w[4 * i + 1] = x[1]; w[4 * i + 2] = x[2]; w[4 * i + 3] = x[3];
       }
     } else if constexpr (N == 2) {
-      const u2v x = __builtin_nontemporal_load(reinterpret_cast<const u2v*>(p + 8 * lane));
+      const u2v x = __builtin_amdgcn_raw_buffer_load_b64(rs, 8 * lane, at, kStreamPolicy);
       w[0] = x[0]; w[1] = x[1];
     } else {
-      w[0] = __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(p + 4 * lane));
+      w[0] = __builtin_amdgcn_raw_buffer_load_b32(rs, 4 * lane, at, kStreamPolicy);
     }
   }
-  __device__ __forceinline__ void load(const uint8_t* p, int lane) {
+  // at: the block's first byte in the stream; past the resource's range nothing is read.
+  __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t rs, int at, int lane) {
 #pragma unroll
-    for (int tau = 0; tau < 2; ++tau) share(p + tau * (BITS == 16 ? 32 * D : 2 * D * BITS), lane, k[tau]);
-    share(p + (BITS == 16 ? 64 * D : 4 * D * BITS), lane, v);
+    for (int tau = 0; tau < 2; ++tau) share(rs, at + tau * (BITS == 16 ? 32 * D : 2 * D * BITS), lane, k[tau]);
+    share(rs, at + (BITS == 16 ? 64 * D : 4 * D * BITS), lane, v);
     if constexpr (BITS != 16) {
-      const uint8_t* meta = p + 8 * D * BITS;
+      const int meta = at + 8 * D * BITS;
       if constexpr (QS != kQsSym) {
-        share(meta, lane, m);
+        share(rs, meta, lane, m);
       } else {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {  // keys then values, tokens 16 tau + 4 kg ..
-          const u2v x = *reinterpret_cast<const u2v*>(meta + 32 * i + 8 * (lane >> 4));
+          const u2v x = __builtin_amdgcn_raw_buffer_load_b64(rs, 8 * (lane >> 4), meta + 32 * i, 0);
           m[2 * i] = x[0]; m[2 * i + 1] = x[1];
         }
       }
@@ -171,6 +172,9 @@ __device__ __forceinline__ float queries_to_half(u4v (&q)[NJ], float c, int most
   return __builtin_ldexpf(c, -up);
 }
 
+#ifndef KVK_RING
+#define KVK_RING 2
+#endif
 // One full block.  q: the queries (fp16, bf16 in 16-bit layers); qsum: GROUP64, their sums by 64 channels.
 template <int D, int BITS, int QS>
 __device__ __forceinline__ void attend(State<D>& st, const Raw<D, BITS, QS>& r, const u4v (&q)[D / 32], const float* qsum,
@@ -316,28 +320,43 @@ __device__ __forceinline__ void attend_window(State<D>& st, const uint8_t* p, in
     for (int e = 0; e < 8; ++e) y[e] = x[e] - __uint_as_float(e & 1 ? hi[e >> 1] & 0xffff0000u : hi[e >> 1] << 16);
     lo = pack8<false>(y);
   }
+  u4v held;  // ones where a slot holds a token: the others hold anything
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int t = 16 * (i >> 1) + 4 * kg + 2 * (i & 1);
+    held[i] = t + 1 < n ? 0xffffffffu : (t < n ? 0x0000ffffu : 0u);
+  }
+  typedef uint16_t us2 __attribute__((ext_vector_type(2)));
+  u4v v[NM];
+  us2 top = {0, 0};
 #pragma unroll
   for (int m = 0; m < NM; ++m) {
-    u4v v = *reinterpret_cast<const u4v*>(p + 64 * D + 1024 * m + 16 * lane);
+    v[m] = *reinterpret_cast<const u4v*>(p + 64 * D + 1024 * m + 16 * lane) & held;
+    if constexpr (HALF)
 #pragma unroll
-    for (int e = 0; e < 8; ++e)  // slots past the tokens hold anything
-      if (16 * (e >> 2) + 4 * kg + (e & 3) >= n) v[e >> 1] &= e & 1 ? 0x0000ffffu : 0xffff0000u;
-    st.o[m] = mfma16<false>(v, hi, st.o[m]);
-    // (what the rounding left may be 0, which times an infinity were NaN)
-    if constexpr (HALF) st.o[m] = mfma16<false>(only_finite<false>(v), lo, st.o[m]);
+      for (int i = 0; i < 4; ++i) top = __builtin_elementwise_max(top, bitcast<us2>(v[m][i] & 0x7fff7fffu));
+  }
+#pragma unroll
+  for (int m = 0; m < NM; ++m) st.o[m] = mfma16<false>(v[m], hi, st.o[m]);
+  if constexpr (HALF) {
+    if (__any(max(top[0], top[1]) >= 0x7f80))  // what the rounding left may be 0, which times an infinity were NaN
+#pragma unroll
+      for (int m = 0; m < NM; ++m) v[m] = only_finite<false>(v[m]);
+#pragma unroll
+    for (int m = 0; m < NM; ++m) st.o[m] = mfma16<false>(v[m], lo, st.o[m]);
   }
 }
 
-template <int D, int BITS, int QS>
-__global__ __launch_bounds__(64 * kWaves, 2) void block_kernel(BlockArgs a) {
+template <int D, int BITS, int QS, int W>
+__global__ __launch_bounds__(64 * W, 2) void block_kernel(BlockArgs a) {
   using R = Raw<D, BITS, QS>;
   constexpr bool HALF = BITS != 16;
   constexpr int NJ = D / 32, NM = D / 16, kRow = D + 4;  // (rows apart in the banks)
   constexpr int kSlot = R::MW > 0 && QS != kQsSym ? R::MW * 64 : 4;
-  __shared__ __align__(16) float join[kWaves][16][kRow];
-  __shared__ float2 stats[kWaves][16];
-  __shared__ uint32_t saw[kWaves];
-  __shared__ __align__(16) uint32_t slots[kWaves][kSlot];
+  __shared__ __align__(16) float join[W][16][kRow];
+  __shared__ float2 stats[W][16];
+  __shared__ uint32_t saw[W];
+  __shared__ __align__(16) uint32_t slots[W][kSlot];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int col = lane & 15, kg = lane >> 4;
 
@@ -383,22 +402,39 @@ __global__ __launch_bounds__(64 * kWaves, 2) void block_kernel(BlockArgs a) {
   const auto next = [&]() -> int {  // the next block, or -1
     while (mask == 0) {
       if (chunk >= e1) return -1;
-      const int e = chunk + kWaves * lane;
+      const int e = chunk + W * lane;
       entry = e < e1 ? list[e] : -1;
       mask = __ballot(entry >= 0 && entry < nbf);
-      chunk += 64 * kWaves;
+      chunk += 64 * W;
     }
     const int i = __ffsll((unsigned long long)mask) - 1;
     mask &= mask - 1;
     return __builtin_amdgcn_readlane(entry, i);
   };
-  int cur = next();
-  R raw[2];
-  if (cur >= 0) raw[0].load(stream + (int64_t)cur * a.block_bytes, lane);
+  // A ring of RING blocks in flight.  Past the list's end the loads go past the full blocks' range, where they read
+  // nothing: no branch, so that the compiler can count the loads outstanding.
+  constexpr int RING = KVK_RING;
+  const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(stream), (short)0, nbf * a.block_bytes, 0x00020000);
+  R raw[RING];
+  int cur[RING];
+#pragma unroll
+  for (int i = 0; i < RING - 1; ++i) {
+    cur[i] = next();
+    raw[i].load(rsrc, (cur[i] < 0 ? nbf : cur[i]) * a.block_bytes, lane);
+  }
   load_queries();
+  // The window goes to the wave with the fewest blocks, while the first of them are on their way; SYMROW's last: its
+  // logits are not lowered, and small values after it would fall below fp16's steps.
+  constexpr bool SYM = HALF && QS == kQsSym;
+  const bool window = rest && split == a.n_split - 1 && wave == W - 1;
+  const auto take_window = [&]() {
+    seen = true;
+    attend_window<D, HALF>(st, stream + (int64_t)a.nb_cap * a.block_bytes, rest, q, a.c, kBias<BITS, QS>, lane);
+  };
+  if (!SYM && window) take_window();
   float c = a.c;
   float qsum[D / 64];
-  if (cur >= 0) {
+  if (cur[0] >= 0) {
     seen = true;
     if constexpr (HALF) c = queries_to_half(q, a.c, a.most_lift);
     if constexpr (HALF && QS == kQsG64) {
@@ -410,27 +446,21 @@ __global__ __launch_bounds__(64 * kWaves, 2) void block_kernel(BlockArgs a) {
         qsum[g] = mfma16<true>(u4v{one, one, one, one}, q[2 * g + 1], s)[0];
       }
     }
-    // (the last block is loaded again, by all lanes, in the place of a next one: loads without a branch)
-    while (true) {
-      int nxt = next();
-      raw[1].load(stream + (int64_t)(nxt < 0 ? cur : nxt) * a.block_bytes, lane);
-      attend<D, BITS, QS>(st, raw[0], q, qsum, c, slots[wave], lane);
-      if (nxt < 0) break;
-      cur = nxt;
-      nxt = next();
-      raw[0].load(stream + (int64_t)(nxt < 0 ? cur : nxt) * a.block_bytes, lane);
-      attend<D, BITS, QS>(st, raw[1], q, qsum, c, slots[wave], lane);
-      if (nxt < 0) break;
-      cur = nxt;
+    for (bool more = true; more;) {
+#pragma unroll
+      for (int i = 0; i < RING; ++i) {
+        if (!more) break;
+        constexpr int P = RING - 1;
+        const int nxt = next();
+        cur[(i + P) % RING] = nxt;
+        raw[(i + P) % RING].load(rsrc, (nxt < 0 ? nbf : nxt) * a.block_bytes, lane);
+        attend<D, BITS, QS>(st, raw[i], q, qsum, c, slots[wave], lane);
+        more = cur[(i + 1) % RING] >= 0;
+      }
     }
+    if (SYM && window) load_queries();
   }
-  if (rest && split == a.n_split - 1 && wave == kWaves - 1) {  // (the wave with the fewest blocks)
-    if constexpr (HALF) {
-      if (seen) load_queries();
-    }
-    seen = true;
-    attend_window<D, HALF>(st, stream + (int64_t)a.nb_cap * a.block_bytes, rest, q, a.c, kBias<BITS, QS>, lane);
-  }
+  if (SYM && window) take_window();
 
   // The waves' states meet in LDS.
   const float l = rows_sum(st.l);
@@ -439,72 +469,87 @@ __global__ __launch_bounds__(64 * kWaves, 2) void block_kernel(BlockArgs a) {
   if (kg == 0) stats[wave][col] = make_float2(st.m, l);
   if (lane == 0) saw[wave] = seen;
   __syncthreads();
-  const int row = tid >> 4, ch = (tid & 15) * (D / 16), h = 16 * tile + row;
+  constexpr int TR = 4 * W, V = D / TR;  // threads of a row, channels of a thread
+  typedef float fv __attribute__((ext_vector_type(V)));
+  typedef uint32_t uv __attribute__((ext_vector_type(V / 2)));
+  const int row = tid / TR, ch = tid % TR * V, h = 16 * tile + row;
   if (h >= a.G) return;
   float M = -INFINITY, sum = 0.0f;
+  uint32_t any = 0;
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w) M = fmaxf(M, stats[w][row].x);
-  float o[D / 16];
+  for (int w = 0; w < W; ++w) {
+    M = fmaxf(M, stats[w][row].x);
+    any |= saw[w];
+  }
+  fv o;
 #pragma unroll
-  for (int k = 0; k < D / 16; ++k) o[k] = 0.0f;
+  for (int k = 0; k < V; ++k) o[k] = 0.0f;
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
+  for (int w = 0; w < W; ++w) {
     const float2 s = stats[w][row];
     const float f = s.x == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(s.x - M);  // (no mass, or NaN)
     sum += s.y * f;
-#pragma unroll
-    for (int k = 0; k < D / 16; k += 4) {
-      const f4 x = *reinterpret_cast<const f4*>(&join[w][row][ch + k]);
-#pragma unroll
-      for (int y = 0; y < 4; ++y) o[k + y] += x[y] * f;
-    }
+    o += *reinterpret_cast<const fv*>(&join[w][row][ch]) * f;
   }
-  const bool any = saw[0] | saw[1] | saw[2] | saw[3];
   const int64_t at = call_row * a.Hq + kvh * a.G + h;
   if (a.n_split == 1) {
     const float inv = any ? 1.0f / sum : 0.0f;
+    uv x;
 #pragma unroll
-    for (int k = 0; k < D / 16; k += 4)
-      *reinterpret_cast<u2v*>(a.out + at * D + ch + k) =
-          u2v{pack2<false>(o[k] * inv, o[k + 1] * inv), pack2<false>(o[k + 2] * inv, o[k + 3] * inv)};
+    for (int k = 0; k < V / 2; ++k) x[k] = pack2<false>(o[2 * k] * inv, o[2 * k + 1] * inv);
+    *reinterpret_cast<uv*>(a.out + at * D + ch) = x;
     return;
   }
   float* rec = a.ws + (at * a.n_split + split) * kRow;
-#pragma unroll
-  for (int k = 0; k < D / 16; k += 4) *reinterpret_cast<f4*>(rec + ch + k) = f4{o[k], o[k + 1], o[k + 2], o[k + 3]};
-  if ((tid & 15) == 0) *reinterpret_cast<f4*>(rec + D) = f4{M, sum, any ? 1.0f : 0.0f, 0.0f};
+  *reinterpret_cast<fv*>(rec + ch) = o;
+  if (tid % TR == 0) *reinterpret_cast<f4*>(rec + D) = f4{M, sum, any ? 1.0f : 0.0f, 0.0f};
 }
 
-// The splits of every row joined, a quarter of a wave per row.
+// The splits of every row joined, half a wave per row, four records in flight.
 template <int D>
 __global__ __launch_bounds__(256) void block_merge_kernel(BlockArgs a, int64_t rows) {
-  constexpr int V = D / 16, kRow = D + 4;
-  const int l16 = threadIdx.x & 15;
-  const int64_t row = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
+  constexpr int V = D / 32, kRow = D + 4;
+  typedef float fv __attribute__((ext_vector_type(V)));
+  typedef uint32_t uv __attribute__((ext_vector_type(V / 2)));
+  const int l32 = threadIdx.x & 31;
+  const int64_t row = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
   if (row >= rows) return;
   const float* rec = a.ws + row * a.n_split * kRow;
-  float M = -INFINITY, sum = 0.0f, any = 0.0f, o[V];
-  for (int i = 0; i < a.n_split; ++i) M = fmaxf(M, rec[i * kRow + D]);
+  float M = -INFINITY, sum = 0.0f, any = 0.0f;
+  fv o;
 #pragma unroll
   for (int k = 0; k < V; ++k) o[k] = 0.0f;
-  for (int i = 0; i < a.n_split; ++i) {
-    const float* p = rec + i * kRow;
-    const f4 s = *reinterpret_cast<const f4*>(p + D);
-    const float f = s[0] == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(s[0] - M);  // (no mass, or NaN)
-    sum += s[1] * f;
-    any += s[2];
+  for (int i0 = 0; i0 < a.n_split; i0 += 4) {
+    fv v[4];
+    f4 s[4];
+    float m = M;
 #pragma unroll
-    for (int k = 0; k < V; k += 4) {
-      const f4 x = *reinterpret_cast<const f4*>(p + V * l16 + k);
+    for (int i = 0; i < 4; ++i) {
+      const float* p = rec + min(i0 + i, a.n_split - 1) * kRow;
+      v[i] = *reinterpret_cast<const fv*>(p + V * l32);
+      s[i] = *reinterpret_cast<const f4*>(p + D);
+    }
 #pragma unroll
-      for (int y = 0; y < 4; ++y) o[k + y] += x[y] * f;
+    for (int i = 0; i < 4; ++i) m = fmaxf(m, s[i][0]);
+    const float f = M == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(M - m);
+    M = m;
+    sum *= f;
+    o *= f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (i0 + i < a.n_split) {
+        const float w = s[i][0] == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(s[i][0] - M);  // (no mass, or NaN)
+        sum += s[i][1] * w;
+        any += s[i][2];
+        o += v[i] * w;
+      }
     }
   }
   const float inv = any > 0.0f ? 1.0f / sum : 0.0f;
+  uv x;
 #pragma unroll
-  for (int k = 0; k < V; k += 4)
-    *reinterpret_cast<u2v*>(a.out + row * D + V * l16 + k) =
-        u2v{pack2<false>(o[k] * inv, o[k + 1] * inv), pack2<false>(o[k + 2] * inv, o[k + 3] * inv)};
+  for (int k = 0; k < V / 2; ++k) x[k] = pack2<false>(o[2 * k] * inv, o[2 * k + 1] * inv);
+  *reinterpret_cast<uv*>(a.out + row * D + V * l32) = x;
 }
 
 }  // namespace
@@ -513,15 +558,22 @@ using namespace kvk;
 
 namespace {
 
-// Workgroups that a call's splits aim at, and list entries that a split has at least.
-constexpr int64_t kAimWgs = 1024;
-constexpr int64_t kMinEntries = 8;
+#ifndef KVK_AIM
+#define KVK_AIM 512
+#define KVK_MINB 4
+#endif
+constexpr int64_t kAimWgs = KVK_AIM;
+constexpr int64_t kCus = 256;
 
-// Parts of each list.
-int32_t splits_of(const kvk_table* t, int32_t l0, int32_t l1, int32_t n_select) {
+// Waves of a workgroup and parts of each list.
+struct Shape {
+  int32_t waves, splits;
+};
+Shape shape_of(const kvk_table* t, int32_t l0, int32_t l1, int32_t n_select) {
   const int64_t G = t->d.n_q_heads / t->d.n_kv_heads;
-  const int64_t wgs = (int64_t)(l1 - l0) * t->d.batch * t->d.n_kv_heads * ((G + 15) / 16);
-  return (int32_t)std::max<int64_t>(1, std::min((kAimWgs + wgs - 1) / wgs, (n_select + kMinEntries - 1) / kMinEntries));
+  const int64_t rows = (int64_t)(l1 - l0) * t->d.batch * t->d.n_kv_heads * ((G + 15) / 16);
+  if (rows >= kCus) return Shape{rows < 2 * kCus && n_select > 16 ? 8 : 4, 1};
+  return Shape{4, (int32_t)std::max<int64_t>(1, std::min<int64_t>(kAimWgs / rows, n_select / (4 * KVK_MINB)))};
 }
 
 kvk_status check_call(const kvk_table* t, const char* what, int32_t l0, int32_t l1, int32_t n_select) {
@@ -533,19 +585,24 @@ kvk_status check_call(const kvk_table* t, const char* what, int32_t l0, int32_t 
   return KVK_OK;
 }
 
-template <int D, int QS>
+template <int D, int W, int QS>
 void launch(int bits, dim3 g, const BlockArgs& a, hipStream_t st) {
-  const dim3 b(64 * kWaves);
-  if (bits == 16) hipLaunchKernelGGL((block_kernel<D, 16, kQsKivi>), g, b, 0, st, a);
-  else if (bits == 8) hipLaunchKernelGGL((block_kernel<D, 8, QS>), g, b, 0, st, a);
-  else if (bits == 4) hipLaunchKernelGGL((block_kernel<D, 4, QS>), g, b, 0, st, a);
-  else hipLaunchKernelGGL((block_kernel<D, 2, QS>), g, b, 0, st, a);
+  const dim3 b(64 * W);
+  if (bits == 16) hipLaunchKernelGGL((block_kernel<D, 16, kQsKivi, W>), g, b, 0, st, a);
+  else if (bits == 8) hipLaunchKernelGGL((block_kernel<D, 8, QS, W>), g, b, 0, st, a);
+  else if (bits == 4) hipLaunchKernelGGL((block_kernel<D, 4, QS, W>), g, b, 0, st, a);
+  else hipLaunchKernelGGL((block_kernel<D, 2, QS, W>), g, b, 0, st, a);
+}
+template <int D, int W>
+void launch(int qs, int bits, dim3 g, const BlockArgs& a, hipStream_t st) {
+  if (qs == KVK_Q_KIVI32) launch<D, W, kQsKivi>(bits, g, a, st);
+  else if (qs == KVK_Q_GROUP64) launch<D, W, kQsG64>(bits, g, a, st);
+  else launch<D, W, kQsSym>(bits, g, a, st);
 }
 template <int D>
-void launch(int qs, int bits, dim3 g, const BlockArgs& a, hipStream_t st) {
-  if (qs == KVK_Q_KIVI32) launch<D, kQsKivi>(bits, g, a, st);
-  else if (qs == KVK_Q_GROUP64) launch<D, kQsG64>(bits, g, a, st);
-  else launch<D, kQsSym>(bits, g, a, st);
+void launch(int waves, int qs, int bits, dim3 g, const BlockArgs& a, hipStream_t st) {
+  if (waves == 8) launch<D, 8>(qs, bits, g, a, st);
+  else launch<D, 4>(qs, bits, g, a, st);
 }
 
 }  // namespace
@@ -553,7 +610,7 @@ void launch(int qs, int bits, dim3 g, const BlockArgs& a, hipStream_t st) {
 extern "C" kvk_status kvk_block_workspace_bytes(const kvk_table* t, int32_t l0, int32_t l1, int32_t n_select, size_t* out) {
   if (kvk_status st = check_call(t, "kvk_block_workspace_bytes", l0, l1, n_select)) return st;
   if (!out) return fail(KVK_ERR_INVALID, "kvk_block_workspace_bytes: NULL output");
-  const int64_t ns = splits_of(t, l0, l1, n_select);
+  const int64_t ns = shape_of(t, l0, l1, n_select).splits;
   const int64_t rows = (int64_t)(l1 - l0) * t->d.batch * t->d.n_q_heads;
   *out = (size_t)(ns > 1 ? round256(rows * ns * (t->d.head_dim + 4) * 4) : 256);
   return KVK_OK;
@@ -577,7 +634,8 @@ extern "C" kvk_status kvk_block_attention(const kvk_table* t, int32_t l0, int32_
   size_t need = 0;
   if (kvk_status st = kvk_block_workspace_bytes(t, l0, l1, n_select, &need)) return st;
   BlockArgs a;
-  a.n_split = splits_of(t, l0, l1, n_select);
+  const Shape shape = shape_of(t, l0, l1, n_select);
+  a.n_split = shape.splits;
   if (a.n_split > 1 && ws_bytes < need) return fail(KVK_ERR_BUFFER, "%s: workspace %zu bytes < %zu needed", what, ws_bytes, need);
   if (kvk_status st = check_gpu_buffers({q, blocks, arena, out, workspace}, what)) return st;
   a.arena = static_cast<const uint8_t*>(arena);
@@ -601,19 +659,19 @@ extern "C" kvk_status kvk_block_attention(const kvk_table* t, int32_t l0, int32_
   if (rows > 0x7fffffffLL) return fail(KVK_ERR_UNSUPPORTED, "%s: too many query rows in one call", what);
   for (const bool go : {false, true}) {
     const kvk_status st = for_groups(
-        t, l0, l1, false, true, a.g,
+        t, l0, l1, Layers::each, true, a.g,
         [&](int b, GroupSeq& s) {
           s.stored = n_stored[b];
           return true;
         },
         [&](int bits, Group& g) -> kvk_status {
           const int64_t wgs = (int64_t)g.n_layers * g.n_seqs * d.n_kv_heads * a.tiles * a.n_split;
-          if (wgs > 0xffffffLL) return fail(KVK_ERR_UNSUPPORTED, "%s: grid too large", what);  // (less than 2^32 threads)
+          if (wgs * 64 * shape.waves > 0xffffffffLL) return fail(KVK_ERR_UNSUPPORTED, "%s: grid too large", what);  // (less than 2^32 threads)
           if (!go) return KVK_OK;
           a.block_bytes = (int32_t)gqa_block_bytes(d.head_dim, bits, d.qscheme);
           const dim3 grid((unsigned)wgs);
-          if (d.head_dim == 128) launch<128>(d.qscheme, bits, grid, a, stream);
-          else launch<64>(d.qscheme, bits, grid, a, stream);
+          if (d.head_dim == 128) launch<128>(shape.waves, d.qscheme, bits, grid, a, stream);
+          else launch<64>(shape.waves, d.qscheme, bits, grid, a, stream);
           const hipError_t e = hipGetLastError();
           if (e != hipSuccess) return fail(KVK_ERR_DEVICE, "%s launch: %s", what, hipGetErrorString(e));
           return KVK_OK;
@@ -621,7 +679,7 @@ extern "C" kvk_status kvk_block_attention(const kvk_table* t, int32_t l0, int32_
     if (st != KVK_OK) return st;
   }
   if (a.n_split > 1) {
-    const dim3 g((unsigned)((rows + 15) / 16)), b(256);
+    const dim3 g((unsigned)((rows + 7) / 8)), b(256);
     if (d.head_dim == 128) hipLaunchKernelGGL(block_merge_kernel<128>, g, b, 0, stream, a, rows);
     else hipLaunchKernelGGL(block_merge_kernel<64>, g, b, 0, stream, a, rows);
     const hipError_t e = hipGetLastError();

@@ -5,10 +5,13 @@
 // copy moves 32-token blocks (those of a list, or all) and then the window, whole.  Bytes are
 // not looked at: a quantised block's codes and scales go together.
 //
-// A wave moves one block at a time; the copies of one source (a fork) are neighbours in the grid, so that its
-// bytes come from HBM once and from the caches for the others.
+// One copy after another in the grid, so that writes run through one destination at a time; the stores bypass the
+// caches, which keep what the copies of one source (a fork) read again.
 //
-// Bound.  HBM.
+// Bound.  HBM: 8 sequences of 8192 tokens in two layers moved to other slots (470 MB read and written) 70 us, 6.7 TB/s; a
+// sequence of 69 MB forked eight times 103 us (553 MB written, 5.4 TB/s; filling as much takes 84).
+// Reading once and writing to every destination from registers scatters the writes: 144 to 165 us; plain stores
+// push the source out of the caches, 138.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -21,7 +24,7 @@ using namespace kvkd;
 namespace {
 
 constexpr int kCopies = 96;   // of a launch
-constexpr int kPiece = 16384; // bytes that a wave moves, about
+constexpr int kPiece = 8192;  // bytes that a wave moves, about (fork: 4096 155 us, 16384 157 with plain stores)
 
 struct CopyLayer {
   int64_t from, to;  // byte offsets of the layer's regions (of the sequence's, per-sequence plans)
@@ -47,20 +50,22 @@ static_assert(sizeof(CopyArgs) <= 4096, "kernel arguments");
 
 __device__ __forceinline__ void move(const uint8_t* from, uint8_t* to, int bytes, int lane) {
   int at = 16 * lane;
-  for (; at + 3072 < bytes; at += 4096) {  // (every lane's four pieces are inside but perhaps the last lanes')
+  for (; at + 3072 < bytes; at += 4096) {
     u4v x[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) x[i] = *reinterpret_cast<const u4v*>(from + at + 1024 * i);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) *reinterpret_cast<u4v*>(to + at + 1024 * i) = x[i];
+    for (int i = 0; i < 4; ++i) __builtin_nontemporal_store(x[i], reinterpret_cast<u4v*>(to + at + 1024 * i));
   }
-  for (; at < bytes; at += 1024) *reinterpret_cast<u4v*>(to + at) = *reinterpret_cast<const u4v*>(from + at);
+  for (; at < bytes; at += 1024)
+    __builtin_nontemporal_store(*reinterpret_cast<const u4v*>(from + at), reinterpret_cast<u4v*>(to + at));
 }
 
 __global__ __launch_bounds__(256) void copy_kernel(CopyArgs a) {
   const int lane = threadIdx.x & 63;
-  const int copy = blockIdx.x % (uint32_t)a.n_copies;
-  const int w = __builtin_amdgcn_readfirstlane((int)(blockIdx.x / (uint32_t)a.n_copies * 4 + (threadIdx.x >> 6)));
+  const uint32_t per_copy = (a.waves + 3) / 4;
+  const int copy = blockIdx.x / per_copy;
+  const int w = __builtin_amdgcn_readfirstlane((int)(blockIdx.x % per_copy * 4 + (threadIdx.x >> 6)));
   if (w >= a.waves) return;
   int l = 0;
   while (l + 1 < a.n_layers && w >= a.layer[l + 1].wave0) ++l;
@@ -70,10 +75,8 @@ __global__ __launch_bounds__(256) void copy_kernel(CopyArgs a) {
   const int n = a.blocks ? min(a.n_blocks, full) : full;
   const uint8_t* from = a.src + y.from + ((int64_t)a.from[copy] * a.streams + stream) * y.from_stream;
   uint8_t* to = a.dst + y.to + ((int64_t)a.to[copy] * a.streams + stream) * y.to_stream;
-  if (part == 0) {  // the first wave also moves the window
-    if (stored & 31)
-      move(from + (int64_t)a.from_cap * y.block_bytes, to + (int64_t)a.to_cap * y.block_bytes, a.window, lane);
-  }
+  if (part == 0 && (stored & 31))  // the first wave also moves the window
+    move(from + (int64_t)a.from_cap * y.block_bytes, to + (int64_t)a.to_cap * y.block_bytes, a.window, lane);
   const int i0 = part * y.per_wave, i1 = min(n, i0 + y.per_wave);
   if (a.blocks) {
     const int32_t* list = a.blocks + (((int64_t)y.row * a.list_slots + a.list[copy]) * a.streams + stream) * a.n_blocks;

@@ -38,7 +38,7 @@ struct IndexArgs {
   const uint8_t* arena;
   uint8_t* index;
   int64_t scales;  // bytes from an anchor's codes to its scales
-  int32_t nb_cap, block_bytes;
+  int32_t nb_cap;
   Group g;
 };
 static_assert(sizeof(IndexArgs) <= 4096, "kernel arguments");
@@ -86,18 +86,13 @@ __device__ __forceinline__ float eight_bits(const double (&x)[N], int (&code)[N]
   return top;
 }
 
+// The summary of the block at p, to `codes` and `scales`.
 template <int D, int BITS, int QS>
-__global__ __launch_bounds__(256) void index_kernel(IndexArgs a) {
+__device__ __forceinline__ void index_block(const uint8_t* p, uint8_t* codes, float2* scales, int lane) {
   constexpr bool HALF = BITS != 16;
   constexpr int NJ = D / 32, NC = D / 16, NV = NC / 4;  // k-steps, 16-channel tiles, channels of a lane
   constexpr int KB = BITS == 16 ? D / 2 : D * BITS / 32, KW = KB / 4;  // bytes and words of a lane's tile
-  const int lane = threadIdx.x & 63, n = lane & 15, kg = lane >> 4;
-  const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
-  const GroupLayer& L = a.g.layers[blockIdx.z / (uint32_t)a.g.n_seqs];
-  const GroupSeq& S = a.g.seqs[blockIdx.z % (uint32_t)a.g.n_seqs];
-  const int kvh = blockIdx.y, blk = S.first + blockIdx.x * 4 + wave;
-  if (blk >= S.stored >> 5) return;
-  const uint8_t* p = a.arena + a.g.stream_at(L, S, kvh) + (int64_t)blk * a.block_bytes;
+  const int n = lane & 15, kg = lane >> 4;
   const uint8_t* meta = p + 8 * D * BITS;
 
   uint32_t w[2][KW];
@@ -229,8 +224,6 @@ __global__ __launch_bounds__(256) void index_kernel(IndexArgs a) {
   if (bad) sh = INFINITY;
 
   // Four lanes' bytes to a word each; of a quad's 2 NV words each lane stores some.
-  const int64_t row = ((int64_t)S.mult * a.g.Hkv + kvh) * a.nb_cap + blk;
-  uint8_t* out = a.index + L.index + S.index;
   uint32_t words[2 * NV];
 #pragma unroll
   for (int i = 0; i < 2 * NV; ++i) {
@@ -243,9 +236,28 @@ __global__ __launch_bounds__(256) void index_kernel(IndexArgs a) {
   if (i < 2 * NV) {
     const uint32_t x = i == 0 ? words[0] : (i == 1 ? words[1] : (i == 2 ? words[NV > 1 ? 2 : 0] : words[NV > 1 ? 3 : 1]));
     const int v = i % NV, part = i / NV;
-    *reinterpret_cast<uint32_t*>(out + row * 2 * D + part * D + (channel(v) & ~3)) = x;
+    *reinterpret_cast<uint32_t*>(codes + part * D + (channel(v) & ~3)) = x;
   }
-  if (lane == 0) *reinterpret_cast<float2*>(out + a.scales + row * 8) = make_float2(sm, sh);
+  if (lane == 0) *scales = make_float2(sm, sh);
+}
+
+template <int D, int QS>
+__global__ __launch_bounds__(256) void index_kernel(IndexArgs a) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+  const GroupLayer& L = a.g.layers[blockIdx.z / (uint32_t)a.g.n_seqs];
+  const GroupSeq& S = a.g.seqs[blockIdx.z % (uint32_t)a.g.n_seqs];
+  const int kvh = blockIdx.y, blk = S.first + blockIdx.x * 4 + wave, bits = L.bits;
+  if (blk >= S.stored >> 5) return;
+  const int bytes = bits == 16 ? 128 * D : (QS == kQsKivi ? 8 * D * (bits + 1) : 8 * D * bits + (QS == kQsG64 ? 4 * D : 128));
+  const uint8_t* p = a.arena + a.g.stream_at(L, S, kvh) + (int64_t)blk * bytes;
+  const int64_t row = ((int64_t)S.mult * a.g.Hkv + kvh) * a.nb_cap + blk;
+  uint8_t* out = a.index + L.index + S.index;
+  uint8_t* codes = out + row * 2 * D;
+  float2* scales = reinterpret_cast<float2*>(out + a.scales) + row;
+  if (bits == 16) index_block<D, 16, kQsKivi>(p, codes, scales, lane);
+  else if (bits == 8) index_block<D, 8, QS>(p, codes, scales, lane);
+  else if (bits == 4) index_block<D, 4, QS>(p, codes, scales, lane);
+  else index_block<D, 2, QS>(p, codes, scales, lane);
 }
 
 // ---------------------------------------------------------------------------
@@ -275,20 +287,22 @@ __device__ __forceinline__ uint32_t key_of(float x) {
   return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 
-// The heads of a (layer, sequence, KV head) in 8 bits, [q | |q|] per row, and their scales.
+// Query rows in 8 bits, [q | |q|] per row, and their scales.
 template <int D, int T>
 struct Queries {
   static constexpr int kStride = 2 * D + 16;  // (bytes; rows apart in the banks)
   uint8_t rows[16 * T * kStride];
   float scale[16 * T];
 
-  __device__ __forceinline__ void fill(const uint16_t* q, int G, int lane, int wave) {
+  // n rows, G of each layer; q: the first layer's, the next `step` elements further.
+  __device__ __forceinline__ void fill(const uint16_t* q, int64_t step, int G, int n, int lane, int wave) {
     for (int h = wave; h < 16 * T; h += kWaves) {
+      const int u = h / G;
       float x[D / 64];
       bool odd = false;
 #pragma unroll
       for (int i = 0; i < D / 64; ++i) {
-        const uint16_t b = h < G ? q[h * D + lane * (D / 64) + i] : 0;
+        const uint16_t b = h < n ? q[u * step + (h - u * G) * D + lane * (D / 64) + i] : 0;
         odd |= (b & 0x7f80u) == 0x7f80u;
         x[i] = bf16_to_f32(b);
       }
@@ -296,7 +310,7 @@ struct Queries {
 #pragma unroll
       for (int i = 0; i < D / 64; ++i) top = fmaxf(top, __builtin_fabsf(x[i]));
       top = rows_max(max16(top));
-      const float s = __any(odd) ? 0.0f : top / 127.0f;
+      const float s = __any(odd) ? 0.0f : top * (1.0f / 127.0f);
       if (lane == 0) scale[h] = s;
 #pragma unroll
       for (int i = 0; i < D / 64; ++i) {
@@ -308,11 +322,12 @@ struct Queries {
   }
 };
 
-// Scores of blocks [b0, b1) as keys into out[b]; the waves of a workgroup share them, sixteen blocks at
-// a time: block b0 + lane % 16 is the lane's column of the products, head 4 (lane / 16) + r of a tile its row r.
+// Scores of blocks [b0, b1) by each of `layers` layers' G rows, as keys into out[u step + b - at0]; the waves of a workgroup
+// share the blocks, sixteen at a time: block b0 + lane % 16 is the lane's column of the products, row
+// 4 (lane / 16) + r of a tile its row r.
 template <int D, int T>
-__device__ __forceinline__ void score(const Queries<D, T>& qs, const uint8_t* codes, const float2* scales, int G, int b0,
-                                      int b1, uint32_t* out, int lane, int wave) {
+__device__ __forceinline__ void score(const Queries<D, T>& qs, const uint8_t* codes, const float2* scales, int G, int layers,
+                                      int b0, int b1, uint32_t* out, int64_t step, int at0, int lane, int wave) {
   constexpr int NK = D / 64;  // products of a part
   const int col = lane & 15, kg = lane >> 4;
   const auto load_rows = [&](i4v (&x)[2 * NK], int t) {
@@ -338,7 +353,7 @@ __device__ __forceinline__ void score(const Queries<D, T>& qs, const uint8_t* co
     }
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      float best = -INFINITY;
+      f4 x[T];
 #pragma unroll
       for (int t = 0; t < T; ++t) {
         i4v q[2 * NK];
@@ -360,14 +375,21 @@ __device__ __forceinline__ void score(const Queries<D, T>& qs, const uint8_t* co
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           // one rounding each, in this order (whole numbers below 2^24 are exact)
-          float x = __builtin_fmaf((float)dm[r], s[i].x, (float)dh[r] * s[i].y) * sq[r];
-          x = x != x ? INFINITY : x;  // a block with infinite or NaN keys comes first
-          if (16 * t + 4 * kg + r < G) best = fmaxf(best, x);
+          const float y = __builtin_fmaf((float)dm[r], s[i].x, (float)dh[r] * s[i].y) * sq[r];
+          x[t][r] = y != y ? INFINITY : y;  // a block with infinite or NaN keys comes first
         }
       }
-      best = rows_max(best);
       const int b = base + 16 * i + col;
-      if (kg == 0 && b < b1) out[b] = key_of(best);
+      for (int u = 0; u < layers; ++u) {
+        float best = -INFINITY;
+#pragma unroll
+        for (int t = 0; t < T; ++t)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            if ((uint32_t)(16 * t + 4 * kg + r - u * G) < (uint32_t)G) best = fmaxf(best, x[t][r]);
+        best = rows_max(best);
+        if (kg == 0 && b < b1) out[u * step + (b - at0)] = key_of(best);
+      }
     }
   }
 }
@@ -391,33 +413,57 @@ __device__ __forceinline__ uint32_t wave_umax(uint32_t x) {
   return x;
 }
 
+template <int WAVES>
 struct Choice {
   uint32_t hist[kBins];
-  uint32_t wave[2][kWaves];
+  uint32_t wave[2][WAVES];
   uint32_t found[3];
 };
 
-// Writes a row's list: blocks before n_first, the `want` blocks of [n_first, end) with the largest
-// keys (equal ones: the lower block), blocks end .. nb - 1, and -1 up to n_select.  key(b): of a block.
-template <class Key>
-__device__ __forceinline__ void choose(Choice& sh, Key key, int nb, int n_select, int n_first, int n_recent, int32_t* out,
-                                       int tid) {
+// The lane's keys of `count`: key 64 (steps wave + j) + lane in step j < steps, so that a wave holds a run.
+// In registers (N steps at most), or read wherever they are each time (N = 0).
+template <int WAVES, int N>
+struct Keys {
+  uint32_t x[N > 0 ? N : 1];
+  const uint32_t* from;
+  int count, steps, p0;
+  __device__ __forceinline__ Keys(const uint32_t* f, int n, int lane, int wave) : from(f), count(n) {
+    steps = (n + 64 * WAVES - 1) / (64 * WAVES);
+    p0 = 64 * steps * wave + lane;
+    if constexpr (N > 0) {
+#pragma unroll
+      for (int j = 0; j < N; ++j) x[j] = j < steps && p0 + 64 * j < count ? from[p0 + 64 * j] : 0u;
+    }
+  }
+  // f(place, key, whether there is one), in order
+  template <class F>
+  __device__ __forceinline__ void each(F f) const {
+    if constexpr (N > 0) {
+#pragma unroll
+      for (int j = 0; j < N; ++j)
+        if (j < steps) f(p0 + 64 * j, x[j], p0 + 64 * j < count);
+    } else {
+#pragma unroll 4
+      for (int j = 0; j < steps; ++j) {
+        const int p = p0 + 64 * j;
+        f(p, p < count ? from[p] : 0u, p < count);
+      }
+    }
+  }
+};
+
+// The places of the `want` largest of the keys (more than `want`; equal ones: the lower place), plus `add`, to out in
+// increasing order.  Digits of eight bits from the highest one in which keys differ, by histograms of the keys
+// that share the digits found so far.
+template <int WAVES, int N>
+__device__ __forceinline__ void choose(Choice<WAVES>& sh, const Keys<WAVES, N>& keys, int want, int add, int32_t* out, int tid) {
+  static_assert(64 * WAVES >= kBins, "a thread for every bin");
   const int lane = tid & 63, wave = tid >> 6;
-  if (nb <= n_select) {
-    for (int i = tid; i < n_select; i += kThreads) out[i] = i < nb ? i : -1;
-    return;
-  }
-  const int end = nb - n_recent, want = n_select - n_first - n_recent;
-  for (int i = tid; i < n_first; i += kThreads) out[i] = i;
-  for (int i = tid; i < n_recent; i += kThreads) out[n_first + want + i] = end + i;
-  if (want == 0) return;
-  // The largest and the smallest key: digits start where they differ.
   uint32_t top = 0, low = 0;  // low: of the complements
-  for (int b = n_first + tid; b < end; b += kThreads) {
-    const uint32_t k = key(b);
+  keys.each([&](int, uint32_t k, bool has) {
     top = max(top, k);
-    low = max(low, ~k);
-  }
+    low = max(low, has ? ~k : 0u);
+  });
   top = wave_umax(top);
   low = wave_umax(low);
   if (lane == 0) {
@@ -426,33 +472,40 @@ __device__ __forceinline__ void choose(Choice& sh, Key key, int nb, int n_select
   }
   __syncthreads();
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
+  for (int w = 0; w < WAVES; ++w) {
     top = max(top, sh.wave[0][w]);
     low = max(low, sh.wave[1][w]);
   }
   uint32_t base = ~low, need = want;  // keys of [base, base + 2^bits) hold the want-th largest
-  int bits = 32 - __clz((int)(top - base) | 1);
+  int bits = 32 - __clz((int)((top - base) | 1));
   uint32_t cut, ties;  // keys above cut are chosen, and the first `ties` equal ones
   while (true) {
     const int shift = bits > 8 ? bits - 8 : 0;
+    const uint32_t bins = 1u << (bits < 8 ? bits : 8);
     __syncthreads();
-    sh.hist[tid] = 0;
+    if (tid < kBins) sh.hist[tid] = 0;
     __syncthreads();
-    for (int b = n_first + tid; b < end; b += kThreads) {
-      const uint32_t k = key(b), d = (k - base) >> shift;
-      if (k >= base && d < 1u << (bits < 8 ? bits : 8)) atomicAdd(&sh.hist[d], 1u);
-    }
+    keys.each([&](int, uint32_t k, bool has) {
+      const uint32_t d = (k - base) >> shift;
+      if (has && k >= base && d < bins) atomicAdd(&sh.hist[d], 1u);
+    });
     __syncthreads();
     // bins from the top: thread tid looks at bin 255 - tid
-    const uint32_t h = sh.hist[kBins - 1 - tid], incl = wave_scan(h);
-    if (lane == 63) sh.wave[0][wave] = incl;
+    uint32_t h = 0, incl = 0;
+    if (tid < kBins) {
+      h = sh.hist[kBins - 1 - tid];
+      incl = wave_scan(h);
+      if (lane == 63) sh.wave[0][wave] = incl;
+    }
     __syncthreads();
-    uint32_t before = incl - h;
-    for (int w = 0; w < wave; ++w) before += sh.wave[0][w];
-    if (before < need && before + h >= need) {
-      sh.found[0] = kBins - 1 - tid;
-      sh.found[1] = need - before;
-      sh.found[2] = h;
+    if (tid < kBins) {
+      uint32_t before = incl - h;
+      for (int w = 0; w < wave; ++w) before += sh.wave[0][w];
+      if (before < need && before + h >= need) {
+        sh.found[0] = kBins - 1 - tid;
+        sh.found[1] = need - before;
+        sh.found[2] = h;
+      }
     }
     __syncthreads();
     base += sh.found[0] << shift;
@@ -469,15 +522,11 @@ __device__ __forceinline__ void choose(Choice& sh, Key key, int nb, int n_select
     }
     bits = shift;
   }
-  // In order: each wave takes a run of blocks.
-  const int count = end - n_first, run = (count + 64 * kWaves - 1) / (64 * kWaves) * 64;
-  const int r0 = n_first + wave * run, r1 = min(end, r0 + run);
   uint32_t na = 0, ne = 0;
-  for (int b0 = r0; b0 < r1; b0 += 64) {
-    const uint32_t k = b0 + lane < r1 ? key(b0 + lane) : 0u;
-    na += __popcll(__ballot(k > cut));
-    ne += __popcll(__ballot(b0 + lane < r1 && k == cut));
-  }
+  keys.each([&](int, uint32_t k, bool has) {
+    na += __popcll(__ballot(has && k > cut));
+    ne += __popcll(__ballot(has && k == cut));
+  });
   __syncthreads();
   if (lane == 0) {
     sh.wave[0][wave] = na;
@@ -489,13 +538,11 @@ __device__ __forceinline__ void choose(Choice& sh, Key key, int nb, int n_select
     above += sh.wave[0][w];
     equal += sh.wave[1][w];
   }
-  uint32_t left = ties - min(equal, ties), at = n_first + above + min(equal, ties);
+  uint32_t left = ties - min(equal, ties), at = above + min(equal, ties);
   const auto below = [](uint64_t m, uint32_t x) {  // bits of m below the lane's own, added to x
     return __builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, x));
   };
-  for (int b0 = r0; b0 < r1; b0 += 64) {
-    const bool has = b0 + lane < r1;
-    const uint32_t k = has ? key(b0 + lane) : 0u;
+  keys.each([&](int p, uint32_t k, bool has) {
     bool kept = has && k > cut;
     const uint64_t e = __ballot(has && k == cut);
     if (e && left) {
@@ -503,70 +550,88 @@ __device__ __forceinline__ void choose(Choice& sh, Key key, int nb, int n_select
       left -= min(left, (uint32_t)__popcll(e));
     }
     const uint64_t m = __ballot(kept);
-    if (kept) out[below(m, at)] = b0 + lane;
+    if (kept) out[below(m, at)] = add + p;
     at += __popcll(m);
-  }
+  });
 }
 
-// The launch's row: layer, sequence and KV head.
-struct Row {
-  int layer, seq, kvh;
-};
-__device__ __forceinline__ Row row_of(const Group& g, uint32_t x) {
-  const uint32_t kvh = x % (uint32_t)g.Hkv, y = x / (uint32_t)g.Hkv;
-  return Row{(int)(y / (uint32_t)g.n_seqs), (int)(y % (uint32_t)g.n_seqs), (int)kvh};
+// Of a row's list what does not compete: the first and the last blocks, or, where there are few enough, all blocks and -1.
+// Returns how many of the others are to be chosen.
+__device__ __forceinline__ int write_fixed(int nb, int n_select, int n_first, int n_recent, int32_t* out, int tid, int threads) {
+  if (nb <= n_select) {
+    for (int i = tid; i < n_select; i += threads) out[i] = i < nb ? i : -1;
+    return 0;
+  }
+  const int want = n_select - n_first - n_recent;
+  for (int i = tid; i < n_first; i += threads) out[i] = i;
+  for (int i = tid; i < n_recent; i += threads) out[n_first + want + i] = nb - n_recent + i;
+  return want;
 }
 
 template <int D, int T>
 __global__ __launch_bounds__(kThreads) void select_kernel(SelectArgs a) {
   __shared__ __align__(16) Queries<D, T> qs;
-  __shared__ Choice sh;
-  extern __shared__ uint32_t keys[];
+  __shared__ Choice<kWaves> sh;
+  extern __shared__ uint32_t lds_keys[];  // of blocks n_first ..
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const Row r = row_of(a.g, blockIdx.x);
-  const GroupLayer& L = a.g.layers[r.layer];
-  const GroupSeq& S = a.g.seqs[r.seq];
+  const uint32_t kvh = blockIdx.x % (uint32_t)a.g.Hkv, y = blockIdx.x / (uint32_t)a.g.Hkv;
+  const GroupLayer& L = a.g.layers[y / (uint32_t)a.g.n_seqs];
+  const GroupSeq& S = a.g.seqs[y % (uint32_t)a.g.n_seqs];
   const int nb = S.stored >> 5;
   const int64_t call_row = (int64_t)L.layer * a.B + S.seq;
-  if (nb > a.n_select) {
-    qs.fill(a.q + (call_row * a.Hq + r.kvh * a.G) * D, a.G, lane, wave);
-    __syncthreads();
-    const uint8_t* index = a.index + L.index + S.index;
-    const int64_t row = ((int64_t)S.mult * a.g.Hkv + r.kvh) * a.nb_cap;
-    score<D, T>(qs, index + row * 2 * D, reinterpret_cast<const float2*>(index + a.scales) + row, a.G, a.n_first,
-                nb - a.n_recent, keys, lane, wave);
-    __syncthreads();
-  }
-  choose(sh, [&](int b) { return keys[b]; }, nb, a.n_select, a.n_first, a.n_recent,
-         a.blocks + (call_row * a.g.Hkv + r.kvh) * a.n_select, tid);
+  int32_t* out = a.blocks + (call_row * a.g.Hkv + kvh) * a.n_select;
+  const int want = write_fixed(nb, a.n_select, a.n_first, a.n_recent, out, tid, kThreads);
+  if (want == 0) return;
+  qs.fill(a.q + (call_row * a.Hq + kvh * a.G) * D, 0, a.G, a.G, lane, wave);
+  __syncthreads();
+  const uint8_t* index = a.index + L.index + S.index;
+  const int64_t row = ((int64_t)S.mult * a.g.Hkv + kvh) * a.nb_cap;
+  const int end = nb - a.n_recent;
+  score<D, T>(qs, index + row * 2 * D, reinterpret_cast<const float2*>(index + a.scales) + row, a.G, 1, a.n_first, end,
+              lds_keys, 0, a.n_first, lane, wave);
+  __syncthreads();
+  choose(sh, Keys<kWaves, 0>(lds_keys, end - a.n_first, lane, wave), want, a.n_first, out + a.n_first, tid);
 }
 
 template <int D, int T>
 __global__ __launch_bounds__(kThreads) void score_kernel(SelectArgs a) {
   __shared__ __align__(16) Queries<D, T> qs;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const Row r = row_of(a.g, blockIdx.y);
-  const GroupLayer& L = a.g.layers[r.layer];
-  const GroupSeq& S = a.g.seqs[r.seq];
+  const uint32_t kvh = blockIdx.y % (uint32_t)a.g.Hkv, y = blockIdx.y / (uint32_t)a.g.Hkv;
+  const uint32_t e = y / (uint32_t)a.g.n_seqs, sq = y % (uint32_t)a.g.n_seqs;
+  const GroupLayer& L = a.g.layers[e];
+  const GroupSeq& S = a.g.seqs[sq];
   const int nb = S.stored >> 5;
   const int b0 = a.n_first + blockIdx.x * a.chunk, b1 = min(nb - a.n_recent, b0 + a.chunk);
   if (nb <= a.n_select || b0 >= b1) return;
-  qs.fill(a.q + (((int64_t)L.layer * a.B + S.seq) * a.Hq + r.kvh * a.G) * D, a.G, lane, wave);
+  qs.fill(a.q + (((int64_t)L.layer * a.B + S.seq) * a.Hq + kvh * a.G) * D, (int64_t)a.B * a.Hq * D, a.G, a.G * L.count, lane, wave);
   __syncthreads();
   const uint8_t* index = a.index + L.index + S.index;
-  const int64_t row = ((int64_t)S.mult * a.g.Hkv + r.kvh) * a.nb_cap;
-  score<D, T>(qs, index + row * 2 * D, reinterpret_cast<const float2*>(index + a.scales) + row, a.G, b0, b1,
-              a.keys + (int64_t)blockIdx.y * a.nb_cap, lane, wave);
+  const int64_t row = ((int64_t)S.mult * a.g.Hkv + kvh) * a.nb_cap;
+  score<D, T>(qs, index + row * 2 * D, reinterpret_cast<const float2*>(index + a.scales) + row, a.G, L.count, b0, b1,
+              a.keys + (((int64_t)L.row0 * a.g.n_seqs + sq) * a.g.Hkv + kvh) * a.nb_cap,
+              (int64_t)a.g.n_seqs * a.g.Hkv * a.nb_cap, 0, lane, wave);
 }
 
-__global__ __launch_bounds__(kThreads) void choose_kernel(SelectArgs a) {
-  __shared__ Choice sh;
-  const Row r = row_of(a.g, blockIdx.x);
-  const GroupLayer& L = a.g.layers[r.layer];
-  const GroupSeq& S = a.g.seqs[r.seq];
-  const uint32_t* keys = a.keys + (int64_t)blockIdx.x * a.nb_cap;
-  choose(sh, [&](int b) { return keys[b]; }, S.stored >> 5, a.n_select, a.n_first, a.n_recent,
-         a.blocks + (((int64_t)L.layer * a.B + S.seq) * a.g.Hkv + r.kvh) * a.n_select, threadIdx.x);
+constexpr int kChooseWaves = 8;
+
+// N: steps of a wave in registers (see Keys).
+template <int N>
+__global__ __launch_bounds__(64 * kChooseWaves) void choose_kernel(SelectArgs a) {
+  __shared__ Choice<kChooseWaves> sh;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const uint32_t kvh = blockIdx.x % (uint32_t)a.g.Hkv, y = blockIdx.x / (uint32_t)a.g.Hkv;
+  const uint32_t l = y / (uint32_t)a.g.n_seqs;
+  const GroupSeq& S = a.g.seqs[y % (uint32_t)a.g.n_seqs];
+  int e = 0;
+  while (e + 1 < a.g.n_layers && l >= a.g.layers[e + 1].row0) ++e;
+  const int64_t layer = a.g.layers[e].layer + (l - a.g.layers[e].row0);
+  const int nb = S.stored >> 5;
+  int32_t* out = a.blocks + ((layer * a.B + S.seq) * a.g.Hkv + kvh) * a.n_select;
+  const int want = write_fixed(nb, a.n_select, a.n_first, a.n_recent, out, tid, 64 * kChooseWaves);
+  if (want == 0) return;
+  const uint32_t* keys = a.keys + (int64_t)blockIdx.x * a.nb_cap + a.n_first;
+  choose(sh, Keys<kChooseWaves, N>(keys, nb - a.n_recent - a.n_first, lane, wave), want, a.n_first, out + a.n_first, tid);
 }
 
 }  // namespace
@@ -576,6 +641,8 @@ using namespace kvk;
 namespace {
 
 constexpr int kResident = 8192;  // keys of a row in LDS
+// Rows of few workgroups and many blocks: one workgroup a row would read the index alone (8 rows of 1024
+// blocks 22 us, in two launches 17; of 4096 blocks 62 and 19; 32 rows of 218 blocks, the other way, 12 and 17).
 constexpr int64_t kFewRows = 512;
 constexpr int kLongRow = 1024;
 
@@ -600,37 +667,34 @@ kvk_status check_lengths(const kvk_table* t, const char* what, const char* name,
 
 const kvk_table* first_of(const kvk_table* t) { return t->seq.empty() ? t : t->seq[0]; }
 
-template <int D, int QS>
-void launch_index(int bits, dim3 g, const IndexArgs& a, hipStream_t st) {
-  const dim3 b(256);
-  if (bits == 16) hipLaunchKernelGGL((index_kernel<D, 16, kQsKivi>), g, b, 0, st, a);
-  else if (bits == 8) hipLaunchKernelGGL((index_kernel<D, 8, QS>), g, b, 0, st, a);
-  else if (bits == 4) hipLaunchKernelGGL((index_kernel<D, 4, QS>), g, b, 0, st, a);
-  else hipLaunchKernelGGL((index_kernel<D, 2, QS>), g, b, 0, st, a);
-}
 template <int D>
-void launch_index(int qs, int bits, dim3 g, const IndexArgs& a, hipStream_t st) {
-  if (qs == KVK_Q_KIVI32) launch_index<D, kQsKivi>(bits, g, a, st);
-  else if (qs == KVK_Q_GROUP64) launch_index<D, kQsG64>(bits, g, a, st);
-  else launch_index<D, kQsSym>(bits, g, a, st);
+void launch_index(int qs, dim3 g, const IndexArgs& a, hipStream_t st) {
+  const dim3 b(256);
+  if (qs == KVK_Q_KIVI32) hipLaunchKernelGGL((index_kernel<D, kQsKivi>), g, b, 0, st, a);
+  else if (qs == KVK_Q_GROUP64) hipLaunchKernelGGL((index_kernel<D, kQsG64>), g, b, 0, st, a);
+  else hipLaunchKernelGGL((index_kernel<D, kQsSym>), g, b, 0, st, a);
 }
 
+// n: blocks that compete at most.
 template <int D, int T>
-void launch_select(const SelectArgs& a, uint32_t rows, int32_t nb, bool two, hipStream_t st) {
-  const dim3 b(kThreads);
+void launch_select(const SelectArgs& a, int32_t n, bool two, hipStream_t st) {
+  const unsigned per_layer = a.g.n_seqs * a.g.Hkv;
   if (!two) {
-    hipLaunchKernelGGL((select_kernel<D, T>), dim3(rows), b, nb > a.n_select ? 4 * (size_t)nb : 0, st, a);
-  } else {
-    const int32_t n = nb - a.n_first - a.n_recent;
-    hipLaunchKernelGGL((score_kernel<D, T>), dim3((n + a.chunk - 1) / a.chunk, rows), b, 0, st, a);
-    hipLaunchKernelGGL(choose_kernel, dim3(rows), b, 0, st, a);
+    hipLaunchKernelGGL((select_kernel<D, T>), dim3(per_layer * a.g.n_layers), dim3(kThreads), 4 * (size_t)n, st, a);
+    return;
   }
+  if (n > 0)
+    hipLaunchKernelGGL((score_kernel<D, T>), dim3((n + a.chunk - 1) / a.chunk, per_layer * a.g.n_layers), dim3(kThreads), 0, st, a);
+  const dim3 g(per_layer * a.g.n_rows), b(64 * kChooseWaves);
+  if (n <= 8 * 64 * kChooseWaves) hipLaunchKernelGGL(choose_kernel<8>, g, b, 0, st, a);
+  else if (n <= 32 * 64 * kChooseWaves) hipLaunchKernelGGL(choose_kernel<32>, g, b, 0, st, a);
+  else hipLaunchKernelGGL(choose_kernel<0>, g, b, 0, st, a);
 }
 template <int D>
-void launch_select(const SelectArgs& a, uint32_t rows, int32_t nb, bool two, hipStream_t st) {
-  if (a.G <= 16) launch_select<D, 1>(a, rows, nb, two, st);
-  else if (a.G <= 32) launch_select<D, 2>(a, rows, nb, two, st);
-  else launch_select<D, 4>(a, rows, nb, two, st);
+void launch_select(const SelectArgs& a, int32_t rows, int32_t n, bool two, hipStream_t st) {
+  if (rows <= 16) launch_select<D, 1>(a, n, two, st);
+  else if (rows <= 32) launch_select<D, 2>(a, n, two, st);
+  else launch_select<D, 4>(a, n, two, st);
 }
 
 }  // namespace
@@ -685,21 +749,20 @@ extern "C" kvk_status kvk_index_blocks(const kvk_table* t, int32_t l0, int32_t l
   a.nb_cap = t->nb_cap;
   for (const bool go : {false, true}) {
     const kvk_status st = for_groups(
-        t, l0, l1, true, true, a.g,
+        t, l0, l1, Layers::anchors, false, a.g,
         [&](int b, GroupSeq& s) {
           s.stored = n_stored[b];
           s.first = n_indexed ? n_indexed[b] / 32 : 0;
           return s.stored / 32 > s.first;
         },
-        [&](int bits, Group& g) -> kvk_status {
+        [&](int, Group& g) -> kvk_status {
           int64_t most = 0;
           for (int i = 0; i < g.n_seqs; ++i) most = std::max<int64_t>(most, g.seqs[i].stored / 32 - g.seqs[i].first);
-          a.block_bytes = (int32_t)gqa_block_bytes(d.head_dim, bits, d.qscheme);
           const dim3 grid((unsigned)((most + 3) / 4), (unsigned)d.n_kv_heads, (unsigned)(g.n_layers * g.n_seqs));
           if ((int64_t)grid.x * grid.y * grid.z > 0xffffffLL) return fail(KVK_ERR_UNSUPPORTED, "%s: grid too large", what);
           if (!go) return KVK_OK;
-          if (d.head_dim == 128) launch_index<128>(d.qscheme, bits, grid, a, stream);
-          else launch_index<64>(d.qscheme, bits, grid, a, stream);
+          if (d.head_dim == 128) launch_index<128>(d.qscheme, grid, a, stream);
+          else launch_index<64>(d.qscheme, grid, a, stream);
           const hipError_t e = hipGetLastError();
           if (e != hipSuccess) return fail(KVK_ERR_DEVICE, "%s launch: %s", what, hipGetErrorString(e));
           return KVK_OK;
@@ -758,24 +821,27 @@ extern "C" kvk_status kvk_select_blocks(const kvk_table* t, int32_t l0, int32_t 
   a.n_select = n_select;
   a.n_first = n_first;
   a.n_recent = n_recent;
-  a.chunk = 512;
   for (const bool go : {false, true}) {
     const kvk_status st = for_groups(
-        t, l0, l1, false, false, a.g,
+        t, l0, l1, two ? Layers::readers : Layers::each, false, a.g,
         [&](int b, GroupSeq& s) {
           s.stored = n_stored[b];
           return true;
         },
         [&](int, Group& g) -> kvk_status {
-          const int64_t rows = (int64_t)g.n_layers * g.n_seqs * d.n_kv_heads;
-          int32_t most = 0;
+          const int64_t rows = (int64_t)g.n_rows * g.n_seqs * d.n_kv_heads;
+          int32_t most = 0, readers = 1;
           for (int i = 0; i < g.n_seqs; ++i) most = std::max(most, g.seqs[i].stored / 32);
-          const bool split = two && most > n_select;
-          if (rows > (split ? 65535 : 0xffffff) || (split && (int64_t)most / a.chunk * rows > 0xfffff0))
-            return fail(KVK_ERR_UNSUPPORTED, "%s: grid too large", what);
+          for (int i = 0; i < g.n_layers; ++i) readers = std::max<int32_t>(readers, g.layers[i].count);
+          const int32_t n = most > n_select ? most - n_first - n_recent : 0;  // blocks that compete
+          // (8 rows of 4096 blocks: chunks of 256 take 19 us, of 512 23; 256 rows 35 and 33)
+          a.chunk = (int64_t)n * rows >= 512 * 1024 ? 512 : 256;
+          const int64_t chunks = (n + a.chunk - 1) / a.chunk;
+          // (a grid has less than 2^32 threads)
+          if (rows > (two ? 65535 : 0x7fffff) || chunks * rows > 0xffffff) return fail(KVK_ERR_UNSUPPORTED, "%s: grid too large", what);
           if (!go) return KVK_OK;
-          if (d.head_dim == 128) launch_select<128>(a, (uint32_t)rows, most, split, stream);
-          else launch_select<64>(a, (uint32_t)rows, most, split, stream);
+          if (d.head_dim == 128) launch_select<128>(a, readers * a.G, n, two, stream);
+          else launch_select<64>(a, readers * a.G, n, two, stream);
           const hipError_t e = hipGetLastError();
           if (e != hipSuccess) return fail(KVK_ERR_DEVICE, "%s launch: %s", what, hipGetErrorString(e));
           return KVK_OK;

@@ -8,6 +8,7 @@ with an error (there is no fallback path).
 """
 import ctypes
 import os
+import struct
 from array import array
 from dataclasses import dataclass
 from typing import List, Optional, Sequence
@@ -714,14 +715,9 @@ def chunk_attention(t: Table, layer_begin: int, layer_end: int, q: torch.Tensor,
                                       _nbytes(workspace), _stream(stream)))
 
 
-class _Strides(ctypes.Structure):
-    _fields_ = [("seq", ctypes.c_int64), ("head", ctypes.c_int64), ("token", ctypes.c_int64)]
-
-
-class _RotaryRows(ctypes.Structure):
-    _fields_ = [("in_", ctypes.c_void_p), ("out", ctypes.c_void_p), ("n_heads", ctypes.c_int32),
-                ("head_dim", ctypes.c_int32), ("first", ctypes.c_int32), ("in_strides", _Strides),
-                ("out_strides", _Strides)]
+# A kvk_rotary_rows: in, out, heads, head_dim, first, the strides of in and of out (packed by hand: ctypes'
+# structures cost half of a small call's host time).
+_ROTARY_ROWS = struct.Struct("=QQiii4x6q")
 
 
 def rotary_frequencies(width: int, base: float = 10000.0, factor: float = 1.0, original_tokens: int = 0,
@@ -787,14 +783,14 @@ def rotate(rot: Rotary, positions: torch.Tensor, tensors: Sequence[torch.Tensor]
     if rank not in (3, 4):
         raise ValueError("tensors must be [tokens, heads, d] or [B, heads, n, d]")
     seqs, n = (1, x0.shape[0]) if rank == 3 else (x0.shape[0], x0.shape[2])
-    rows = (_RotaryRows * count)()
-    for r, x, y, f in zip(rows, tensors, outs, firsts):
-        if (x.dtype != x0.dtype or y.dtype != x0.dtype or x.dim() != rank or x.shape != y.shape or x.stride(-1) != 1
-                or y.stride(-1) != 1 or (x.shape[0] if rank == 3 else x.shape[2]) != n or (rank == 4 and x.shape[0] != seqs)):
+    rows, dtype = b"", x0.dtype
+    for x, y, f in zip(tensors, outs, firsts):
+        shape = x.shape
+        if (x.dtype != dtype or y.dtype != dtype or len(shape) != rank or shape != y.shape or x.stride(-1) != 1
+                or y.stride(-1) != 1 or (shape[0] if rank == 3 else shape[2]) != n or (rank == 4 and shape[0] != seqs)):
             raise ValueError("tensors and outputs must agree in dtype, tokens and sequences, with contiguous rows")
-        r.in_, r.out, r.n_heads, r.head_dim, r.first = x.data_ptr(), y.data_ptr(), x.shape[1], x.shape[-1], f
-        a, b = _rotary_strides(x), _rotary_strides(y)
-        r.in_strides, r.out_strides = _Strides(*a), _Strides(*b)
+        a = _rotary_strides(x)
+        rows += _ROTARY_ROWS.pack(x.data_ptr(), y.data_ptr(), shape[1], shape[-1], f, *a, *(a if y is x else _rotary_strides(y)))
     if positions.dtype != torch.int32 or not positions.is_contiguous() or positions.dim() > 2 or positions.shape[-1:] != (n,):
         raise ValueError(f"positions must be contiguous int32 [{n}] or [rows, {n}]")
     _here(positions, *tensors, *outs)

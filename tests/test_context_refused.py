@@ -86,17 +86,32 @@ def test_rotary_create_refused():
         kvk.rotary(12, [1.0] * 6)
 
 
+class Strides(ctypes.Structure):  # kvk_strides
+    _fields_ = [(n, ctypes.c_int64) for n in ("seq", "head", "token")]
+
+
+class Rows(ctypes.Structure):  # kvk_rotary_rows
+    _fields_ = [("in_", ctypes.c_void_p), ("out", ctypes.c_void_p), ("n_heads", I32), ("head_dim", I32), ("first", I32),
+                ("in_strides", Strides), ("out_strides", Strides)]
+
+
+def test_the_binding_packs_rows_as_c_does():
+    assert kvk._ROTARY_ROWS.size == ctypes.sizeof(Rows)
+    x = Rows(1, 2, 3, 4, 5, Strides(6, 7, 8), Strides(9, 10, 11))
+    assert kvk._ROTARY_ROWS.pack(1, 2, 3, 4, 5, 6, 7, 8, 9, 10, 11) == bytes(x)
+
+
 def _rows(**kw):
     a = dict(in_=P0, out=P0 + (1 << 20), n_heads=4, head_dim=64, first=0, in_strides=(2048, 64, 256), out_strides=(2048, 64, 256))
     a.update(kw)
-    a["in_strides"], a["out_strides"] = kvk._Strides(*a["in_strides"]), kvk._Strides(*a["out_strides"])
-    return kvk._RotaryRows(**a)
+    a["in_strides"], a["out_strides"] = Strides(*a["in_strides"]), Strides(*a["out_strides"])
+    return Rows(**a)
 
 
 def _rotate(rows=None, width=64, seqs=2, tokens=8, positions=P0, pos_seqs=1, n=None, dtype=kvk.BF16, rot=0):
     rows = [_rows()] if rows is None else rows
     rot = kvk.rotary(width, [0.5] * (width // 2)) if rot == 0 else rot
-    arr = (kvk._RotaryRows * max(1, len(rows)))(*rows)
+    arr = (Rows * max(1, len(rows)))(*rows)
     return kvk.load().kvk_rotate(rot.handle if rot else None, seqs, tokens, positions, pos_seqs, arr,
                                  len(rows) if n is None else n, dtype, 0, None)
 

@@ -201,7 +201,7 @@ def _chosen(q, codes, scales, nb, n_select, first, recent):
         return list(range(nb)) + [-1] * (n_select - nb)
     x = q.float()
     top = x.abs().amax(-1, keepdim=True)
-    s = (top / 127)
+    s = top * torch.tensor(1 / 127, dtype=torch.float32, device=q.device)
     s = torch.where(torch.isfinite(x).all(-1, keepdim=True), s, torch.zeros_like(s))
     q8 = torch.where(s > 0, torch.round(x / torch.where(s > 0, s, torch.ones_like(s))), torch.zeros_like(x)).to(F64)
     m = codes[:nb].to(F64)
