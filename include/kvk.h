@@ -821,7 +821,7 @@ kvk_status kvk_index_blocks(const kvk_table* table, int32_t layer_begin, int32_t
  * is NaN counts as infinite (blocks with infinite or NaN keys come first), equal scores go to the lower block.
  *   q        : device bf16 [layer_end-layer_begin][B][Hq][d_h].
  *   n_stored : host [B]; the nb = n_stored[b] / 32 full blocks compete.
- *   n_select : blocks chosen, >= 1; the n_first first and the n_recent last blocks are among them in any
+ *   n_select : blocks chosen, 1 .. 2^30; the n_first first and the n_recent last blocks are among them in any
  *              case (n_first + n_recent <= n_select).
  *   blocks   : device int32 [layer_end-layer_begin][B][Hkv][n_select], written in increasing order; where
  *              a sequence has fewer blocks, all of them and then -1.
@@ -844,13 +844,13 @@ kvk_status kvk_select_blocks(const kvk_table* table, int32_t layer_begin, int32_
  *              n_stored[b] % 32 tokens.
  *   blocks   : device int32 [layer_end-layer_begin][B][Hkv][n_select], any order; entries outside
  *              0 .. n_stored[b] / 32 - 1 are passed over, a block listed twice counts twice.
- *   n_select : >= 1.
+ *   n_select : 1 .. 2^30.
  *   out      : device bf16, as q; zeros where no token is seen.
  *   workspace: device, >= kvk_block_workspace_bytes of the range and n_select, 256-byte aligned; its contents on
  *              entry are ignored.  Calls that overlap on one workspace race.
  * Layers that share an anchor read their own blocks of it.  Per-sequence tables need no set-up.  Values are
  * held as by kvk_chunk_attention (fp16 for quantised layers, KIVI32's and GROUP64's dequantised values within
- * its range; SYMROW's of any size, its value scales as there), sums in fp32.  A row whose seen scores are
+ * its range; SYMROW's keys of any size, its values as there), sums in fp32.  A row whose seen scores are
  * all -inf, or NaN in one, yields NaN; infinite values count as in kvk_prompt_attention.
  * Errors: KVK_ERR_INVALID (range, lengths, scale not finite, NULL, misalignment: q, arena and out 16 B, blocks
  *         4 B, workspace 256 B; host memory), KVK_ERR_BUFFER (workspace), KVK_ERR_UNSUPPORTED (MLA table; too

@@ -30,8 +30,8 @@ FLAGS = [
 # Per-source flags.  The selector's attention kernel rescales its product
 # accumulators on the VALU now and then; with the accumulators in AGPRs the compiler
 # copies them to VGPRs and back on every loop iteration, so its MFMAs write VGPRs; the
-# prompt, chunk and block kernels do the same.
-EXTRA = {src: ["-mllvm", "-amdgpu-mfma-vgpr-form"] for src in ("selector.hip", "prompt.hip", "chunk.hip", "blocks.hip")}
+# prompt, chunk and block kernels do the same, and the index kernel's minima run over what its MFMAs write.
+EXTRA = {src: ["-mllvm", "-amdgpu-mfma-vgpr-form"] for src in ("selector.hip", "prompt.hip", "chunk.hip", "blocks.hip", "index.hip")}
 
 
 def _compile(src: str) -> str:

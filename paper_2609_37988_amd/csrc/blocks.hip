@@ -11,12 +11,17 @@
 // so that a head's maximum and sum live in its column and the probabilities feed the second product
 // from where the first left them.  The next block's bytes are in flight meanwhile.
 //
-// Precision, in quantised layers: codes are exact in fp16.  KIVI32's keys and values, and GROUP64's
-// values, are dequantised to fp16 (2^-11 of a value's ulp range, one rounding); the scales of GROUP64's keys and of SYMROW's
-// keys multiply the products, in fp32; SYMROW's value scales (bf16, beyond fp16's range) multiply the probabilities, each block
-// scaled by the power of two that brings its largest to [1, 2).  Queries are bf16, in fp16 exactly (each row scaled by
-// a power of two); probabilities fp16, kept below 2^15.  16-bit layers: keys, values and queries exact, the probabilities bf16.
-// The window's probabilities enter as two bf16 parts in quantised layers.  Sums are fp32, outputs rounded once, to bf16.
+// Precision, in quantised layers: codes are exact in fp16.  KIVI32's keys and values, and GROUP64's values, are
+// dequantised to fp16 (one rounding, 2^-11); the scales of GROUP64's and SYMROW's keys multiply the products, in fp32;
+// SYMROW's value scales (bf16, beyond fp16's range) multiply the probabilities, each block's scaled by the power of two
+// that brings the largest to [1, 2).  Queries are bf16, in fp16 exactly (each row scaled by a power of two, values
+// 2^29 times smaller than its largest lose digits); probabilities fp16, at most 2^15.  16-bit layers: keys, values and
+// queries exact, the probabilities bf16.  The window's probabilities enter as two bf16 parts in quantised layers.
+// Sums are fp32, outputs rounded once, to bf16.
+//
+// Bound.  8 and 16 bits: HBM, where rows are enough (256 streams of 8192 tokens, 32 blocks for each of two layers, int8,
+// 152 MB: 31 us, 4.9 TB/s).  2 bits: about 300 vector instructions a block (96 rows of 256 blocks, 76 MB: 24.5 us with the
+// merge of five parts, 4.5 of them).  Few rows: the chain launch, list, block, join (32 rows of 16 4-bit blocks 9 us).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -172,9 +177,6 @@ __device__ __forceinline__ float queries_to_half(u4v (&q)[NJ], float c, int most
   return __builtin_ldexpf(c, -up);
 }
 
-#ifndef KVK_RING
-#define KVK_RING 2
-#endif
 // One full block.  q: the queries (fp16, bf16 in 16-bit layers); qsum: GROUP64, their sums by 64 channels.
 template <int D, int BITS, int QS>
 __device__ __forceinline__ void attend(State<D>& st, const Raw<D, BITS, QS>& r, const u4v (&q)[D / 32], const float* qsum,
@@ -244,9 +246,9 @@ __device__ __forceinline__ void attend(State<D>& st, const Raw<D, BITS, QS>& r, 
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         float y = acc[tau][e];
-        if constexpr (HALF && QS == kQsSym) {
+        if constexpr (HALF && QS == kQsSym) {  // (with c at once: a lifted query's score may be beyond fp32 before c)
           const uint32_t w = r.m[2 * tau + (e >> 1)];
-          y *= __uint_as_float(e & 1 ? w & 0xffff0000u : w << 16);
+          y *= __uint_as_float(e & 1 ? w & 0xffff0000u : w << 16) * c;
         }
         x[4 * tau + e] = y;
       }
@@ -265,7 +267,7 @@ __device__ __forceinline__ void attend(State<D>& st, const Raw<D, BITS, QS>& r, 
     const int ex = __builtin_amdgcn_readfirstlane((int)(t >> 23));
     const int up = ex == 0 ? 0 : max(min(127 - ex, kBlockLift), -kBlockLift);
     const float f = power_of_two(up);
-    softmax_step<D>(st, x, c, bias, (float)up, f);
+    softmax_step<D>(st, x, 1.0f, bias, (float)up, f);
 #pragma unroll
     for (int e = 0; e < 8; ++e) x[e] *= vs[e] * f;
     const u4v p = pack8<true>(x);
@@ -411,9 +413,9 @@ __global__ __launch_bounds__(64 * W, 2) void block_kernel(BlockArgs a) {
     mask &= mask - 1;
     return __builtin_amdgcn_readlane(entry, i);
   };
-  // A ring of RING blocks in flight.  Past the list's end the loads go past the full blocks' range, where they read
+  // Two blocks in flight (three and four were as fast at best: 4-bit 16.2 and 17.4 us against 14.5).  Past the list's end the loads go past the full blocks' range, where they read
   // nothing: no branch, so that the compiler can count the loads outstanding.
-  constexpr int RING = KVK_RING;
+  constexpr int RING = 2;
   const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(stream), (short)0, nbf * a.block_bytes, 0x00020000);
   R raw[RING];
   int cur[RING];
@@ -558,14 +560,14 @@ using namespace kvk;
 
 namespace {
 
-#ifndef KVK_AIM
-#define KVK_AIM 512
-#define KVK_MINB 4
-#endif
-constexpr int64_t kAimWgs = KVK_AIM;
 constexpr int64_t kCus = 256;
 
-// Waves of a workgroup and parts of each list.
+// Waves of a workgroup and parts of each list.  From a row (sixteen heads of a layer, sequence and KV head) per CU
+// on, lists are whole: a second launch and the parts' records cost more than they save (512 rows of 32
+// 8-bit blocks: whole 34 us, in two parts 38); eight waves share one where four would leave a CU half empty (256
+// rows of 32 4-bit blocks: 14.5 us, four waves 18).  Fewer rows are split to two workgroups per CU, down to
+// four blocks a wave (96 rows of 256 2-bit blocks: five parts 31 us, ten 31, two 52; 64 rows of 64 bf16 blocks:
+// four blocks a wave 20, two 22).
 struct Shape {
   int32_t waves, splits;
 };
@@ -573,7 +575,7 @@ Shape shape_of(const kvk_table* t, int32_t l0, int32_t l1, int32_t n_select) {
   const int64_t G = t->d.n_q_heads / t->d.n_kv_heads;
   const int64_t rows = (int64_t)(l1 - l0) * t->d.batch * t->d.n_kv_heads * ((G + 15) / 16);
   if (rows >= kCus) return Shape{rows < 2 * kCus && n_select > 16 ? 8 : 4, 1};
-  return Shape{4, (int32_t)std::max<int64_t>(1, std::min<int64_t>(kAimWgs / rows, n_select / (4 * KVK_MINB)))};
+  return Shape{4, (int32_t)std::max<int64_t>(1, std::min<int64_t>(2 * kCus / rows, n_select / 16))};
 }
 
 kvk_status check_call(const kvk_table* t, const char* what, int32_t l0, int32_t l1, int32_t n_select) {
@@ -581,7 +583,7 @@ kvk_status check_call(const kvk_table* t, const char* what, int32_t l0, int32_t 
   if (t->d.kind != KVK_GQA) return fail(KVK_ERR_UNSUPPORTED, "%s: GQA tables only", what);
   if (l0 < 0 || l1 > t->d.n_layers || l0 >= l1)
     return fail(KVK_ERR_INVALID, "layer range [%d, %d) invalid for %d layers", l0, l1, t->d.n_layers);
-  if (n_select < 1) return fail(KVK_ERR_INVALID, "%s: n_select %d", what, n_select);
+  if (n_select < 1 || n_select > 1 << 30) return fail(KVK_ERR_INVALID, "%s: n_select %d", what, n_select);
   return KVK_OK;
 }
 
@@ -652,9 +654,8 @@ extern "C" kvk_status kvk_block_attention(const kvk_table* t, int32_t l0, int32_
   a.nb_cap = t->nb_cap;
   a.qsign = scale > 0.0f ? 1 : (scale < 0.0f ? -1 : 0);
   a.c = a.qsign ? std::fabs(scale) * kLog2e : 1.0f;
-  // c / 2^(most_lift + kBlockLift) stays a normal number; queries so small that this binds give
-  // logits that do not count.  (c itself may have overflowed)
-  a.most_lift = std::isinf(a.c) ? 120 : std::min(120, std::ilogb(a.c) + 60);
+  // c / 2^most_lift stays a normal number (c itself may have overflowed)
+  a.most_lift = std::isinf(a.c) ? 120 : std::min(120, std::ilogb(a.c) + 125);
   const int64_t rows = (int64_t)(l1 - l0) * d.batch * d.n_q_heads;
   if (rows > 0x7fffffffLL) return fail(KVK_ERR_UNSUPPORTED, "%s: too many query rows in one call", what);
   for (const bool go : {false, true}) {

@@ -7,14 +7,20 @@
 // one fp32 scale for each part (the query's, one for both), so that the products are sums of integers:
 // exact, the same in any order, and the choice is the same on every run.
 //
-//   index_kernel   one wave per block.  Its keys pass through the matrix cores (a product with a
-//                  selection of 16 channels is exact and turns tokens x channels into one channel per
-//                  lane), so that minima and maxima run over registers; codes are enough for KIVI32,
-//                  whose scale and zero belong to the channel.  Sums, scales and codes are in 64 bits:
-//                  they cost a wave 4 values per lane.
-//   select_kernel  one workgroup per (layer, sequence, KV head): scores into LDS, then the choice.
-//   score_kernel, choose_kernel  the same in two launches, the scores through the workspace: for
-//                  launches of few rows or of more blocks than LDS holds.
+//   index_kernel   one wave per block.  Its keys pass through the matrix cores (a product with a selection of 16
+//                  channels is exact and turns tokens x channels into one channel per lane), so that minima and
+//                  maxima run over registers; codes are enough for KIVI32, whose scale and zero belong to the
+//                  channel.  Middles, scales and codes are in 64 bits: four values per lane.
+//                  Bound: about 400 vector instructions a block beside its keys' bytes (27 700 blocks of four
+//                  bit-widths, 117 MB of keys: 38 us, 3.1 TB/s; a launch per bit-width 66).  One block per
+//                  sequence (256 blocks): 4.7 us, the latency of a block.
+//   select_kernel  one workgroup per (layer, sequence, KV head): scores into LDS, then the choice.  Bound: latency
+//                  (32 rows of up to 218 blocks 9 us); 12 288 rows of 256 blocks 110 us.
+//   score_kernel, choose_kernel  the same in two launches, the scores through the workspace: for launches of few rows
+//                  or of more blocks than LDS holds.  The layers that read one anchor share a read of its index.
+//                  Bound: the index's bytes, then the choice's latency (128 indexes of up to 4096 blocks, 117 MB, two
+//                  layers each: 28 us, 4.2 TB/s, and 8 us; a read for each layer 43 and, keys read again for every
+//                  digit, 19).
 #include <hip/hip_runtime.h>
 
 #include <cmath>
@@ -80,9 +86,15 @@ __device__ __forceinline__ float eight_bits(const double (&x)[N], int (&code)[N]
 #pragma unroll
   for (int i = 0; i < N; ++i) top = fmaxf(top, (float)quotient(__builtin_fabs(x[i]), 127.0, 1.0 / 127.0));
   top = rows_max(max16(top));  // (rounding keeps the order)
-  const double s = (double)top, r = top > 0.0f ? 1.0 / s : 0.0;
+  const double s = (double)top;
+  double r = 0.0;
+  if (top > 0.0f) {  // 1 / s by two steps of Newton's iteration
+    r = __builtin_amdgcn_rcp(s);
+    r = __builtin_fma(__builtin_fma(-s, r, 1.0), r, r);
+    r = __builtin_fma(__builtin_fma(-s, r, 1.0), r, r);
+  }
 #pragma unroll
-  for (int i = 0; i < N; ++i) code[i] = (int)fmin(fmax(__builtin_rint(quotient(x[i], s, r)), -127.0), 127.0);
+  for (int i = 0; i < N; ++i) code[i] = min(max((int)__builtin_rint(quotient(x[i], s, r)), -127), 127);
   return top;
 }
 
@@ -153,6 +165,14 @@ __device__ __forceinline__ void index_block(const uint8_t* p, uint8_t* codes, fl
     for (int i = 0; i < 4; ++i)
       sel[h][i] = kg == 2 * h + (n >> 3) && ((n & 7) >> 1) == i ? (n & 1 ? kOne << 16 : kOne) : 0u;
 
+  // Codes are not negative, so they order as their bits do; as integers they need no quieting of NaN.
+  constexpr bool CODES = BITS != 16 && QS == kQsKivi;
+  const auto least = [](float x, float y) {
+    return CODES ? __uint_as_float(min(__float_as_uint(x), __float_as_uint(y))) : fminf(x, y);
+  };
+  const auto most = [](float x, float y) {
+    return CODES ? __uint_as_float(max(__float_as_uint(x), __float_as_uint(y))) : fmaxf(x, y);
+  };
   float lo[NC], hi[NC];
   float nan = 0.0f;
 #pragma unroll
@@ -192,13 +212,13 @@ __device__ __forceinline__ void index_block(const uint8_t* p, uint8_t* codes, fl
       lo[c] = hi[c] = x[0];
 #pragma unroll
       for (int e = 1; e < 8; ++e) {
-        lo[c] = fminf(lo[c], x[e]);
-        hi[c] = fmaxf(hi[c], x[e]);
+        lo[c] = least(lo[c], x[e]);
+        hi[c] = most(hi[c], x[e]);
       }
     }
   }
-  rows_scatter(lo, [](float x, float y) { return fminf(x, y); });
-  rows_scatter(hi, [](float x, float y) { return fmaxf(x, y); });
+  rows_scatter(lo, least);
+  rows_scatter(hi, most);
   double mid[NV], half[NV];
 #pragma unroll
   for (int v = 0; v < NV; ++v) {
@@ -271,7 +291,7 @@ struct SelectArgs {
   uint32_t* keys;      // [rows of the launch][nb_cap], in the workspace
   int64_t scales;
   int32_t nb_cap, B, Hq, G, n_select, n_first, n_recent;
-  int32_t chunk;       // blocks that a workgroup of score_kernel scores
+  int32_t chunk, chunks;  // blocks that a workgroup of score_kernel scores, and workgroups of a row
   Group g;
 };
 static_assert(sizeof(SelectArgs) <= 4096, "kernel arguments");
@@ -407,10 +427,19 @@ __device__ __forceinline__ uint32_t wave_scan(uint32_t x) {
   x = dpp_add<0x142, 0xA>(x);  // the last lane of a row to the next row
   return dpp_add<0x143, 0xC>(x);  // ... of the first half to the second
 }
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t dpp_max(uint32_t x) {
+  return max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, ROWS, 0xF, false));
+}
+// The largest of the wave, by the steps of the prefix sum.
 __device__ __forceinline__ uint32_t wave_umax(uint32_t x) {
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) x = max(x, (uint32_t)__shfl_xor((int)x, d));
-  return x;
+  x = dpp_max<0x111, 0xF>(x);
+  x = dpp_max<0x112, 0xF>(x);
+  x = dpp_max<0x114, 0xF>(x);
+  x = dpp_max<0x118, 0xF>(x);
+  x = dpp_max<0x142, 0xA>(x);
+  x = dpp_max<0x143, 0xC>(x);
+  return (uint32_t)__builtin_amdgcn_readlane((int)x, 63);
 }
 
 template <int WAVES>
@@ -597,12 +626,13 @@ template <int D, int T>
 __global__ __launch_bounds__(kThreads) void score_kernel(SelectArgs a) {
   __shared__ __align__(16) Queries<D, T> qs;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const uint32_t kvh = blockIdx.y % (uint32_t)a.g.Hkv, y = blockIdx.y / (uint32_t)a.g.Hkv;
+  const uint32_t part = blockIdx.x % (uint32_t)a.chunks, r = blockIdx.x / (uint32_t)a.chunks;
+  const uint32_t kvh = r % (uint32_t)a.g.Hkv, y = r / (uint32_t)a.g.Hkv;
   const uint32_t e = y / (uint32_t)a.g.n_seqs, sq = y % (uint32_t)a.g.n_seqs;
   const GroupLayer& L = a.g.layers[e];
   const GroupSeq& S = a.g.seqs[sq];
   const int nb = S.stored >> 5;
-  const int b0 = a.n_first + blockIdx.x * a.chunk, b1 = min(nb - a.n_recent, b0 + a.chunk);
+  const int b0 = a.n_first + part * a.chunk, b1 = min(nb - a.n_recent, b0 + a.chunk);
   if (nb <= a.n_select || b0 >= b1) return;
   qs.fill(a.q + (((int64_t)L.layer * a.B + S.seq) * a.Hq + kvh * a.G) * D, (int64_t)a.B * a.Hq * D, a.G, a.G * L.count, lane, wave);
   __syncthreads();
@@ -684,7 +714,7 @@ void launch_select(const SelectArgs& a, int32_t n, bool two, hipStream_t st) {
     return;
   }
   if (n > 0)
-    hipLaunchKernelGGL((score_kernel<D, T>), dim3((n + a.chunk - 1) / a.chunk, per_layer * a.g.n_layers), dim3(kThreads), 0, st, a);
+    hipLaunchKernelGGL((score_kernel<D, T>), dim3(a.chunks * per_layer * a.g.n_layers), dim3(kThreads), 0, st, a);
   const dim3 g(per_layer * a.g.n_rows), b(64 * kChooseWaves);
   if (n <= 8 * 64 * kChooseWaves) hipLaunchKernelGGL(choose_kernel<8>, g, b, 0, st, a);
   else if (n <= 32 * 64 * kChooseWaves) hipLaunchKernelGGL(choose_kernel<32>, g, b, 0, st, a);
@@ -790,7 +820,7 @@ extern "C" kvk_status kvk_select_blocks(const kvk_table* t, int32_t l0, int32_t 
   if (kvk_status st = check_call(t, what, l0, l1)) return st;
   const kvk_dims& d = t->d;
   if (!q || !n_stored || !index || !blocks) return fail(KVK_ERR_INVALID, "%s: NULL buffer", what);
-  if (n_select < 1) return fail(KVK_ERR_INVALID, "%s: n_select %d", what, n_select);
+  if (n_select < 1 || n_select > 1 << 30) return fail(KVK_ERR_INVALID, "%s: n_select %d", what, n_select);
   if (n_first < 0 || n_recent < 0 || n_first > n_select || n_recent > n_select - n_first)
     return fail(KVK_ERR_INVALID, "%s: %d first and %d recent blocks of %d", what, n_first, n_recent, n_select);
   if (kvk_status st = check_lengths(t, what, "n_stored", n_stored, nullptr)) return st;
@@ -836,9 +866,9 @@ extern "C" kvk_status kvk_select_blocks(const kvk_table* t, int32_t l0, int32_t 
           const int32_t n = most > n_select ? most - n_first - n_recent : 0;  // blocks that compete
           // (8 rows of 4096 blocks: chunks of 256 take 19 us, of 512 23; 256 rows 35 and 33)
           a.chunk = (int64_t)n * rows >= 512 * 1024 ? 512 : 256;
-          const int64_t chunks = (n + a.chunk - 1) / a.chunk;
+          a.chunks = (n + a.chunk - 1) / a.chunk;
           // (a grid has less than 2^32 threads)
-          if (rows > (two ? 65535 : 0x7fffff) || chunks * rows > 0xffffff) return fail(KVK_ERR_UNSUPPORTED, "%s: grid too large", what);
+          if (rows > 0x7fffff || a.chunks * rows > 0xffffff) return fail(KVK_ERR_UNSUPPORTED, "%s: grid too large", what);
           if (!go) return KVK_OK;
           if (d.head_dim == 128) launch_select<128>(a, readers * a.G, n, two, stream);
           else launch_select<64>(a, readers * a.G, n, two, stream);

@@ -755,15 +755,12 @@ def rotary(width: int, frequencies: Sequence[float], layout: int = HALVES, magni
     return Rotary(h, layout, width)
 
 
-def _rotary_strides(x: torch.Tensor):
+def _rotary_strides(shape, st):
     """Element strides of sequence, head and token of a packed [tokens, heads, d] or padded
     [B, heads, n, d] tensor.  (The stride of a dimension of one element is never taken.)"""
-    shape, st = x.shape, x.stride()
     if len(shape) == 3:
-        n, h, d = shape
-        return 0, st[1] if h > 1 else 0, st[0] if n > 1 else 0
-    b, h, n, d = shape
-    return st[0] if b > 1 else 0, st[1] if h > 1 else 0, st[2] if n > 1 else 0
+        return 0, st[1] if shape[1] > 1 else 0, st[0] if shape[0] > 1 else 0
+    return st[0] if shape[0] > 1 else 0, st[1] if shape[1] > 1 else 0, st[2] if shape[2] > 1 else 0
 
 
 def rotate(rot: Rotary, positions: torch.Tensor, tensors: Sequence[torch.Tensor],
@@ -779,24 +776,30 @@ def rotate(rot: Rotary, positions: torch.Tensor, tensors: Sequence[torch.Tensor]
     if len(outs) != count or len(firsts) != count or not 1 <= count <= 4:
         raise ValueError("1 to 4 tensors, with an output and a first channel each")
     x0 = tensors[0]
-    rank = x0.dim()
+    dtype, rank = x0.dtype, x0.dim()
     if rank not in (3, 4):
         raise ValueError("tensors must be [tokens, heads, d] or [B, heads, n, d]")
     seqs, n = (1, x0.shape[0]) if rank == 3 else (x0.shape[0], x0.shape[2])
-    rows, dtype = b"", x0.dtype
+    rows = b""
     for x, y, f in zip(tensors, outs, firsts):
-        shape = x.shape
-        if (x.dtype != dtype or y.dtype != dtype or len(shape) != rank or shape != y.shape or x.stride(-1) != 1
-                or y.stride(-1) != 1 or (shape[0] if rank == 3 else shape[2]) != n or (rank == 4 and shape[0] != seqs)):
-            raise ValueError("tensors and outputs must agree in dtype, tokens and sequences, with contiguous rows")
-        a = _rotary_strides(x)
-        rows += _ROTARY_ROWS.pack(x.data_ptr(), y.data_ptr(), shape[1], shape[-1], f, *a, *(a if y is x else _rotary_strides(y)))
-    if positions.dtype != torch.int32 or not positions.is_contiguous() or positions.dim() > 2 or positions.shape[-1:] != (n,):
+        shape, st = x.shape, x.stride()
+        if y is x:
+            so = st
+        else:
+            so = y.stride()
+            if y.dtype != dtype or y.shape != shape or so[-1] != 1:
+                raise ValueError("outputs must be as their tensors, with contiguous rows")
+        if x.dtype != dtype or len(shape) != rank or st[-1] != 1 or shape[2 if rank == 4 else 0] != n or \
+                (rank == 4 and shape[0] != seqs):
+            raise ValueError("tensors must agree in dtype, tokens and sequences, with contiguous rows")
+        rows += _ROTARY_ROWS.pack(x.data_ptr(), y.data_ptr(), shape[1], shape[-1], f, *_rotary_strides(shape, st),
+                                  *_rotary_strides(shape, so))
+    places = positions.shape
+    if positions.dtype != torch.int32 or not positions.is_contiguous() or not 1 <= len(places) <= 2 or places[-1] != n:
         raise ValueError(f"positions must be contiguous int32 [{n}] or [rows, {n}]")
     _here(positions, *tensors, *outs)
-    pos_seqs = positions.shape[0] if positions.dim() == 2 else 1
-    _check(load().kvk_rotate(rot.handle, seqs, n, positions.data_ptr(), pos_seqs, rows, count, _dtype_code(x0), int(inverse),
-                             _stream(stream)))
+    _check(load().kvk_rotate(rot.handle, seqs, n, positions.data_ptr(), places[0] if len(places) == 2 else 1, rows, count,
+                             _dtype_code(x0), int(inverse), _stream(stream)))
 
 
 def index_bytes(t: Table) -> int:
@@ -901,8 +904,8 @@ def copy_sequences(src_table: Table, src_arena: torch.Tensor, dst_table: Table, 
     _here(src_arena, dst_arena, blocks)
     if _nbytes(src_arena) < src_table.arena_bytes or _nbytes(dst_arena) < dst_table.arena_bytes:
         raise ValueError("arena smaller than arena_bytes")
-    a, count = array("i", src), len(src)
-    b, stored = _lengths(dst, count, "dst"), _lengths(n_stored, count, "n_stored")
+    count = len(src)
+    a, b, stored = _lengths(src, count, "src"), _lengths(dst, count, "dst"), _lengths(n_stored, count, "n_stored")
     if blocks is not None:
         d = src_table.dims
         lead = (d.n_layers, d.batch) + (() if d.kind == MLA else (d.n_kv_heads,))

@@ -248,9 +248,9 @@ def test_select_refused():
     for name, off in (("q", 8), ("index", 128), ("blocks", 2)):
         _refused(_select(t, **{name: None}), kvk.ERR_INVALID, "NULL")
         _refused(_select(t, **{name: P0 + off}), kvk.ERR_INVALID, "misaligned")
-    for n in (0, -1):
+    for n in (0, -1, 2**30 + 1, 2**31 - 1):
         _refused(_select(t, n=n), kvk.ERR_INVALID, "n_select")
-    for first, recent in ((-1, 0), (0, -1), (3, 0), (0, 3), (1, 2), (2**31 - 1, 2**31 - 1)):
+    for first, recent in ((-1, 0), (0, -1), (3, 0), (0, 3), (1, 2), (2**31 - 1, 2**31 - 1)):  # of 2
         _refused(_select(t, first=first, recent=recent), kvk.ERR_INVALID, "first and")
     _refused(_select(t, ws=P0 + 128), kvk.ERR_INVALID, "misaligned")
     assert kvk.select_workspace_bytes(t, 0, 2) == 0
@@ -273,7 +273,7 @@ def test_attend_refused():
     for name, off in (("q", 8), ("blocks", 2), ("arena", 8), ("out", 8), ("ws", 128)):
         _refused(_attend(t, **{name: None}), kvk.ERR_INVALID, "NULL")
         _refused(_attend(t, **{name: P0 + off}), kvk.ERR_INVALID, "misaligned")
-    for n in (0, -5):
+    for n in (0, -5, 2**30 + 1):
         _refused(_attend(t, n=n), kvk.ERR_INVALID, "n_select")
     for scale in (float("nan"), float("inf")):
         _refused(_attend(t, scale=scale), kvk.ERR_INVALID, "finite")

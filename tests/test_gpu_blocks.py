@@ -459,6 +459,18 @@ def test_block_attention_many_entries():
     _check_attend(c, q, blocks, 0.1, _attend(c, q, blocks, 0.1))
 
 
+@pytest.mark.parametrize("bits,scheme", [(16, "kivi"), (8, "kivi"), (4, "sym"), (8, "g64"), (2, "kivi")])
+@pytest.mark.parametrize("d,hq,hkv,B", [(128, 5, 1, 256), (128, 34, 2, 70), (64, 6, 2, 150)])
+def test_block_attention_eight_waves(bits, scheme, d, hq, hkv, B):
+    """Launches of a workgroup per CU and more, whose rows eight waves share."""
+    c = Cache(hq, hkv, d, [(37 * b) % 1500 for b in range(B)], [(0, bits)], scheme)
+    g = _gen(31)
+    q = _randn(g, 1, B, hq, d).bfloat16()
+    for n in (17, 40):
+        blocks = _lists(g, c, n)
+        _check_attend(c, q, blocks, 0.1, _attend(c, q, blocks, 0.1))
+
+
 @pytest.mark.parametrize("bits,scheme", [(16, "kivi"), (8, "kivi"), (4, "sym")])
 def test_every_block_is_the_chunk_attention(bits, scheme):
     c = Cache(10, 2, 128, [1003, 320, 5], [(0, bits), (1, 2)], scheme)
@@ -491,11 +503,12 @@ def test_block_attention_small_and_large_values():
     c = Cache(4, 1, 64, [n], [(0, 8)], "sym", values=(k, v))
     blocks = torch.arange(12, dtype=torch.int32, device=DEV).view(1, 1, 1, 12)
     _check_attend(c, q, blocks, 0.125, _attend(c, q, blocks, 0.125))
-    # keys 2^40 apart from queries 2^-40
-    k2, q2 = (k.float() * 2.0**40).bfloat16(), (q.float() * 2.0**-40).bfloat16()
-    for scheme, bits in (("sym", 8), ("kivi", 16)):
-        c = Cache(4, 1, 64, [n], [(0, bits)], scheme, values=(k2, k))
-        _check_attend(c, q2, blocks, 0.125, _attend(c, q2, blocks, 0.125))
+    # large keys with small queries, and small keys with large queries
+    for up in (40, 100, -40, -100):
+        k2, q2 = (k.float() * 2.0**up).bfloat16(), (q.float() * 2.0**-up).bfloat16()
+        for scheme, bits in (("sym", 8), ("sym", 2), ("kivi", 16)):
+            c = Cache(4, 1, 64, [n], [(0, bits)], scheme, values=(k2, k))
+            _check_attend(c, q2, blocks, 0.125, _attend(c, q2, blocks, 0.125))
 
 
 def test_block_attention_rising_scores():
