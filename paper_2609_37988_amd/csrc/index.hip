@@ -11,9 +11,10 @@
 //                  channels is exact and turns tokens x channels into one channel per lane), so that minima and
 //                  maxima run over registers; codes are enough for KIVI32, whose scale and zero belong to the
 //                  channel.  Middles, scales and codes are in 64 bits: four values per lane.
-//                  Bound: about 400 vector instructions a block beside its keys' bytes (27 700 blocks of four
-//                  bit-widths, 117 MB of keys: 38 us, 3.1 TB/s; a launch per bit-width 66).  One block per
-//                  sequence (256 blocks): 4.7 us, the latency of a block.
+//                  Bound: the keys' bytes, read in pieces of 0.5 to 8 KB with the values between them, beside 390
+//                  vector instructions a block (27 700 blocks of four bit-widths, 117 MB of keys: 34 us, 3.7 TB/s; a
+//                  launch per bit-width 66; runs of two to eight blocks a wave 35 to 37).  One block per sequence
+//                  (256 blocks): 4 us, the latency of a block.
 //   select_kernel  one workgroup per (layer, sequence, KV head): scores into LDS, then the choice.  Bound: latency
 //                  (32 rows of up to 218 blocks 9 us); 12 288 rows of 256 blocks 110 us.
 //   score_kernel, choose_kernel  the same in two launches, the scores through the workspace: for launches of few rows
