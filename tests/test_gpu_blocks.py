@@ -586,9 +586,55 @@ def test_block_attention_past_4_gib():
     q = _randn(g, 2, B, 4, 128).bfloat16()
     blocks = torch.full((2, B, 4, 1), n // 32, dtype=torch.int32, device=DEV)
     out = _attend(c, q, blocks, 0.1)
+    index = _index_of(c, [n] * B)  # the last block's summaries, of every stream
+    for l in range(2):
+        codes, scales = kvk.index_views(c.table, index, l)
+        want, ws = _summary(k[l, :, :, :32].float())
+        assert torch.equal(codes[:, :, n // 32], want) and torch.equal(scales[:, :, n // 32], ws)
     p = torch.softmax((q.to(F64).unsqueeze(3) * k.to(F64)).sum(-1) * 0.1, -1)
     want = (p[..., None] * v.to(F64)).sum(3)
     assert ((out.to(F64) - want).abs() <= 2.0**-6 * (p[..., None] * v.to(F64).abs()).sum(3) + 1e-3).all()
+
+
+def test_select_past_4_gib():
+    """The last sequence's part of the last anchor of an index of 4.4 GB."""
+    n = 524288
+    c = Shape(8, 8, 128, [0] * 63 + [n], [(0, 4), (0, 4)], cap=n)
+    assert kvk.index_bytes(c.table) > 2**32 + 2**26
+    index, g = torch.zeros(kvk.index_bytes(c.table), dtype=torch.uint8, device=DEV), _gen(32)
+    codes, scales = kvk.index_views(c.table, index, 1)
+    codes[63] = torch.randint(-127, 128, codes[63].shape, generator=g, device=DEV)
+    scales[63] = torch.rand(scales[63].shape, generator=g, device=DEV)
+    q = _randn(g, 2, 64, 8, 128).bfloat16()
+    blocks = _select(c, q, index, 100, 1, 2)
+    for h in range(8):
+        assert blocks[1, 63, h].tolist() == _chosen(q[1, 63, h:h + 1], codes[63, h], scales[63, h], n // 32, 100, 1, 2)
+    assert (blocks[:, :63] == -1).all()
+
+
+def test_captured_index_and_long_choice():
+    """The index's launch and the choice in two launches, captured and replayed on other contents."""
+    c = Cache(4, 2, 64, [300, 64], [(0, 8), (0, 4)])
+    long = Shape(8, 2, 64, [64000, 40000], [(0, 4), (1, 4)])
+    index, g = torch.zeros(kvk.index_bytes(c.table), dtype=torch.uint8, device=DEV), _gen(33)
+    far, q = _fake_index(long, 34), _randn(g, 2, 2, 8, 64).bfloat16()
+    blocks = torch.zeros(2, 2, 2, 50, dtype=torch.int32, device=DEV)
+    ws = _workspace(kvk.select_workspace_bytes(long.table, 0, 2))
+    assert ws is not None
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        kvk.index_blocks(c.table, 0, 2, c.stored, c.arena, index)
+        kvk.select_blocks(long.table, 0, 2, q, long.stored, far, blocks, 1, 1, ws)
+    for i in range(3):
+        k, v = (_randn(g, 2, 2, 2, 300, 64).bfloat16() for _ in range(2))
+        kvk.append_chunk(c.table, 0, 2, k, v, 0, c.stored, c.arena)
+        q.copy_(_randn(g, *q.shape))
+        c.k, c.v = k, v
+        index.fill_(0x55)
+        graph.replay()
+        torch.cuda.synchronize()
+        _check_index(c, index)
+        _check_select(long, q, far, blocks, 1, 1)
 
 
 def test_streams_graphs_and_shared_workspaces():
