@@ -843,7 +843,9 @@ kvk_status kvk_select_blocks(const kvk_table* table, int32_t layer_begin, int32_
  *   n_stored : host [B], tokens stored per stream (the new token among them); the window is its last
  *              n_stored[b] % 32 tokens.
  *   blocks   : device int32 [layer_end-layer_begin][B][Hkv][n_select], any order; entries outside
- *              0 .. n_stored[b] / 32 - 1 are passed over, a block listed twice counts twice.
+ *              0 .. n_stored[b] / 32 - 1 are passed over, a block listed twice counts twice.  Where
+ *              n_stored[b] % 32 == 0 the newest tokens, the query's own among them, are in the last block (a
+ *              choice with n_recent >= 1 names it).
  *   n_select : 1 .. 2^30.
  *   out      : device bf16, as q; zeros where no token is seen.
  *   workspace: device, >= kvk_block_workspace_bytes of the range and n_select, 256-byte aligned; its contents on
@@ -876,8 +878,8 @@ kvk_status kvk_block_attention(const kvk_table* table, int32_t layer_begin, int3
  *   blocks    : NULL, or device int32 [n_layers][src batch][Hkv][n_blocks] (MLA: [n_layers][src batch][n_blocks]; anchors'
  *               rows are read), as kvk_select_blocks writes them for all layers: entry j is the block that
  *               becomes block j, for j < min(n_blocks, n_stored[i] / 32).  The copy then stores
- *               32 min(n_blocks, n_stored[i] / 32) + n_stored[i] % 32 tokens.  Entries are trusted to name
- *               blocks of the sequence; others are clamped.
+ *               32 min(n_blocks, n_stored[i] / 32) + n_stored[i] % 32 tokens (keys as they were rotated).
+ *               Entries are trusted to name blocks of the sequence; others are clamped.
  * An index is not copied: kvk_index_blocks writes the new slots' part.  The host arrays are read before the
  * call returns.
  * Errors: KVK_ERR_INVALID (tables, slots, lengths, plans, overlap, NULL, misalignment: arenas 16 B, blocks 4 B;

@@ -413,10 +413,12 @@ __global__ __launch_bounds__(64 * W, 2) void block_kernel(BlockArgs a) {
     mask &= mask - 1;
     return __builtin_amdgcn_readlane(entry, i);
   };
-  // Two blocks in flight (three and four were as fast at best: 4-bit 16.2 and 17.4 us against 14.5).  Past the list's end the loads go past the full blocks' range, where they read
+  // Two blocks in flight (256 rows of 32 4-bit blocks 14.5 us, three in flight 16.2, four 17.4).  Past the list's
+  // end the loads go past the full blocks' range, where they read
   // nothing: no branch, so that the compiler can count the loads outstanding.
   constexpr int RING = 2;
-  const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(stream), (short)0, nbf * a.block_bytes, 0x00020000);
+  const auto rsrc =
+      __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(stream), (short)0, nbf * a.block_bytes, 0x00020000);
   R raw[RING];
   int cur[RING];
 #pragma unroll
@@ -562,20 +564,23 @@ namespace {
 
 constexpr int64_t kCus = 256;
 
-// Waves of a workgroup and parts of each list.  From a row (sixteen heads of a layer, sequence and KV head) per CU
-// on, lists are whole: a second launch and the parts' records cost more than they save (512 rows of 32
-// 8-bit blocks: whole 34 us, in two parts 38); eight waves share one where four would leave a CU half empty (256
-// rows of 32 4-bit blocks: 14.5 us, four waves 18).  Fewer rows are split to two workgroups per CU, down to
-// four blocks a wave (96 rows of 256 2-bit blocks: five parts 31 us, ten 31, two 52; 64 rows of 64 bf16 blocks:
-// four blocks a wave 20, two 22).
-struct Shape {
-  int32_t waves, splits;
-};
-Shape shape_of(const kvk_table* t, int32_t l0, int32_t l1, int32_t n_select) {
+// Parts of each list, by the rows of a call (sixteen heads of a layer, sequence and KV head).  From a row per CU on,
+// lists are whole: a second launch and the parts' records cost more than they save (512 rows of 32 8-bit blocks:
+// whole 34 us, in two parts 38).  Fewer rows are split to two workgroups per CU, down to four blocks a wave (96 rows of
+// 256 2-bit blocks: five parts 31 us, ten 31, two 52; 64 rows of 64 bf16 blocks: four blocks a wave 20, two 22).
+int64_t rows_of(const kvk_table* t, int32_t l0, int32_t l1) {
   const int64_t G = t->d.n_q_heads / t->d.n_kv_heads;
-  const int64_t rows = (int64_t)(l1 - l0) * t->d.batch * t->d.n_kv_heads * ((G + 15) / 16);
-  if (rows >= kCus) return Shape{rows < 2 * kCus && n_select > 16 ? 8 : 4, 1};
-  return Shape{4, (int32_t)std::max<int64_t>(1, std::min<int64_t>(2 * kCus / rows, n_select / 16))};
+  return (int64_t)(l1 - l0) * t->d.batch * t->d.n_kv_heads * ((G + 15) / 16);
+}
+int32_t splits_of(int64_t rows, int32_t n_select) {
+  return rows >= kCus ? 1 : (int32_t)std::max<int64_t>(1, std::min<int64_t>(2 * kCus / rows, n_select / 16));
+}
+// Waves of a workgroup.  Eight share a whole list where four would leave a CU half empty (256 rows of 32 4-bit blocks:
+// 14.5 us, four 18), and shorten the chain where rows are few (32 rows of 16 4-bit blocks 10.1 and 11.0
+// us; of bf16 blocks 12.2 and 11.5).
+int waves_of(int64_t rows, int32_t n_select, int32_t splits, int bits) {
+  if (splits > 1 || rows >= 2 * kCus) return 4;
+  return rows >= kCus ? (n_select > 16 ? 8 : 4) : (n_select > 8 && bits < 16 ? 8 : 4);
 }
 
 kvk_status check_call(const kvk_table* t, const char* what, int32_t l0, int32_t l1, int32_t n_select) {
@@ -612,7 +617,7 @@ void launch(int waves, int qs, int bits, dim3 g, const BlockArgs& a, hipStream_t
 extern "C" kvk_status kvk_block_workspace_bytes(const kvk_table* t, int32_t l0, int32_t l1, int32_t n_select, size_t* out) {
   if (kvk_status st = check_call(t, "kvk_block_workspace_bytes", l0, l1, n_select)) return st;
   if (!out) return fail(KVK_ERR_INVALID, "kvk_block_workspace_bytes: NULL output");
-  const int64_t ns = shape_of(t, l0, l1, n_select).splits;
+  const int64_t ns = splits_of(rows_of(t, l0, l1), n_select);
   const int64_t rows = (int64_t)(l1 - l0) * t->d.batch * t->d.n_q_heads;
   *out = (size_t)(ns > 1 ? round256(rows * ns * (t->d.head_dim + 4) * 4) : 256);
   return KVK_OK;
@@ -636,9 +641,10 @@ extern "C" kvk_status kvk_block_attention(const kvk_table* t, int32_t l0, int32_
   size_t need = 0;
   if (kvk_status st = kvk_block_workspace_bytes(t, l0, l1, n_select, &need)) return st;
   BlockArgs a;
-  const Shape shape = shape_of(t, l0, l1, n_select);
-  a.n_split = shape.splits;
-  if (a.n_split > 1 && ws_bytes < need) return fail(KVK_ERR_BUFFER, "%s: workspace %zu bytes < %zu needed", what, ws_bytes, need);
+  const int64_t tiles = rows_of(t, l0, l1);
+  a.n_split = splits_of(tiles, n_select);
+  if (a.n_split > 1 && ws_bytes < need)
+    return fail(KVK_ERR_BUFFER, "%s: workspace %zu bytes < %zu needed", what, ws_bytes, need);
   if (kvk_status st = check_gpu_buffers({q, blocks, arena, out, workspace}, what)) return st;
   a.arena = static_cast<const uint8_t*>(arena);
   a.q = static_cast<const uint16_t*>(q);
@@ -667,12 +673,14 @@ extern "C" kvk_status kvk_block_attention(const kvk_table* t, int32_t l0, int32_
         },
         [&](int bits, Group& g) -> kvk_status {
           const int64_t wgs = (int64_t)g.n_layers * g.n_seqs * d.n_kv_heads * a.tiles * a.n_split;
-          if (wgs * 64 * shape.waves > 0xffffffffLL) return fail(KVK_ERR_UNSUPPORTED, "%s: grid too large", what);  // (less than 2^32 threads)
+          const int waves = waves_of(tiles, n_select, a.n_split, bits);
+          if (wgs * 64 * waves > 0xffffffffLL)  // (a grid has less than 2^32 threads)
+            return fail(KVK_ERR_UNSUPPORTED, "%s: grid too large", what);
           if (!go) return KVK_OK;
           a.block_bytes = (int32_t)gqa_block_bytes(d.head_dim, bits, d.qscheme);
           const dim3 grid((unsigned)wgs);
-          if (d.head_dim == 128) launch<128>(shape.waves, d.qscheme, bits, grid, a, stream);
-          else launch<64>(shape.waves, d.qscheme, bits, grid, a, stream);
+          if (d.head_dim == 128) launch<128>(waves, d.qscheme, bits, grid, a, stream);
+          else launch<64>(waves, d.qscheme, bits, grid, a, stream);
           const hipError_t e = hipGetLastError();
           if (e != hipSuccess) return fail(KVK_ERR_DEVICE, "%s launch: %s", what, hipGetErrorString(e));
           return KVK_OK;

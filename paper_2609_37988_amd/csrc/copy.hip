@@ -138,12 +138,15 @@ extern "C" kvk_status kvk_copy_sequences(const kvk_table* st, const void* src_ar
     return fail(KVK_ERR_INVALID, "%s: the arenas overlap (one arena: the same pointer and table twice)", what);
   const auto plan_of = [](const kvk_table* t, int b) { return t->seq.empty() ? t : t->seq[b]; };
   for (int i = 0; i < n_copies; ++i) {
-    if (src[i] < 0 || src[i] >= st->d.batch) return fail(KVK_ERR_INVALID, "%s: src[%d] = %d outside 0..%d", what, i, src[i], st->d.batch - 1);
-    if (dst[i] < 0 || dst[i] >= dt->d.batch) return fail(KVK_ERR_INVALID, "%s: dst[%d] = %d outside 0..%d", what, i, dst[i], dt->d.batch - 1);
+    if (src[i] < 0 || src[i] >= st->d.batch)
+      return fail(KVK_ERR_INVALID, "%s: src[%d] = %d outside 0..%d", what, i, src[i], st->d.batch - 1);
+    if (dst[i] < 0 || dst[i] >= dt->d.batch)
+      return fail(KVK_ERR_INVALID, "%s: dst[%d] = %d outside 0..%d", what, i, dst[i], dt->d.batch - 1);
     if (n_stored[i] < 0 || n_stored[i] > st->cap)
       return fail(KVK_ERR_INVALID, "%s: n_stored[%d] = %d outside 0..%d", what, i, n_stored[i], st->cap);
     const int32_t kept = blocks ? std::min(n_blocks, n_stored[i] / 32) * 32 + n_stored[i] % 32 : n_stored[i];
-    if (kept > dt->cap) return fail(KVK_ERR_INVALID, "%s: %d tokens of copy %d beyond the capacity %d", what, kept, i, dt->cap);
+    if (kept > dt->cap)
+      return fail(KVK_ERR_INVALID, "%s: %d tokens of copy %d beyond the capacity %d", what, kept, i, dt->cap);
   }
   {  // every slot written once, and none read that is written
     uint64_t use[1024] = {};

@@ -486,7 +486,8 @@ struct Keys {
 // increasing order.  Digits of eight bits from the highest one in which keys differ, by histograms of the keys
 // that share the digits found so far.
 template <int WAVES, int N>
-__device__ __forceinline__ void choose(Choice<WAVES>& sh, const Keys<WAVES, N>& keys, int want, int add, int32_t* out, int tid) {
+__device__ __forceinline__ void choose(Choice<WAVES>& sh, const Keys<WAVES, N>& keys, int want, int add, int32_t* out,
+                                       int tid) {
   static_assert(64 * WAVES >= kBins, "a thread for every bin");
   const int lane = tid & 63, wave = tid >> 6;
   uint32_t top = 0, low = 0;  // low: of the complements
@@ -585,9 +586,11 @@ __device__ __forceinline__ void choose(Choice<WAVES>& sh, const Keys<WAVES, N>& 
   });
 }
 
-// Of a row's list what does not compete: the first and the last blocks, or, where there are few enough, all blocks and -1.
+// Of a row's list what does not compete: the first and the last blocks, or, where there are few enough, all blocks
+// and -1.
 // Returns how many of the others are to be chosen.
-__device__ __forceinline__ int write_fixed(int nb, int n_select, int n_first, int n_recent, int32_t* out, int tid, int threads) {
+__device__ __forceinline__ int write_fixed(int nb, int n_select, int n_first, int n_recent, int32_t* out, int tid,
+                                           int threads) {
   if (nb <= n_select) {
     for (int i = tid; i < n_select; i += threads) out[i] = i < nb ? i : -1;
     return 0;
@@ -635,7 +638,8 @@ __global__ __launch_bounds__(kThreads) void score_kernel(SelectArgs a) {
   const int nb = S.stored >> 5;
   const int b0 = a.n_first + part * a.chunk, b1 = min(nb - a.n_recent, b0 + a.chunk);
   if (nb <= a.n_select || b0 >= b1) return;
-  qs.fill(a.q + (((int64_t)L.layer * a.B + S.seq) * a.Hq + kvh * a.G) * D, (int64_t)a.B * a.Hq * D, a.G, a.G * L.count, lane, wave);
+  qs.fill(a.q + (((int64_t)L.layer * a.B + S.seq) * a.Hq + kvh * a.G) * D, (int64_t)a.B * a.Hq * D, a.G, a.G * L.count,
+          lane, wave);
   __syncthreads();
   const uint8_t* index = a.index + L.index + S.index;
   const int64_t row = ((int64_t)S.mult * a.g.Hkv + kvh) * a.nb_cap;
