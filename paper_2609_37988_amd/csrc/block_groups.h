@@ -9,6 +9,7 @@
 namespace kvk {
 
 constexpr int kGroupSeqs = 64;  // sequences of a launch
+constexpr int kReaderRows = 64; // query rows of layers that are read for together
 
 // Layers of one launch: each an entry of its own, or (of Layers::readers) the layers that read one anchor together.
 struct GroupLayer {
@@ -59,7 +60,7 @@ inline int64_t index_total(const kvk_table* t) { return index_offset(t, t->d.n_l
 enum class Layers {
   anchors,  // of the range
   each,     // of the range, with its anchor's part
-  readers,  // of the range that read one anchor: one entry (per-sequence plans: each)
+  readers,  // of the range that read one anchor: one entry for at most kReaderRows rows (per-sequence plans: each)
 };
 
 // Calls f(bits, group) for the layers of [l0, l1) of a GQA table, all bit-widths of a one-plan table in one group
@@ -68,6 +69,7 @@ enum class Layers {
 template <class Of, class F>
 kvk_status for_groups(const kvk_table* t, int l0, int l1, Layers which, bool by_bits, Group& g, Of of, F f) {
   g.Hkv = t->d.n_kv_heads;
+  const int together = std::max(1, kReaderRows / (t->d.n_q_heads / t->d.n_kv_heads));
   constexpr int kBits[4] = {16, 8, 4, 2};
   if (t->seq.empty()) {
     for (int k = 0; k < (by_bits ? 4 : 1); ++k) {
@@ -76,7 +78,7 @@ kvk_status for_groups(const kvk_table* t, int l0, int l1, Layers which, bool by_
       int rows = 0;
       for (int l = l0; l < l1;) {
         const int anc = t->info.anchor_of[l];
-        const int n = which == Layers::readers ? std::min<int>(t->next_anchor[anc], l1) - l : 1;
+        const int n = which == Layers::readers ? std::min(together, std::min<int>(t->next_anchor[anc], l1) - l) : 1;
         if ((!by_bits || t->bits[anc] == bits) && (which != Layers::anchors || anc == l)) {
           g.layers[g.n_layers++] = GroupLayer{t->info.layer_offset[anc], index_offset(t, anc), (int32_t)t->info.stream_bytes[anc],
                                               (uint8_t)(l - l0), (uint8_t)n, (uint8_t)rows, (uint8_t)t->bits[anc]};

@@ -315,7 +315,7 @@ struct Queries {
   uint8_t rows[16 * T * kStride];
   float scale[16 * T];
 
-  // n rows, G of each layer; q: the first layer's, the next `step` elements further.
+  // n rows (at most sixteen for each T), G of each layer; q: the first layer's, the next `step` elements further.
   __device__ __forceinline__ void fill(const uint16_t* q, int64_t step, int G, int n, int lane, int wave) {
     for (int h = wave; h < 16 * T; h += kWaves) {
       const int u = h / G;
@@ -343,12 +343,12 @@ struct Queries {
   }
 };
 
-// Scores of blocks [b0, b1) by each of `layers` layers' G rows, as keys into out[u step + b - at0]; the waves of a workgroup
-// share the blocks, sixteen at a time: block b0 + lane % 16 is the lane's column of the products, row
-// 4 (lane / 16) + r of a tile its row r.
+// Scores of blocks [b0, b1) by each of `layers` layers' G rows, as keys into out[u step + b - at0] (`more`: where they
+// are larger than what this lane has written there); the waves of a workgroup share the blocks, sixteen at a time:
+// block b0 + lane % 16 is the lane's column of the products, row 4 (lane / 16) + r of a tile its row r.
 template <int D, int T>
 __device__ __forceinline__ void score(const Queries<D, T>& qs, const uint8_t* codes, const float2* scales, int G, int layers,
-                                      int b0, int b1, uint32_t* out, int64_t step, int at0, int lane, int wave) {
+                                      int b0, int b1, uint32_t* out, int64_t step, int at0, bool more, int lane, int wave) {
   constexpr int NK = D / 64;  // products of a part
   const int col = lane & 15, kg = lane >> 4;
   const auto load_rows = [&](i4v (&x)[2 * NK], int t) {
@@ -409,8 +409,30 @@ __device__ __forceinline__ void score(const Queries<D, T>& qs, const uint8_t* co
           for (int r = 0; r < 4; ++r)
             if ((uint32_t)(16 * t + 4 * kg + r - u * G) < (uint32_t)G) best = fmaxf(best, x[t][r]);
         best = rows_max(best);
-        if (kg == 0 && b < b1) out[u * step + (b - at0)] = key_of(best);
+        if (kg == 0 && b < b1) {
+          uint32_t* at = out + u * step + (b - at0);
+          const uint32_t key = key_of(best);
+          *at = more ? max(*at, key) : key;
+        }
       }
+    }
+  }
+}
+
+// The queries' rows, then the scores, sixteen T rows at a time (one layer's, where they are more than that).
+template <int D, int T>
+__device__ __forceinline__ void fill_and_score(Queries<D, T>& qs, const uint16_t* q, int64_t q_step, const uint8_t* codes,
+                                               const float2* scales, int G, int layers, int b0, int b1, uint32_t* out,
+                                               int64_t step, int at0, int lane, int wave) {
+  qs.fill(q, q_step, G, min(G * layers, 16 * T), lane, wave);
+  __syncthreads();
+  score<D, T>(qs, codes, scales, G, layers, b0, b1, out, step, at0, false, lane, wave);
+  if constexpr (16 * T == kvk::kReaderRows) {
+    for (int h = 16 * T; h < G; h += 16 * T) {
+      __syncthreads();
+      qs.fill(q + (int64_t)h * D, 0, G, min(G - h, 16 * T), lane, wave);
+      __syncthreads();
+      score<D, T>(qs, codes, scales, G - h, 1, b0, b1, out, 0, at0, true, lane, wave);
     }
   }
 }
@@ -615,13 +637,12 @@ __global__ __launch_bounds__(kThreads) void select_kernel(SelectArgs a) {
   int32_t* out = a.blocks + (call_row * a.g.Hkv + kvh) * a.n_select;
   const int want = write_fixed(nb, a.n_select, a.n_first, a.n_recent, out, tid, kThreads);
   if (want == 0) return;
-  qs.fill(a.q + (call_row * a.Hq + kvh * a.G) * D, 0, a.G, a.G, lane, wave);
-  __syncthreads();
   const uint8_t* index = a.index + L.index + S.index;
   const int64_t row = ((int64_t)S.mult * a.g.Hkv + kvh) * a.nb_cap;
   const int end = nb - a.n_recent;
-  score<D, T>(qs, index + row * 2 * D, reinterpret_cast<const float2*>(index + a.scales) + row, a.G, 1, a.n_first, end,
-              lds_keys, 0, a.n_first, lane, wave);
+  fill_and_score<D, T>(qs, a.q + (call_row * a.Hq + kvh * a.G) * D, 0, index + row * 2 * D,
+                       reinterpret_cast<const float2*>(index + a.scales) + row, a.G, 1, a.n_first, end, lds_keys, 0,
+                       a.n_first, lane, wave);
   __syncthreads();
   choose(sh, Keys<kWaves, 0>(lds_keys, end - a.n_first, lane, wave), want, a.n_first, out + a.n_first, tid);
 }
@@ -638,14 +659,12 @@ __global__ __launch_bounds__(kThreads) void score_kernel(SelectArgs a) {
   const int nb = S.stored >> 5;
   const int b0 = a.n_first + part * a.chunk, b1 = min(nb - a.n_recent, b0 + a.chunk);
   if (nb <= a.n_select || b0 >= b1) return;
-  qs.fill(a.q + (((int64_t)L.layer * a.B + S.seq) * a.Hq + kvh * a.G) * D, (int64_t)a.B * a.Hq * D, a.G, a.G * L.count,
-          lane, wave);
-  __syncthreads();
   const uint8_t* index = a.index + L.index + S.index;
   const int64_t row = ((int64_t)S.mult * a.g.Hkv + kvh) * a.nb_cap;
-  score<D, T>(qs, index + row * 2 * D, reinterpret_cast<const float2*>(index + a.scales) + row, a.G, L.count, b0, b1,
-              a.keys + (((int64_t)L.row0 * a.g.n_seqs + sq) * a.g.Hkv + kvh) * a.nb_cap,
-              (int64_t)a.g.n_seqs * a.g.Hkv * a.nb_cap, 0, lane, wave);
+  fill_and_score<D, T>(qs, a.q + (((int64_t)L.layer * a.B + S.seq) * a.Hq + kvh * a.G) * D, (int64_t)a.B * a.Hq * D,
+                       index + row * 2 * D, reinterpret_cast<const float2*>(index + a.scales) + row, a.G, L.count, b0, b1,
+                       a.keys + (((int64_t)L.row0 * a.g.n_seqs + sq) * a.g.Hkv + kvh) * a.nb_cap,
+                       (int64_t)a.g.n_seqs * a.g.Hkv * a.nb_cap, 0, lane, wave);
 }
 
 constexpr int kChooseWaves = 8;

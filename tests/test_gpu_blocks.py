@@ -288,6 +288,27 @@ def test_select_long(stored, n_select, first, recent):
     _check_select(c, q, index, _select(c, q, index, n_select, first, recent), first, recent)
 
 
+@pytest.mark.parametrize("hq,hkv", [(65, 1), (96, 1), (256, 2)])
+@pytest.mark.parametrize("stored", [[3200, 700], [64000]])
+def test_select_groups_of_many_heads(hq, hkv, stored):
+    """More than 64 heads of a KV head, any of which may hold the largest score."""
+    c = Shape(hq, hkv, 64, stored, [(0, 4), (1, 4)])
+    index, g = _fake_index(c, 61), _gen(62)
+    q = _randn(g, c.nl, c.B, hq, 64)
+    q = (q * (1 + 3 * torch.rand(q.shape[:-1] + (1,), generator=g, device=DEV))).bfloat16()
+    _check_select(c, q, index, _select(c, q, index, 20, 1, 2), 1, 2)
+
+
+@pytest.mark.parametrize("hq,hkv,readers", [(40, 1, 3), (14, 2, 9), (4, 1, 40), (7, 1, 10)])
+def test_select_anchors_of_many_readers(hq, hkv, readers):
+    """More than 64 rows read one anchor's index."""
+    c = Shape(hq, hkv, 64, [64000, 40000], [(0, 4)] + [(1, 4)] * (readers - 1) + [(0, 2), (1, 2)])
+    assert kvk.select_workspace_bytes(c.table, 0, c.nl) > 0
+    index, g = _fake_index(c, 63), _gen(64)
+    q = _randn(g, c.nl, c.B, hq, 64).bfloat16()
+    _check_select(c, q, index, _select(c, q, index, 9, 1, 2), 1, 2)
+
+
 def test_select_many_rows():
     """Launches of more rows than go through the workspace, at the longest that LDS holds, and of many sequences."""
     c = Shape(4, 4, 64, [32 * 8192] + [32 * 70] * 129, [(0, 4)])
