@@ -515,7 +515,7 @@ void kvk_rotary_destroy(kvk_rotary* rotary);
  * multiples of 8, first + width <= head_dim. */
 typedef struct {
   const void* in;
-  void* out;         /* in itself (the same strides), or rows that overlap none of the call's inputs */
+  void* out;         /* in itself (the same strides), or rows that overlap no others of the call */
   int32_t n_heads, head_dim, first;
   kvk_strides in_strides, out_strides;
 } kvk_rotary_rows;
@@ -531,9 +531,9 @@ typedef struct {
  *               call, and with m = 1 its inverse (a key moved by d positions: the forward
  *               call with d).
  * Each pair is read before it is written; an infinite or NaN value makes its pair so.
- * Errors: KVK_ERR_INVALID (sizes, strides, rows of out that overlap, NULL, misalignment: rows 16 B, positions
- *         4 B; host memory), KVK_ERR_UNSUPPORTED (more than 2^31 pieces of a row in one call),
- *         KVK_ERR_DEVICE. */
+ * Errors: KVK_ERR_INVALID (sizes, strides, rows of out that overlap, one tensor written twice, NULL,
+ *         misalignment: rows 16 B, positions 4 B; host memory), KVK_ERR_UNSUPPORTED (more than 2^31 pieces of
+ *         a row in one call), KVK_ERR_DEVICE. */
 kvk_status kvk_rotate(const kvk_rotary* rotary, int32_t n_seqs, int32_t n_tokens, const int32_t* positions,
                       int32_t pos_seqs, const kvk_rotary_rows* rows, int32_t n_rows, int32_t dtype, int32_t inverse,
                       hipStream_t stream);

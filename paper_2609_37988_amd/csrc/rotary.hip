@@ -320,6 +320,9 @@ extern "C" kvk_status kvk_rotate(const kvk_rotary* rotary, int32_t n_seqs, int32
       return fail(KVK_ERR_INVALID, "%s: misaligned buffer (16 B)", what);
     if (kvk_status st = check_rows(what, i, "in", x.in_strides, x.head_dim, n_seqs, x.n_heads, n_tokens, false)) return st;
     if (kvk_status st = check_rows(what, i, "out", x.out_strides, x.head_dim, n_seqs, x.n_heads, n_tokens, true)) return st;
+    for (int j = 0; j < n_rows; ++j)
+      if (j != i && (x.out == rows[j].out || x.out == rows[j].in))
+        return fail(KVK_ERR_INVALID, "%s: out of tensor %d is another tensor's rows", what, i);
     const bool in_place = x.in == x.out;
     const kvk_strides &p = x.in_strides, &q = x.out_strides;
     if (in_place && ((n_seqs > 1 && p.seq != q.seq) || (x.n_heads > 1 && p.head != q.head) || (n_tokens > 1 && p.token != q.token)))

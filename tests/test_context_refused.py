@@ -143,6 +143,9 @@ def test_rotate_refused():
         _refused(_rotate(rows=[_rows(out_strides=bad)]), kvk.ERR_INVALID, "overlap")
     _refused(_rotate(rows=[_rows(out=P0, out_strides=(4096, 64, 256))]), kvk.ERR_INVALID, "in place")
     _refused(_rotate(rows=[_rows(in_strides=(2**62, 64, 256))]), kvk.ERR_INVALID, "beyond")
+    far, a = P0 + (1 << 20), _rows()
+    for rows in ([a, a], [a, _rows(in_=P0 + 4096)], [a, _rows(in_=far, out=P0 + (1 << 21))], [_rows(out=P0)] * 2):
+        _refused(_rotate(rows=rows), kvk.ERR_INVALID, "another tensor's")
     # the stride of a dimension of one element is never taken; inputs may repeat
     _refused(_rotate(rows=[_rows(out_strides=(0, 64, 256))], seqs=1), kvk.ERR_INVALID, "not GPU-accessible")
     _refused(_rotate(rows=[_rows(in_strides=(0, 0, 0))]), kvk.ERR_INVALID, "not GPU-accessible")
