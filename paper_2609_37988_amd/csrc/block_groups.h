@@ -51,11 +51,9 @@ inline int64_t index_anchor_bytes(const kvk_table* t) {
   return index_codes_bytes(t) + round256((int64_t)t->d.batch * t->d.n_kv_heads * t->nb_cap * 8);
 }
 inline int64_t index_offset(const kvk_table* t, int anchor) {
-  int64_t n = 0;
-  for (int l = 0; l < anchor; ++l) n += !t->plan[l].inherit;
-  return n * index_anchor_bytes(t);
+  return t->anchors_before[anchor] * index_anchor_bytes(t);
 }
-inline int64_t index_total(const kvk_table* t) { return index_offset(t, t->d.n_layers); }
+inline int64_t index_total(const kvk_table* t) { return t->info.n_anchors * index_anchor_bytes(t); }
 
 enum class Layers {
   anchors,  // of the range

@@ -18,6 +18,7 @@ struct kvk_table {
   int32_t rank[KVK_MAX_LAYERS];         // MLA: kept latent width d of each anchor
   int64_t block_bytes[KVK_MAX_LAYERS];  // bytes of one 32-token block (anchors)
   int32_t next_anchor[KVK_MAX_LAYERS];  // first anchor after l (n_layers if none)
+  int32_t anchors_before[KVK_MAX_LAYERS];  // of the layers below l
   int32_t cap;                          // stored tokens capacity per stream
   int32_t nb_cap;                       // full-block capacity per stream (cap / 32)
   // Per-sequence plans: sequence b is the one-sequence table seq[b], whose arena sits

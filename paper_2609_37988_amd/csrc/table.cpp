@@ -454,6 +454,7 @@ extern "C" kvk_status kvk_layer_table(const kvk_dims* dims, const kvk_action* pl
   for (int l = 0; l < d.n_layers; ++l) {
     const kvk_action& a = plan[l];
     inf.layer_offset[l] = -1;
+    t->anchors_before[l] = inf.n_anchors;
     if (!a.inherit) {
       last = l;
       t->bits[l] = a.bits;
