@@ -16,7 +16,8 @@
 //                  launch per bit-width 66; runs of two to eight blocks a wave 35 to 37).  One block per sequence
 //                  (256 blocks): 4 us, the latency of a block.
 //   select_kernel  one workgroup per (layer, sequence, KV head): scores into LDS, then the choice.  Bound: latency
-//                  (32 rows of up to 218 blocks 9 us); 12 288 rows of 256 blocks 110 us.
+//                  (32 rows of up to 218 blocks 7.3 us); 12 288 rows of 256 blocks 100 us, an index read by three
+//                  layers each (850 MB of reads, 8.5 TB/s out of HBM and the caches).
 //   score_kernel, choose_kernel  the same in two launches, the scores through the workspace: for launches of few rows
 //                  or of more blocks than LDS holds.  The layers that read one anchor share a read of its index.
 //                  Bound: the index's bytes, then the choice's latency (128 indexes of up to 4096 blocks, 117 MB, two
@@ -300,6 +301,7 @@ static_assert(sizeof(SelectArgs) <= 4096, "kernel arguments");
 constexpr int kThreads = 256, kWaves = 4;
 constexpr int kBins = 256;
 
+
 typedef int i4v __attribute__((ext_vector_type(4)));
 
 // A score as an unsigned key of the same order (-0 equal to 0); never 0.
@@ -318,12 +320,19 @@ struct Queries {
   // n rows (at most sixteen for each T), G of each layer; q: the first layer's, the next `step` elements further.
   __device__ __forceinline__ void fill(const uint16_t* q, int64_t step, int G, int n, int lane, int wave) {
     for (int h = wave; h < 16 * T; h += kWaves) {
+      uint8_t* row = rows + h * kStride + lane * (D / 64);
+      if (h >= n) {
+#pragma unroll
+        for (int i = 0; i < D / 64; ++i) row[i] = row[D + i] = 0;
+        if (lane == 0) scale[h] = 0.0f;
+        continue;
+      }
       const int u = h / G;
       float x[D / 64];
       bool odd = false;
 #pragma unroll
       for (int i = 0; i < D / 64; ++i) {
-        const uint16_t b = h < n ? q[u * step + (h - u * G) * D + lane * (D / 64) + i] : 0;
+        const uint16_t b = q[u * step + (h - u * G) * D + lane * (D / 64) + i];
         odd |= (b & 0x7f80u) == 0x7f80u;
         x[i] = bf16_to_f32(b);
       }
@@ -336,8 +345,8 @@ struct Queries {
 #pragma unroll
       for (int i = 0; i < D / 64; ++i) {
         const int c = s > 0.0f ? (int)rintf(x[i] / s) : 0;
-        rows[h * kStride + lane * (D / 64) + i] = (uint8_t)c;
-        rows[h * kStride + D + lane * (D / 64) + i] = (uint8_t)(c < 0 ? -c : c);
+        row[i] = (uint8_t)c;
+        row[D + i] = (uint8_t)(c < 0 ? -c : c);
       }
     }
   }
@@ -463,6 +472,11 @@ __device__ __forceinline__ uint32_t wave_umax(uint32_t x) {
   x = dpp_max<0x142, 0xA>(x);
   x = dpp_max<0x143, 0xC>(x);
   return (uint32_t)__builtin_amdgcn_readlane((int)x, 63);
+}
+
+// Bits of m below the lane's own, added to n.
+__device__ __forceinline__ uint32_t bits_below(uint64_t m, uint32_t n) {
+  return __builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, n));
 }
 
 template <int WAVES>
@@ -592,20 +606,72 @@ __device__ __forceinline__ void choose(Choice<WAVES>& sh, const Keys<WAVES, N>& 
     equal += sh.wave[1][w];
   }
   uint32_t left = ties - min(equal, ties), at = above + min(equal, ties);
-  const auto below = [](uint64_t m, uint32_t x) {  // bits of m below the lane's own, added to x
-    return __builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, x));
-  };
   keys.each([&](int p, uint32_t k, bool has) {
     bool kept = has && k > cut;
     const uint64_t e = __ballot(has && k == cut);
     if (e && left) {
-      kept |= has && k == cut && below(e, 0) < left;
+      kept |= has && k == cut && bits_below(e, 0) < left;
       left -= min(left, (uint32_t)__popcll(e));
     }
     const uint64_t m = __ballot(kept);
-    if (kept) out[below(m, at)] = add + p;
+    if (kept) out[bits_below(m, at)] = add + p;
     at += __popcll(m);
   });
+}
+
+// Choices among up to this many keys take one wave and no barriers (12 288 rows of 256 blocks 101 us, by digits 104; 32
+// rows of up to 218 11.0 and 11.6; 512 rows of 1024 29.5 and 28.1).
+constexpr int kFew = 512;
+
+// Of the wave's keys (0: none), of which there are more than `want`: a value such that the `want` largest are those
+// above it and the first `ties` equal to it.  Bit by bit, by counts over the wave.
+template <int N>
+__device__ __forceinline__ void find_cut(const uint32_t (&x)[N], int want, uint32_t& cut, int& ties) {
+  uint32_t top = 0, low = 0;  // low: of the complements
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    top = max(top, x[j]);
+    low = max(low, x[j] ? ~x[j] : 0u);
+  }
+  top = wave_umax(top);
+  low = ~wave_umax(low);
+  // the largest value that `want` keys reach; keys agree above bit `bit`
+  int bit = 31 - __clz((int)((top ^ low) | 1)), above = 0;
+  cut = top >> bit >> 1 << bit << 1;
+  for (; bit >= 0; --bit) {
+    const uint32_t t = cut | 1u << bit;
+    int n = 0;
+#pragma unroll
+    for (int j = 0; j < N; ++j) n += __popcll(__ballot(x[j] >= t));
+    if (n >= want) cut = t;
+    else above = n;  // (larger than the value in the end)
+    if (n == want) break;
+  }
+  ties = want - above;
+  if (bit >= 0) {  // exactly the keys from there on
+    --cut;
+    ties = 0;
+  }
+}
+
+// The same by one wave, of up to 64 N keys.
+template <int N>
+__device__ __forceinline__ void choose_in_wave(const uint32_t* from, int count, int want, int add, int32_t* out, int lane) {
+  uint32_t x[N], cut;
+#pragma unroll
+  for (int j = 0; j < N; ++j) x[j] = 64 * j + lane < count ? from[64 * j + lane] : 0u;
+  int ties, at = 0;
+  find_cut(x, want, cut, ties);
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    const bool equal = x[j] == cut;
+    const uint64_t e = __ballot(equal);
+    const bool kept = x[j] > cut || (equal && (int)bits_below(e, 0) < ties);
+    ties = max(ties - (int)__popcll(e), 0);
+    const uint64_t m = __ballot(kept);
+    if (kept) out[bits_below(m, at)] = add + 64 * j + lane;
+    at += __popcll(m);
+  }
 }
 
 // Of a row's list what does not compete: the first and the last blocks, or, where there are few enough, all blocks
@@ -644,7 +710,14 @@ __global__ __launch_bounds__(kThreads) void select_kernel(SelectArgs a) {
                        reinterpret_cast<const float2*>(index + a.scales) + row, a.G, 1, a.n_first, end, lds_keys, 0,
                        a.n_first, lane, wave);
   __syncthreads();
-  choose(sh, Keys<kWaves, 0>(lds_keys, end - a.n_first, lane, wave), want, a.n_first, out + a.n_first, tid);
+  const int n = end - a.n_first;
+  out += a.n_first;
+  if (n > kFew) {
+    choose(sh, Keys<kWaves, 0>(lds_keys, n, lane, wave), want, a.n_first, out, tid);
+  } else if (wave == 0) {
+    if (n <= kFew / 2) choose_in_wave<kFew / 128>(lds_keys, n, want, a.n_first, out, lane);
+    else choose_in_wave<kFew / 64>(lds_keys, n, want, a.n_first, out, lane);
+  }
 }
 
 template <int D, int T>

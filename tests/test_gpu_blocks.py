@@ -288,6 +288,15 @@ def test_select_long(stored, n_select, first, recent):
     _check_select(c, q, index, _select(c, q, index, n_select, first, recent), first, recent)
 
 
+@pytest.mark.parametrize("ties", [False, True])
+@pytest.mark.parametrize("n_select", [4, 130, 255])
+def test_select_about_256_and_512_competing_blocks(n_select, ties):
+    c = Shape(4, 2, 64, [32 * (n + 3) + 1 for n in (255, 256, 257, 511, 512, 513, 700)], [(0, 4), (0, 2)])
+    index, g = _fake_index(c, 65, ties), _gen(66)
+    q = _randn(g, c.nl, c.B, 4, 64).bfloat16()
+    _check_select(c, q, index, _select(c, q, index, n_select, 1, 2), 1, 2)
+
+
 @pytest.mark.parametrize("hq,hkv", [(65, 1), (96, 1), (256, 2)])
 @pytest.mark.parametrize("stored", [[3200, 700], [64000]])
 def test_select_groups_of_many_heads(hq, hkv, stored):
