@@ -50,7 +50,7 @@ static_assert(sizeof(CopyArgs) <= 4096, "kernel arguments");
 
 __device__ __forceinline__ void move(const uint8_t* from, uint8_t* to, int bytes, int lane) {
   int at = 16 * lane;
-  for (; at + 3072 < bytes; at += 4096) {
+  for (; at + 3 * 1024 < bytes; at += 4 * 1024) {
     u4v x[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) x[i] = *reinterpret_cast<const u4v*>(from + at + 1024 * i);

@@ -464,6 +464,16 @@ def test_block_attention(hq, hkv, d, n, bits, scheme):
         assert torch.equal(out, _attend(c, q, blocks, 1.2 / math.sqrt(d)))
 
 
+@pytest.mark.parametrize("bits,scheme", [(16, "kivi"), (8, "sym"), (4, "kivi"), (2, "g64")])
+@pytest.mark.parametrize("hq,hkv,d", [(65, 1, 64), (194, 2, 128)])
+def test_block_attention_groups_of_many_heads(hq, hkv, d, bits, scheme):
+    c = Cache(hq, hkv, d, [33, 1000], [(0, bits), (1, 16)], scheme)
+    g = _gen(23)
+    q = _randn(g, c.nl, c.B, hq, d).bfloat16()
+    blocks = _lists(g, c, 20, "any")
+    _check_attend(c, q, blocks, 1.0 / math.sqrt(d), _attend(c, q, blocks, 1.0 / math.sqrt(d)))
+
+
 @pytest.mark.parametrize("scale", [-0.2, 0.0, 3.0])
 @pytest.mark.parametrize("bits,scheme", [(16, "kivi"), (8, "sym"), (4, "kivi"), (2, "g64")])
 def test_block_attention_scales(scale, bits, scheme):
